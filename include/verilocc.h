@@ -350,6 +350,95 @@ int vl_occupied_masks(vl_program *prog, const uint16_t *d_row, uint32_t *d_masks
 int vl_expand_masks(const uint32_t *words, uint64_t n_rows, uint32_t P, uint8_t *out);
 
 /*
+ * Scores of sampled tokens under the model (the factorisation of Section 3.1; with masks: decoding that keeps off occupied
+ * registers, Section 4.5, last paragraph).  A descriptor of rows of logits; every pointer in it is DEVICE memory.  Row r holds
+ * n_vocab entries at logits + r * row_stride (elements): tokens of a vocabulary, or the physical registers themselves.
+ * An entry counts if it is open.  With `occupied`, n_masks masks of ceil(n_vocab / 32) words as vl_occupied_masks writes them (set:
+ * occupied; bits from n_vocab on are ignored), row r is under mask mask_rows[r] (a number outside 0..n_masks-1: under none), or
+ * mask r if mask_rows is NULL.  With `widths`, the entries of row r are bases of tuples of widths[r] registers (0 counts as 1): entry i is
+ * open iff i .. i + widths[r] - 1 all are below n_vocab and not occupied.  What a logit that is not open holds makes no difference
+ * (it may be infinite or no number).  An open logit of minus infinity has probability 0; one of plus infinity, or no number, makes the
+ * row's results no numbers.
+ */
+enum { VL_F32 = 0, VL_F16 = 1, VL_BF16 = 2 }; /* element types of logits */
+#define VL_MAX_VOCAB (1u << 30)
+#define VL_MAX_ALTERNATIVES 32
+typedef struct {
+    const void *logits;        /* aligned to its element */
+    int dtype;                 /* VL_F32, VL_F16 or VL_BF16 */
+    uint64_t n_rows;
+    uint32_t n_vocab;          /* 1..VL_MAX_VOCAB */
+    uint64_t row_stride;       /* elements from row to row, at least n_vocab (any for a single row) */
+    const void *tokens;        /* [n_rows] the given token of every row, or NULL.  A row whose token is not one of 0..n_vocab-1 is left out */
+    uint32_t token_bytes;      /* 2: uint16 (entries of candidate rows), 4: int32, 8: int64 */
+    const uint32_t *occupied;  /* [n_masks][ceil(n_vocab / 32)] or NULL */
+    uint64_t n_masks;          /* at least n_rows if mask_rows is NULL */
+    const int32_t *mask_rows;  /* [n_rows] or NULL */
+    const uint8_t *widths;     /* [n_rows] or NULL */
+    float scale;               /* 1 / temperature; finite, above 0 */
+} vl_logits;
+
+/*
+ * For every row, with z = scale * logits and p = softmax of z over the open entries, in 32 bits: d_logprob[r] = ln p of the row's
+ * token; d_entropy[r] = -sum p ln p; d_row_stats[2 r], [2 r + 1] = the largest open logit M and L = ln sum exp(scale (logit - M)), what
+ * vl_token_logprobs_backward takes (8-byte aligned); d_top_ids and d_top_logprobs [n_rows][top], top <= VL_MAX_ALTERNATIVES: the open
+ * entries with the largest logits, largest first, the lowest number first among equals, with their ln p (entries of probability 0 by
+ * a logit of minus infinity, and logits that are no numbers, are none; what is left over is -1 and minus infinity).  Outputs that are
+ * NULL are not written; d_logprob needs tokens.
+ * A closed token has ln p = minus infinity.  A row without open entries: minus infinity for ln p, M and L, entropy 0, no alternatives.
+ * A row that is left out: ln p, M, L and entropy 0, no alternatives.
+ * Stream-ordered on `cuda_stream` of `device`, no synchronisation, no allocation, no working memory: calls may run side by side.
+ * n_rows == 0 is a no-op.  Errors: INVALID_ARG, CUDA.
+ */
+int vl_token_logprobs(int device, const vl_logits *x, float *d_logprob, float *d_entropy, float *d_row_stats, uint32_t top,
+                      int32_t *d_top_ids, float *d_top_logprobs, void *cuda_stream);
+
+/*
+ * The gradient of vl_token_logprobs: from d_g_logprob[r] and d_g_entropy[r] (a loss's derivatives to ln p and entropy of row r; NULL: 0)
+ * to d_dlogits (the type of the logits, rows out_stride elements apart), which is written whole: 0 where an entry is not open and in
+ * rows that are left out or have nothing open.  ln p of a token that is not open is constant and hands nothing on.  d_row_stats, and
+ * d_entropy where d_g_entropy is given, are the forward call's outputs for the same descriptor.  d_dlogits may be the logits themselves
+ * (with the same stride), and overlaps them in no other way.  Each value is rounded once.  Stream order, errors: as vl_token_logprobs.
+ */
+int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_row_stats, const float *d_entropy,
+                               const float *d_g_logprob, const float *d_g_entropy, void *d_dlogits, uint64_t out_stride,
+                               void *cuda_stream);
+
+/*
+ * The verdicts as a training signal (Section 6): a clipped policy objective over sampled candidates.  A candidate's reward is
+ * 1 if it passes, else 0, less pair_cost for each conflict pair and bank_cost for each bank conflict of its verdict; its
+ * advantage A is the reward less the mean over the samples of its program, with `normalise` divided by their standard deviation (of the
+ * population) + eps.  Per token of a candidate, with r = exp(logprob - old): the loss -min(r A, clip(r, 1 - clip_lo, 1 + clip_hi) A), plus
+ * kl (exp q - q - 1) with q = ref - logprob.  The token weighs 1 / (candidates * tokens of its candidate), or with `per_token`
+ * 1 / tokens of all.  The advantage is a constant of the derivative.
+ */
+typedef struct {
+    double pair_cost, bank_cost;
+    double eps;                 /* above 0 with normalise */
+    double clip_lo, clip_hi;    /* at least 0; clip_lo >= 1 or an infinite clip_hi: that side is not clipped */
+    double kl;                  /* 0: no reference model */
+    int normalise, per_token;
+} vl_policy_rules;
+
+/* Bytes of working memory of a vl_policy_loss call. */
+uint64_t vl_policy_work(uint64_t n_candidates, uint64_t n_tokens);
+
+/*
+ * For n programs, program j with K[j] candidates whose verdicts are d_out[j] (as vl_verify wrote them, 16-byte aligned; d_out and K are HOST
+ * arrays, everything else DEVICE): the candidates of all programs in order own the tokens d_token_off[c] .. d_token_off[c + 1] - 1
+ * ([candidates + 1], ascending, 8-byte aligned; a candidate may have none) of the n_tokens entries of d_logprob, d_old_logprob (NULL: d_logprob
+ * itself) and d_ref_logprob (read if kl is not 0).  *d_loss receives the sum of the weighted token losses, d_advantage (or NULL) the candidates'
+ * advantages, d_g_logprob [n_tokens] (or NULL) the derivative of the loss to every ln p, 0 for tokens that no candidate owns.
+ * A token with a ln p of minus infinity on any side adds nothing to the loss and has derivative 0, though it counts as a token.  d_work: at
+ * least vl_policy_work bytes of device memory, 8-byte aligned, the call's own until its work is done.  Equal inputs give equal results, bit for bit.
+ * Stream-ordered on `cuda_stream` of `device`, no synchronisation, no allocation.  Errors: INVALID_ARG, CUDA.
+ */
+int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d_out, const uint64_t *K, const int64_t *d_token_off,
+                   uint64_t n_tokens, const float *d_logprob, const float *d_old_logprob, const float *d_ref_logprob,
+                   const vl_policy_rules *rules, float *d_loss, float *d_advantage, float *d_g_logprob, void *d_work,
+                   uint64_t work_bytes, void *cuda_stream);
+
+/*
  * Block-level liveness without any allocation.  (The paper has no counterpart; this exists for
  * hosts that cannot allocate device memory when they call in: a process that handed all of HBM to
  * its own pools at start-up, a plugin under a memory budget it does not control, or a loop that

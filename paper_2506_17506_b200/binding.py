@@ -7,6 +7,8 @@ Importing this module fails loudly when the library has not been built
 """
 from __future__ import annotations
 
+import collections
+import contextlib
 import ctypes as C
 import os
 
@@ -34,7 +36,8 @@ EXPORTS = ["vl_program_create", "vl_program_destroy", "vl_program_set_option", "
            "vl_kernel_launches", "vl_kernel_times", "vl_last_cuda_error", "vl_strerror", "vl_block_liveness_static",
            "vl_resample_stats", "vl_verify_until_pass", "vl_program_set_constraints", "vl_diagnose", "vl_occupied_masks",
            "vl_expand_masks",
-           "vl_dict_layout", "vl_verify_dict"]
+           "vl_dict_layout", "vl_verify_dict",
+           "vl_token_logprobs", "vl_token_logprobs_backward", "vl_policy_work", "vl_policy_loss"]
 
 VERDICT_DTYPE = np.dtype([("flags", "<u4"), ("first_violation_instr", "<i4"),
                           ("conflict_pairs", "<u4"), ("bank_conflicts", "<u4")])
@@ -107,6 +110,31 @@ _lib.vl_expand_masks.restype = C.c_int
 _lib.vl_expand_masks.argtypes = [C.c_void_p, C.c_uint64, C.c_uint32, C.c_void_p]
 _lib.vl_program_set_constraints.restype = C.c_int
 _lib.vl_program_set_constraints.argtypes = [C.c_void_p, C.c_void_p]
+VL_F32, VL_F16, VL_BF16 = 0, 1, 2
+VL_MAX_VOCAB = 1 << 30
+VL_MAX_ALTERNATIVES = 32
+
+
+class vl_logits(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int), ("n_rows", C.c_uint64), ("n_vocab", C.c_uint32),
+                ("row_stride", C.c_uint64), ("tokens", C.c_void_p), ("token_bytes", C.c_uint32), ("occupied", C.c_void_p),
+                ("n_masks", C.c_uint64), ("mask_rows", C.c_void_p), ("widths", C.c_void_p), ("scale", C.c_float)]
+
+
+class vl_policy_rules(C.Structure):
+    _fields_ = [(n, C.c_double) for n in ("pair_cost", "bank_cost", "eps", "clip_lo", "clip_hi", "kl")] + [
+        ("normalise", C.c_int), ("per_token", C.c_int)]
+
+
+_lib.vl_token_logprobs.restype = C.c_int
+_lib.vl_token_logprobs.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 3
+_lib.vl_token_logprobs_backward.restype = C.c_int
+_lib.vl_token_logprobs_backward.argtypes = [C.c_int] + [C.c_void_p] * 6 + [C.c_uint64, C.c_void_p]
+_lib.vl_policy_work.restype = C.c_uint64
+_lib.vl_policy_work.argtypes = [C.c_uint64, C.c_uint64]
+_lib.vl_policy_loss.restype = C.c_int
+_lib.vl_policy_loss.argtypes = ([C.c_int, C.c_uint32] + [C.c_void_p] * 3 + [C.c_uint64] + [C.c_void_p] * 8 +
+                                [C.c_uint64, C.c_void_p])
 SAMPLE_STATS_DTYPE = np.dtype([("first_pass", "<u8"), ("n_pass", "<u8")])
 
 
@@ -334,14 +362,17 @@ class Program:
         hist[: self.n_banks] = host[8: o_kinds].view(np.uint64)[:n_banks]
         return rec.copy().view(np.uint32).reshape(-1, 3), n, host[o_kinds: o_kinds + self.n_instrs].copy(), hist
 
-    def vl_occupied_masks(self, row, P: int, stream=None):
+    def vl_occupied_masks(self, row, P: int, stream=None, words: bool = False):
         """uint8 numpy array [n_instrs, P]: registers the definitions of every instruction must keep off,
-        for one candidate (CUDA uint16 tensor; entries >= P mean "no register yet")."""
+        for one candidate (CUDA uint16 tensor; entries >= P mean "no register yet").  With ``words`` the masks as they
+        are on the device, a CUDA int32 tensor [n_instrs, ceil(P / 32)] (what vl_token_logprobs takes), without waiting."""
         import torch
         W = (P + 31) // 32
         masks = torch.empty((max(self.n_instrs, 1), W), dtype=torch.int32, device=row.device)
         self._check(_lib.vl_occupied_masks(self._h, row.data_ptr(), masks.data_ptr(), _stream_ptr(stream)),
                     "vl_occupied_masks")
+        if words:
+            return masks[:self.n_instrs]
         words = _to_host(masks, stream)
         out = np.empty((self.n_instrs, P), dtype=np.uint8)
         self._check(_lib.vl_expand_masks(words.ctypes.data, self.n_instrs, P, out.ctypes.data), "vl_expand_masks")
@@ -431,6 +462,162 @@ def vl_resample_stats(outs, ks=(1, 10, 100), device: int = 0, stream=None):
     s = host[2 * m:].copy()
     return rec, dict(n_cases=int(s[0]), n_solved=int(s[1]), sum_tries=int(s[2]), max_tries=int(s[3]),
                      pass_at=[int(x) for x in s[4:4 + len(ks)]])
+
+
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy row_stats top_ids top_logprobs")
+
+
+def _need(ok: bool, where: str, what: str):
+    if not ok:
+        raise VlError(VL_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _on(stream, device):
+    """(the stream's pointer, a context in which torch's allocations belong to it); None: the device's current stream."""
+    import torch
+    if stream is None:
+        return C.c_void_p(torch.cuda.current_stream(device).cuda_stream), contextlib.nullcontext()
+    ptr = int(getattr(stream, "cuda_stream", stream))
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(ptr, device=device) if ptr else torch.cuda.default_stream(device)
+    return C.c_void_p(ptr), torch.cuda.stream(stream)
+
+
+def _vector(t, name, where, like, n, dtypes):
+    """Address of a contiguous vector of n entries on the device of `like`; None for None."""
+    if t is None:
+        return None
+    _need(t.device == like.device and t.dtype in dtypes and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), where,
+          f"{name}: a contiguous vector of {n} entries of {' or '.join(str(d)[6:] for d in dtypes)} on {like.device}")
+    return t.data_ptr() or None
+
+
+def _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale):
+    import torch
+    types = {torch.float32: VL_F32, torch.float16: VL_F16, torch.bfloat16: VL_BF16}
+    _need(logits.is_cuda and logits.dtype in types and logits.dim() == 2, where, "logits: a CUDA matrix of float32, float16 or bfloat16")
+    R, V = logits.shape
+    _need(1 <= V <= VL_MAX_VOCAB, where, f"logits: 1 to {VL_MAX_VOCAB} entries per row")
+    _need(V == 1 or logits.stride(1) == 1, where, "logits: entries of a row side by side")
+    _need(R <= 1 or logits.stride(0) >= V, where, "logits: rows that do not overlap")
+    x = vl_logits(logits=logits.data_ptr(), dtype=types[logits.dtype], n_rows=R, n_vocab=V, row_stride=logits.stride(0) if R > 1 else V,
+                  scale=scale)
+    x.tokens = _vector(tokens, "tokens", where, logits, R, (torch.uint16, torch.int16, torch.int32, torch.int64))
+    x.token_bytes = tokens.element_size() if tokens is not None else 0
+    x.mask_rows = _vector(mask_rows, "mask_rows", where, logits, R, (torch.int32,))
+    x.widths = _vector(widths, "widths", where, logits, R, (torch.uint8,))
+    if occupied is not None:
+        W = (V + 31) // 32
+        _need(occupied.device == logits.device and occupied.dtype in (torch.int32, torch.uint32) and occupied.dim() == 2 and
+              occupied.shape[1] == W and occupied.is_contiguous(), where,
+              f"occupied: a contiguous int32 matrix with {W} words per mask on {logits.device}")
+        _need(mask_rows is not None or occupied.shape[0] >= R, where, "occupied: a mask for every row, or mask_rows")
+        _need(occupied.shape[0] > 0 or R == 0, where, "occupied: at least one mask")
+        x.occupied, x.n_masks = occupied.data_ptr(), occupied.shape[0]
+    _need(occupied is not None or mask_rows is None, where, "mask_rows: the numbers of which masks?")
+    return x
+
+
+def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths=None, scale: float = 1.0, top: int = 0, stream=None):
+    """Scores of rows of logits (CUDA [rows, entries], float32 / float16 / bfloat16, entries side by side): the log
+    probability of the given token of every row (``tokens``: uint16, int32 or int64; a row whose token is no entry is
+    left out), the entropy, what the backward call takes, and the ``top`` best entries with their log probabilities.
+    ``occupied``: masks as ``vl_occupied_masks(..., words=True)`` gives them, mask ``mask_rows[r]`` for row r (or mask r);
+    ``widths``: registers of the tuple that row r places; ``scale``: 1 / temperature.  No wait.
+    Returns TokenLogprobs(logprob, entropy, row_stats [rows, 2], top_ids, top_logprobs); what was not asked for is None."""
+    import torch
+    where = "vl_token_logprobs"
+    x = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
+    _need(0 <= top <= VL_MAX_ALTERNATIVES, where, f"top: at most {VL_MAX_ALTERNATIVES} alternatives")
+    R, dev = logits.shape[0], logits.device
+    ptr, scope = _on(stream, dev)
+    with scope:
+        f = torch.empty(R * ((4 if tokens is not None else 3) + 2 * top), dtype=torch.float32, device=dev)   # one allocation
+    stats, rest = f[:2 * R].view(R, 2), f[2 * R:]
+    ent, rest = rest[:R], rest[R:]
+    lp = ids = lps = None
+    if tokens is not None:
+        lp, rest = rest[:R], rest[R:]
+    if top:
+        ids, lps = rest[:R * top].view(torch.int32).view(R, top), rest[R * top:].view(R, top)
+    rc = _lib.vl_token_logprobs(dev.index, C.byref(x), lp.data_ptr() if lp is not None else None, ent.data_ptr(), stats.data_ptr(), top,
+                                ids.data_ptr() if top else None, lps.data_ptr() if top else None, ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return TokenLogprobs(lp, ent, stats, ids, lps)
+
+
+def vl_token_logprobs_backward(logits, tokens, row_stats, g_logprob=None, entropy=None, g_entropy=None, occupied=None, mask_rows=None,
+                               widths=None, scale: float = 1.0, out=None, stream=None):
+    """Gradient to the logits of a loss whose derivatives to the log probabilities and entropies of ``vl_token_logprobs`` are
+    ``g_logprob`` and ``g_entropy`` (float32 [rows]; a single number in a tensor of stride 0 has to be made contiguous).
+    ``row_stats`` and ``entropy`` come from that call, the other arguments are the ones it had.  ``out``: where to (the logits
+    themselves, or a matrix of their shape and type that does not overlap them); a new matrix without it."""
+    import torch
+    where = "vl_token_logprobs_backward"
+    x = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
+    R, V = logits.shape
+    f32 = (torch.float32,)
+    _need(row_stats.device == logits.device and row_stats.dtype == torch.float32 and tuple(row_stats.shape) == (R, 2) and
+          row_stats.is_contiguous(), where, "row_stats: the contiguous float32 [rows, 2] of vl_token_logprobs")
+    g = _vector(g_logprob, "g_logprob", where, logits, R, f32)
+    h = _vector(g_entropy, "g_entropy", where, logits, R, f32)
+    ent = _vector(entropy, "entropy", where, logits, R, f32)
+    _need(g_logprob is None or tokens is not None, where, "g_logprob: the log probabilities of which tokens?")
+    _need(g_entropy is None or entropy is not None, where, "entropy: needed with g_entropy")
+    ptr, scope = _on(stream, logits.device)
+    if out is None:
+        with scope:
+            out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
+    _need(out.device == logits.device and out.dtype == logits.dtype and out.shape == logits.shape and (V == 1 or out.stride(1) == 1) and
+          (R <= 1 or out.stride(0) >= V), where, "out: a matrix of the logits' shape and type, entries of a row side by side")
+    if out.data_ptr() == logits.data_ptr():
+        _need(R <= 1 or out.stride(0) == logits.stride(0), where, "out: the logits themselves have the logits' stride")
+    elif R:
+        size = logits.element_size()
+        ends = [t.data_ptr() + ((R - 1) * t.stride(0) + V) * size for t in (logits, out)]
+        _need(out.data_ptr() >= ends[0] or logits.data_ptr() >= ends[1], where, "out: overlaps the logits")
+    rc = _lib.vl_token_logprobs_backward(logits.device.index, C.byref(x), row_stats.data_ptr(), ent, g, h, out.data_ptr(),
+                                         out.stride(0) if R > 1 else V, ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return out
+
+
+def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None, pair_cost: float = 0.0, bank_cost: float = 0.0,
+                   normalise: bool = True, eps: float = 1e-6, clip_lo: float = 0.2, clip_hi: float = 0.2, kl: float = 0.0,
+                   per_token: bool = False, stream=None):
+    """The verdicts as a training signal.  ``outs``: verdicts of the samples of every program (as ``vl_verify_batch`` returns
+    them); ``token_off``: CUDA int64, candidate c (over all programs) owns the tokens token_off[c] .. token_off[c + 1] - 1 of
+    ``logprob`` (float32), of ``old_logprob`` (under the model that sampled; None: the same) and ``ref_logprob`` (with ``kl``).
+    Returns (loss, a float32 scalar tensor; advantages of the candidates; derivative of the loss to ``logprob``).  No wait."""
+    import torch
+    where = "vl_policy_loss"
+    n = len(outs)
+    _need(logprob.is_cuda and logprob.dim() == 1, where, "logprob: a CUDA vector")
+    for o in outs:
+        _need(o.device == logprob.device and o.dtype == torch.int32 and o.dim() == 2 and o.shape[1] == 4 and o.is_contiguous(), where,
+              f"outs: contiguous int32 verdicts [samples, 4] on {logprob.device}")
+    N, T, dev = sum(o.shape[0] for o in outs), logprob.shape[0], logprob.device
+    f32 = (torch.float32,)
+    lp = _vector(logprob, "logprob", where, logprob, T, f32)
+    old = _vector(old_logprob, "old_logprob", where, logprob, T, f32)
+    ref = _vector(ref_logprob, "ref_logprob", where, logprob, T, f32)
+    off = _vector(token_off, "token_off", where, logprob, N + 1, (torch.int64,))
+    rules = vl_policy_rules(pair_cost, bank_cost, eps, clip_lo, clip_hi, kl, int(normalise), int(per_token))
+    op = (C.c_void_p * max(n, 1))(*[o.data_ptr() or None for o in outs])
+    Ks = (C.c_uint64 * max(n, 1))(*[o.shape[0] for o in outs])
+    size = int(_lib.vl_policy_work(N, T))
+    ptr, scope = _on(stream, dev)
+    with scope:
+        work = torch.empty(size, dtype=torch.uint8, device=dev)
+        f = torch.empty(1 + N + T, dtype=torch.float32, device=dev)
+    loss, adv, g = f[0], f[1:1 + N], f[1 + N:]
+    rc = _lib.vl_policy_loss(dev.index, n, op, Ks, off, T, lp, old, ref, C.byref(rules), loss.data_ptr(), adv.data_ptr(), g.data_ptr(),
+                             work.data_ptr(), size, ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return loss, adv, g
 
 
 def verdicts_to_numpy(t) -> np.ndarray:
