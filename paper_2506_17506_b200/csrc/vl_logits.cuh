@@ -5,8 +5,6 @@
 
 #include "vl_internal.cuh"
 
-namespace {
-
 // A checked vl_logits in the form the kernels take.
 struct LogitRows {
     const void *x;
@@ -20,13 +18,177 @@ struct LogitRows {
     const uint8_t *widths;
     float scale;
 };
+// Checks a descriptor: VL_OK and the kernels' form of it, or an error.
+int vl_logit_rows(const vl_logits *x, LogitRows *out);
 
+namespace {
+
+template <typename T> __device__ __forceinline__ T lowest_bits();  // minus infinity
+template <> __device__ __forceinline__ float lowest_bits<float>() { return __int_as_float(0xFF800000); }
+template <> __device__ __forceinline__ __half lowest_bits<__half>() { return __ushort_as_half(0xFC00); }
+template <> __device__ __forceinline__ __nv_bfloat16 lowest_bits<__nv_bfloat16>() { return __ushort_as_bfloat16(0xFF80); }
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_f32(float &d, float x) { d = x; }
 __device__ __forceinline__ void from_f32(__half &d, float x) { d = __float2half_rn(x); }
 __device__ __forceinline__ void from_f32(__nv_bfloat16 &d, float x) { d = __float2bfloat16_rn(x); }
+
+template <typename T> constexpr int EPV = 16 / (int)sizeof(T);  // elements of a 16-byte vector
+template <typename T> constexpr uint32_t MINUS_INF2 = sizeof(T) == 4 ? 0xFF800000u : 0u;
+template <> constexpr uint32_t MINUS_INF2<__half> = 0xFC00FC00u;
+template <> constexpr uint32_t MINUS_INF2<__nv_bfloat16> = 0xFF80FF80u;
+
+__device__ __forceinline__ void unpack(const uint4 &r, float (&x)[4], float)
+{
+    x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+}
+__device__ __forceinline__ void unpack(const uint4 &r, float (&x)[8], __nv_bfloat16)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ void unpack(const uint4 &r, float (&x)[8], __half)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        __half2 h;
+        memcpy(&h, &w[j], 4);
+        const float2 f = __half22float2(h);
+        x[2 * j] = f.x; x[2 * j + 1] = f.y;
+    }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __half)
+{
+    const __half2 h = __floats2half2_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    uint32_t w;
+    memcpy(&w, &h, 4);
+    return w;
+}
+__device__ __forceinline__ uint4 pack(const float (&x)[4], float)
+{
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+}
+template <typename T>
+__device__ __forceinline__ uint4 pack(const float (&x)[8], T t)
+{
+    return make_uint4(pack2(x[0], x[1], t), pack2(x[2], x[3], t), pack2(x[4], x[5], t), pack2(x[6], x[7], t));
+}
+// The largest of a vector's elements, of those that are numbers.
+__device__ __forceinline__ float vector_max(const uint4 &r, float)
+{
+    return fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w)));
+}
+__device__ __forceinline__ float vector_max(const uint4 &r, __half)
+{
+    __half2 h[4];
+    memcpy(h, &r, 16);
+    const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+__device__ __forceinline__ float vector_max(const uint4 &r, __nv_bfloat16)
+{
+    __nv_bfloat162 h[4];
+    memcpy(h, &r, 16);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return fmaxf(__low2float(m), __high2float(m));
+}
+
+// A row as 16-byte vectors: vector v holds the entries first(v) .. first(v) + EPV - 1; the first and the last vector may hold
+// entries of no row, which are read one by one around them.
+template <typename T>
+struct RowVectors {
+    const T *row;
+    uint32_t V, lead, n;  // entries; entries of the first vector in front of the row; vectors
+    __device__ __forceinline__ RowVectors(const T *x, uint32_t entries)
+        : row(x), V(entries), lead((uint32_t)((uintptr_t)x & 15) / (uint32_t)sizeof(T)), n((lead + entries + EPV<T> - 1) / EPV<T>) {}
+    __device__ __forceinline__ int first(uint32_t v) const { return (int)(v * EPV<T>) - (int)lead; }
+    __device__ __forceinline__ bool whole(uint32_t v) const { return (v > 0 || lead == 0) && (v + 1) * EPV<T> <= lead + V; }
+    __device__ __forceinline__ const uint4 *at(uint32_t v) const
+    {
+        return reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(row) & ~(uintptr_t)15) + v;
+    }
+    // Entries that are in the row; minus infinity elsewhere.
+    __device__ __forceinline__ uint4 part(uint32_t v) const
+    {
+        T e[EPV<T>];
+#pragma unroll
+        for (int j = 0; j < EPV<T>; ++j) {
+            const int i = first(v) + j;
+            e[j] = (uint32_t)i < V ? row[i] : lowest_bits<T>();
+        }
+        uint4 r;
+        memcpy(&r, e, 16);
+        return r;
+    }
+};
+
+// Entries whose bit is set to minus infinity.
+template <typename T>
+__device__ __forceinline__ void close_entries(uint4 &r, uint32_t bits)
+{
+    uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 4) {
+            if ((bits >> j) & 1) w[j] = MINUS_INF2<T>;
+        } else {
+            const uint32_t m = ((bits >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((bits >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u);
+            w[j] = (w[j] & ~m) | (MINUS_INF2<T> & m);
+        }
+    }
+    r = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Two 32-bit numbers side by side: one instruction works on both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 both(float a, float b)
+{
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void apart(f32x2 r, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(r)); }
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b)
+{
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
+{
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// max that keeps what is no number
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 
 // Token of row r, or -1 where the row is left out (no entry of that number).  Without tokens every row counts, with entry V:
 // one that no index reaches.
@@ -78,6 +240,14 @@ struct RowMask {
         }
         return m;
     }
+    // Closed entries among i .. i + n - 1 (n <= 8; i may be negative: those in front of the row are closed), as the low bits.
+    __device__ __forceinline__ uint32_t closed_from(int i, int n) const
+    {
+        const int w = i >> 5, s = i & 31;
+        const uint32_t a = w < 0 ? 0xFFFFFFFFu : closed((uint32_t)w);
+        const uint32_t b = s + n > 32 ? closed((uint32_t)(w + 1)) : 0u;
+        return __funnelshift_r(a, b, s) & ((1u << n) - 1);
+    }
     __device__ __forceinline__ bool is_closed(uint32_t i) const { return (closed(i >> 5) >> (i & 31)) & 1; }
 };
 __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
@@ -95,9 +265,6 @@ __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
 }
 
 }  // namespace
-
-// Checks a descriptor: VL_OK and the kernels' form of it, or an error.
-int vl_logit_rows(const vl_logits *x, LogitRows *out);
 
 // Makes `device` current and puts the caller's device back at the end of the call.
 struct DeviceScope {

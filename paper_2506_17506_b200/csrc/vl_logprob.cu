@@ -1,36 +1,29 @@
-// Log probabilities of given tokens, entropy and best alternatives of rows of logits, and their gradient: how likely the model
-// behind the candidates found them (the autoregressive factorisation of Section 3.1), under the masks of vl_occupied_masks where
-// it decodes around occupied registers (Section 4.5).
+// Log probabilities of given tokens, entropy and best alternatives of rows of logits: how likely the model behind the candidates found
+// them (the factorisation of Section 3.1), under the masks of vl_occupied_masks where it decodes around occupied registers
+// (Section 4.5).
 //
-// With z = scale x over the open entries, M = max x, e_i = exp(scale (x_i - M)), L = ln sum e_i:
-//   log p_i = scale (x_i - M) - L,   entropy = L - sum e_i scale (x_i - M) / sum e_i
-// Both terms of the entropy are non-negative, so nothing cancels; the sums are held in 32 bits.
+// With z = scale x over the open entries, M = max x, d_i = x_i - M, e_i = exp(scale d_i):
+//   L = ln sum e_i,   log p_i = scale d_i - L,   entropy = L - scale (sum e_i d_i) / (sum e_i)
+// Both terms of the entropy are non-negative, so nothing cancels, and M apart from L keeps digits where the logits are far from zero.
+// One pass: a thread holds the largest logit so far and the two sums in 32 bits, and scales the sums when the largest one rises.
+//
+// What bounds it: reading the logits once; per element also one exponential (16 a clock and multiprocessor: 119 us for the 5.4e8 of
+// 4,096 rows of 131,072, against 164 us for their bytes in bf16) and about six more instructions, of which those on pairs of
+// numbers (f32x2) and of 16-bit halves do two elements at once.
+#include <cooperative_groups.h>
+
 #include "vl_logits.cuh"
 
 namespace {
 
-constexpr uint32_t LP_THREADS = 256;
+namespace cg = cooperative_groups;
+typedef unsigned long long key_t64;
 
-__device__ __forceinline__ float warp_max(float v)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
-    return v;
-}
-__device__ __forceinline__ float warp_sum(float v)
-{
-#pragma unroll
-    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
-}
-
-// A value and its place as one key: larger values first, lower places first among equals (zeros of both signs are equal).
-__device__ __forceinline__ unsigned long long rank_key(float x, uint32_t i)
-{
-    const uint32_t b = __float_as_uint(x + 0.0f);
-    const uint32_t order = (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-    return ((unsigned long long)order << 32) | (0xFFFFFFFFu - i);
-}
+constexpr float LOWEST = -3.402823466e38f;
+// Stands for minus infinity in a difference: times scale >= 1e-20 its exponential is 0, and 0 times it is 0.
+constexpr float FAR_BELOW = -1e30f;
+constexpr uint32_t TOP_MAX = VL_MAX_ALTERNATIVES;
+constexpr uint32_t MAX_PARTS = 8;  // thread blocks of a row
 
 struct ScoreOut {
     float *logprob, *entropy, *stats;
@@ -39,125 +32,347 @@ struct ScoreOut {
     float *lps;
 };
 
+// ---- values with their places, as keys: larger values first, lower places first among equals (zeros of both signs are equal)
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t b = __float_as_uint(x + 0.0f);
+    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
+}
+__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o); }
+__device__ __forceinline__ key_t64 rank_key(float x, uint32_t i) { return ((key_t64)ordered(x) << 32) | (0xFFFFFFFFu - i); }
+__device__ __forceinline__ uint32_t key_place(key_t64 k) { return 0xFFFFFFFFu - (uint32_t)k; }
+__device__ __forceinline__ float key_value(key_t64 k) { return from_ordered((uint32_t)(k >> 32)); }
+
+__device__ __forceinline__ key_t64 exchange(key_t64 k, uint32_t d, bool larger)
+{
+    const key_t64 other = __shfl_xor_sync(0xffffffffu, k, d);
+    return (k > other) == larger ? k : other;
+}
+// A warp's 32 keys, largest first.
+__device__ __forceinline__ key_t64 sort32(key_t64 k, uint32_t lane)
+{
+#pragma unroll
+    for (uint32_t n = 2; n <= 32; n *= 2)
+#pragma unroll
+        for (uint32_t d = n / 2; d; d /= 2) k = exchange(k, d, ((lane & d) == 0) == ((lane & n) == 0));
+    return k;
+}
+// The first 32 of two sorted lists of 32.
+__device__ __forceinline__ key_t64 merge32(key_t64 a, key_t64 b, uint32_t lane)
+{
+    const key_t64 r = __shfl_sync(0xffffffffu, b, 31 - lane);
+    key_t64 k = a > r ? a : r;
+#pragma unroll
+    for (uint32_t d = 16; d; d /= 2) k = exchange(k, d, (lane & d) == 0);
+    return k;
+}
+// NW sorted lists in shared memory; the first 32 of all of them end up in list 0.  Every warp of the block calls it.
+template <int NW>
+__device__ __forceinline__ void merge_lists(key_t64 (*lists)[32], uint32_t warp, uint32_t lane)
+{
+#pragma unroll
+    for (uint32_t half = NW / 2; half; half /= 2) {
+        __syncthreads();
+        if (warp < half) lists[warp][lane] = merge32(lists[warp][lane], lists[warp + half][lane], lane);
+    }
+    __syncthreads();
+}
+
+// ---- running sums
+struct Sums {
+    float m, s, t;  // largest logit; sum e, sum e d relative to it
+};
+__device__ __forceinline__ void raise(Sums &a, float m, float c)
+{
+    const float d = fmaxf(a.m - m, FAR_BELOW), f = ex2(d * c);
+    a.t = (a.t + a.s * d) * f;
+    a.s *= f;
+    a.m = m;
+}
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+__device__ __forceinline__ void warp_join(Sums &a, float c)
+{
+    raise(a, from_ordered(__reduce_max_sync(0xffffffffu, ordered(a.m))), c);
+    a.s = warp_sum(a.s);
+    a.t = warp_sum(a.t);
+}
+
+// A thread's state over the vectors of its stripe.
+struct Run {
+    float m;
+    f32x2 s, t;
+    uint32_t best;  // vector in which m was met first
+};
+template <typename T, int N, bool TOP>
+__device__ __forceinline__ void take(Run &a, const uint4 (&raw)[N], uint32_t v, uint32_t step, float c)
+{
+    float vm[N], m;
+#pragma unroll
+    for (int u = 0; u < N; ++u) vm[u] = vector_max(raw[u], T{});
+    m = vm[0];
+#pragma unroll
+    for (int u = 1; u < N; ++u) m = fmaxf(m, vm[u]);
+    if (m > a.m) {
+        const float d = fmaxf(a.m - m, FAR_BELOW), f = ex2(d * c);
+        a.t = mul2(fma2(a.s, both(d, d), a.t), both(f, f));
+        a.s = mul2(a.s, both(f, f));
+        a.m = m;
+        if (TOP) {
+#pragma unroll
+            for (int u = N - 1; u >= 0; --u)
+                if (vm[u] == m) a.best = v + u * step;
+        }
+    }
+    const float base = fmaxf(a.m, LOWEST);  // (nothing but impossible entries so far)
+    const f32x2 low = both(-base, -base), c2 = both(c, c);
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        float x[EPV<T>];
+        unpack(raw[u], x, T{});
+#pragma unroll
+        for (int j = 0; j < EPV<T>; j += 2) {
+            float d0, d1, y0, y1;
+            apart(add2(both(x[j], x[j + 1]), low), d0, d1);
+            const f32x2 d = both(max_nan(d0, FAR_BELOW), max_nan(d1, FAR_BELOW));
+            apart(mul2(d, c2), y0, y1);
+            const f32x2 e = both(ex2(y0), ex2(y1));
+            a.s = add2(a.s, e);
+            a.t = fma2(e, d, a.t);
+        }
+    }
+}
+
 __device__ __forceinline__ void empty_row(const ScoreOut &o, uint64_t r, bool left_out, uint32_t tid, uint32_t nt)
 {
     const float inf = __int_as_float(0x7f800000);
     if (tid == 0) {
         if (o.logprob) o.logprob[r] = left_out ? 0.0f : -inf;
         if (o.entropy) o.entropy[r] = 0.0f;
-        if (o.stats) o.stats[2 * r] = o.stats[2 * r + 1] = left_out ? 0.0f : -inf;
+        if (o.stats) *reinterpret_cast<float2 *>(o.stats + 2 * r) = left_out ? make_float2(0.0f, 0.0f) : make_float2(-inf, -inf);
     }
     for (uint32_t j = tid; j < o.top; j += nt) { o.ids[r * o.top + j] = -1; o.lps[r * o.top + j] = -inf; }
 }
 
-// One block per row: the maximum, the sums, then the alternatives one by one, each a pass over the row.
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) k_score(const LogitRows q, const ScoreOut o)
+// Keys of a vector's entries that are no smaller than `least` and no impossible ones, handed to f.
+template <typename T, typename F>
+__device__ __forceinline__ void each_key(const uint4 &raw, int first, key_t64 least, F &&f)
 {
-    __shared__ float s_a[8], s_b[8];
-    __shared__ unsigned long long s_k[8];
+    const float inf = __int_as_float(0x7f800000), floor = least ? key_value(least) : -inf;
+    float x[EPV<T>];
+    unpack(raw, x, T{});
+#pragma unroll
+    for (int j = 0; j < EPV<T>; ++j)
+        if (x[j] >= floor && x[j] > -inf) {
+            const key_t64 k = rank_key(x[j], (uint32_t)(first + j));
+            if (k >= least) f(k);
+        }
+}
+
+template <typename T, bool MASKED>
+__device__ __forceinline__ uint4 fetch(const RowVectors<T> &x, const RowMask &mask, uint32_t v)
+{
+    uint4 raw = x.whole(v) ? *x.at(v) : x.part(v);
+    if (MASKED) close_entries<T>(raw, mask.closed_from(x.first(v), EPV<T>));
+    return raw;
+}
+
+constexpr uint32_t CAND = 512;  // candidates for the alternatives of a part
+
+// The alternatives one by one, each a pass over the part: for rows whose best entries are crowded into a few threads' stripes.
+template <typename T, bool MASKED, int NT>
+__device__ __noinline__ void alternatives_one_by_one(const T *row, uint32_t V, const RowMask &mask, uint32_t v0, uint32_t v1, uint32_t top,
+                                                     key_t64 (*lists)[32])
+{
+    const RowVectors<T> x(row, V);
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    key_t64 last = ~0ull, mine = 0;
+    for (uint32_t j = 0; j < top; ++j) {
+        key_t64 best = 0;
+        for (uint32_t v = v0 + threadIdx.x; v < v1; v += NT)
+            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), best, [&](key_t64 k) { if (k < last) best = k; });
+        for (int d = 16; d; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
+        __syncthreads();
+        if (lane == 0) lists[0][warp] = best;
+        __syncthreads();
+        for (uint32_t w = 0; w < NT / 32; ++w) best = max(best, lists[0][w]);
+        if (lane == j) mine = best;
+        last = best;
+    }
+    __syncthreads();
+    if (warp == 0) lists[0][lane] = mine;
+    __syncthreads();
+}
+
+// A part's 32 first keys into lists[0].  The k-th of the threads' best keys bounds the k-th of all from below, and only the k threads
+// at or above it can have entries that are no smaller: their stripes alone are read again (from L2).
+template <typename T, bool MASKED, int NT>
+__device__ __forceinline__ void alternatives(const RowVectors<T> &x, const RowMask &mask, uint32_t v0, uint32_t v1, const Run &a, uint32_t top,
+                                             key_t64 (*lists)[32], key_t64 *cand, uint32_t *n_cand)
+{
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const float inf = __int_as_float(0x7f800000);
-    for (uint64_t r = blockIdx.x; r < q.n_rows; r += gridDim.x) {
+    key_t64 mine = 0;
+    if (a.best < v1)
+        each_key<T>(fetch<T, MASKED>(x, mask, a.best), x.first(a.best), 0ull, [&](key_t64 k) { if (k > mine) mine = k; });
+    lists[warp][lane] = sort32(mine, lane);
+    if (tid == 0) *n_cand = 0;
+    merge_lists<NT / 32>(lists, warp, lane);
+    const key_t64 least = lists[0][top - 1];
+    for (uint32_t j = warp; j < top; j += NT / 32) {
+        const key_t64 k = lists[0][j];
+        if (!k) break;
+        const uint32_t owner = ((key_place(k) + x.lead) / EPV<T> - v0) % NT;
+        for (uint32_t v = v0 + owner + lane * NT; v < v1; v += 32 * NT)
+            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), least, [&](key_t64 q) {
+                const uint32_t at = atomicAdd(n_cand, 1u);
+                if (at < CAND) cand[at] = q;
+            });
+    }
+    __syncthreads();
+    const uint32_t n = *n_cand;
+    if (n > CAND) {
+        alternatives_one_by_one<T, MASKED, NT>(x.row, x.V, mask, v0, v1, top, lists);
+        return;
+    }
+    for (uint32_t j = warp; j < NT / 32; j += NT / 32) {
+        key_t64 k = tid < n ? cand[tid] : 0;
+        if (n > j * 32) k = sort32(k, lane);
+        if (NT < CAND)  // (fewer threads than candidates: the rest of them)
+            for (uint32_t b = tid - lane + NT; b < n; b += NT) k = merge32(k, sort32(b + lane < n ? cand[b + lane] : 0ull, lane), lane);
+        lists[j][lane] = k;
+    }
+    if (n <= 32) __syncthreads();
+    else merge_lists<NT / 32>(lists, warp, lane);
+}
+
+// Long rows: a cluster of thread blocks per row (one block if there are rows enough), each block a run of vectors, each thread every
+// NT-th vector of it.
+template <typename T, bool MASKED, bool TOP, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q, const ScoreOut o, uint32_t parts)
+{
+    constexpr int U = 4, NW = NT / 32;
+    __shared__ float s_sums[3][NW];
+    __shared__ float s_part[MAX_PARTS][3];
+    __shared__ key_t64 s_lists[TOP ? NW : 1][32], s_parts[TOP ? MAX_PARTS : 1][32], s_cand[TOP ? CAND : 1];
+    __shared__ uint32_t s_n;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = blockIdx.x % parts;
+    const float c = q.scale * 1.44269504088896341f, inf = __int_as_float(0x7f800000);
+    for (uint64_t r = blockIdx.x / parts; r < q.n_rows; r += gridDim.x / parts) {
         const int64_t tok = row_token(q, r);
-        if (tok < 0) { empty_row(o, r, true, tid, LP_THREADS); continue; }
-        const T *x = static_cast<const T *>(q.x) + r * q.stride;
+        if (tok < 0) {
+            if (part == 0) empty_row(o, r, true, tid, NT);
+            continue;
+        }
+        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
         const RowMask mask = row_mask(q, r);
-        const bool masked = mask.any();
-        float m = -inf;
-        bool nan = false;
-        for (uint32_t i = tid; i < q.V; i += LP_THREADS) {
-            if (masked && mask.is_closed(i)) continue;
-            const float v = to_f32(x[i]);
-            nan = nan || v != v;
-            m = fmaxf(m, v);
+        const uint32_t per = (x.n + parts - 1) / parts, v0 = min(x.n, part * per), v1 = min(x.n, v0 + per);
+        const uint32_t f0 = max(v0, x.lead ? 1u : 0u), f1 = min(v1, (x.lead + x.V) / EPV<T>);  // whole vectors
+        if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        float x_tok = 0.0f;
+        if (part == 0 && tid == 0 && o.logprob) x_tok = to_f32(x.row[tok]);
+
+        Run a{-inf, 0ull, 0ull, 0xFFFFFFFFu};
+        uint4 raw[U];
+        if (f0 > v0 && tid == 0) {
+            uint4 one[1] = {fetch<T, MASKED>(x, mask, v0)};
+            take<T, 1, TOP>(a, one, v0, NT, c);
         }
-        m = warp_max(m);
-        __syncthreads();
-        if (lane == 0) s_a[warp] = m;
-        nan = __syncthreads_or(nan);
-        m = s_a[0];
-        for (int w = 1; w < 8; ++w) m = fmaxf(m, s_a[w]);
-        if (m == -inf && !nan) { empty_row(o, r, false, tid, LP_THREADS); continue; }
-        float s = 0.0f, t = 0.0f;
-        for (uint32_t i = tid; i < q.V; i += LP_THREADS) {
-            if (masked && mask.is_closed(i)) continue;
-            const float d = (to_f32(x[i]) - m) * q.scale;
-            const float e = expf(d);
-            s += e;
-            if (e != 0.0f) t += e * d;
-        }
-        s = warp_sum(s);
-        t = warp_sum(t);
-        __syncthreads();
-        if (lane == 0) { s_a[warp] = s; s_b[warp] = t; }
-        __syncthreads();
-        s = t = 0.0f;
-        for (int w = 0; w < 8; ++w) { s += s_a[w]; t += s_b[w]; }
-        const float L = logf(s);
-        if (tid == 0) {
-            if (o.logprob)
-                o.logprob[r] = masked && mask.is_closed((uint32_t)tok) ? -inf : (to_f32(x[tok]) - m) * q.scale - L;
-            if (o.entropy) o.entropy[r] = L - t / s;
-            if (o.stats) { o.stats[2 * r] = m; o.stats[2 * r + 1] = L; }
-        }
-        unsigned long long last = ~0ull;
-        for (uint32_t j = 0; j < o.top; ++j) {
-            unsigned long long best = 0;
-            for (uint32_t i = tid; i < q.V; i += LP_THREADS) {
-                if (masked && mask.is_closed(i)) continue;
-                const float v = to_f32(x[i]);
-                if (!(v > -inf)) continue;
-                const unsigned long long k = rank_key(v, i);
-                if (k < last && k > best) best = k;
+        for (uint32_t v = v0 + tid; v < f1; v += NT * U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t w = v + u * NT;
+                raw[u] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+                if (w >= f0 && w < f1) raw[u] = *x.at(w);
             }
-            for (int d = 16; d; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
-            __syncthreads();
-            if (lane == 0) s_k[warp] = best;
-            __syncthreads();
-            for (int w = 0; w < 8; ++w) best = max(best, s_k[w]);
-            if (tid == 0) {
-                const uint32_t i = 0xFFFFFFFFu - (uint32_t)best;
-                o.ids[r * o.top + j] = best ? (int32_t)i : -1;
-                o.lps[r * o.top + j] = best ? (to_f32(x[i]) - m) * q.scale - L : -inf;
+            if (MASKED) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (v + u * NT < f1) close_entries<T>(raw[u], mask.closed_from(x.first(v + u * NT), EPV<T>));
             }
-            last = best;
+            take<T, U, TOP>(a, raw, v, NT, c);
+        }
+        if (f1 < v1 && v1 > f0 && (v1 - 1 - v0) % NT == tid) {
+            uint4 one[1] = {fetch<T, MASKED>(x, mask, v1 - 1)};
+            take<T, 1, TOP>(a, one, v1 - 1, NT, c);
+        }
+
+        float s0, s1, t0, t1;
+        apart(a.s, s0, s1);
+        apart(a.t, t0, t1);
+        Sums w{a.m, s0 + s1, t0 + t1};
+        warp_join(w, c);
+        __syncthreads();  // (what the row in front left in shared memory has been read)
+        if (lane == 0) { s_sums[0][warp] = w.m; s_sums[1][warp] = w.s; s_sums[2][warp] = w.t; }
+        if (TOP) alternatives<T, MASKED, NT>(x, mask, v0, v1, a, o.top, s_lists, s_cand, &s_n);
+        else __syncthreads();
+        if (warp == 0) {
+            w = lane < NW ? Sums{s_sums[0][lane], s_sums[1][lane], s_sums[2][lane]} : Sums{-inf, 0.0f, 0.0f};
+            warp_join(w, c);
+        }
+        if (parts > 1) {  // to the first block of the cluster
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (it has read the row in front, and runs)
+            cg::cluster_group cluster = cg::this_cluster();
+            if (warp == 0) {
+                if (lane == 0) {
+                    float *to = cluster.map_shared_rank(&s_part[part][0], 0);
+                    to[0] = w.m; to[1] = w.s; to[2] = w.t;
+                }
+                if (TOP) *cluster.map_shared_rank(&s_parts[part][lane], 0) = s_lists[0][lane];
+            }
+            cluster.sync();
+            if (part != 0) continue;
+            if (warp == 0) {
+                w = lane < parts ? Sums{s_part[lane][0], s_part[lane][1], s_part[lane][2]} : Sums{-inf, 0.0f, 0.0f};
+                warp_join(w, c);
+                if (TOP) {
+                    key_t64 k = s_parts[0][lane];
+                    for (uint32_t j = 1; j < parts; ++j) k = merge32(k, s_parts[j][lane], lane);
+                    s_lists[0][lane] = k;
+                    __syncwarp();
+                }
+            }
+        }
+        if (warp == 0) {
+            if (w.s == 0.0f) {
+                empty_row(o, r, false, lane, 32);
+            } else {
+                const float L = logf(w.s);
+                if (lane == 0) {
+                    if (o.logprob) o.logprob[r] = MASKED && mask.is_closed((uint32_t)tok) ? -inf : (x_tok - w.m) * q.scale - L;
+                    if (o.entropy) o.entropy[r] = L - q.scale * (w.t / w.s);
+                    if (o.stats) *reinterpret_cast<float2 *>(o.stats + 2 * r) = make_float2(w.m, L);
+                }
+                if (TOP && lane < o.top) {
+                    const key_t64 k = s_lists[0][lane];
+                    o.ids[r * o.top + lane] = k ? (int32_t)key_place(k) : -1;
+                    o.lps[r * o.top + lane] = k ? (key_value(k) - w.m) * q.scale - L : -inf;
+                }
+            }
         }
     }
 }
 
-struct GradIn {
-    const float *stats, *entropy, *g, *h;
-    void *dx;
-    uint64_t stride;
-};
-
-// With l_i = log p_i: d logprob / d x_i = scale ([i = token] - p_i), d entropy / d x_i = -scale p_i (l_i + entropy).
-template <typename T>
-__global__ void __launch_bounds__(LP_THREADS) k_score_grad(const LogitRows q, const GradIn p)
+template <typename T, bool MASKED, bool TOP>
+cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st)
 {
-    const float inf = __int_as_float(0x7f800000);
-    for (uint64_t r = blockIdx.x; r < q.n_rows; r += gridDim.x) {
-        const int64_t tok = row_token(q, r);
-        const float M = p.stats[2 * r], L = p.stats[2 * r + 1];
-        const T *x = static_cast<const T *>(q.x) + r * q.stride;
-        T *dx = static_cast<T *>(p.dx) + r * p.stride;
-        const RowMask mask = row_mask(q, r);
-        const bool masked = mask.any(), dead = tok < 0 || L == -inf;
-        const float H = p.h && !dead ? p.entropy[r] : 0.0f, h = p.h && !dead ? p.h[r] : 0.0f;
-        const float g = !p.g || dead || (masked && mask.is_closed((uint32_t)tok)) ? 0.0f : p.g[r];
-        for (uint32_t i = threadIdx.x; i < q.V; i += LP_THREADS) {
-            float d = 0.0f;
-            if (!dead && !(masked && mask.is_closed(i))) {
-                const float l = (to_f32(x[i]) - M) * q.scale - L;
-                const float e = expf(l);
-                d = e == 0.0f ? 0.0f : -e * (g + h * (l + H));
-                if ((int64_t)i == tok) d += g;
-                d *= q.scale;
-            }
-            from_f32(dx[i], d);
-        }
-    }
+    constexpr int NT = 512;
+    const uint64_t sms = (uint64_t)vl_device_sm_count(device);
+    uint32_t parts = 1;
+    while (parts < MAX_PARTS && q.n_rows * parts < 2 * sms && q.V / (2 * parts) >= NT * EPV<T>) parts *= 2;
+    const uint64_t rows = q.n_rows < (1ull << 27) ? q.n_rows : (1ull << 27);
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = parts;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((uint32_t)(rows * parts)); cfg.blockDim = NT; cfg.stream = st;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    g_vl_launches.fetch_add(1);
+    return cudaLaunchKernelEx(&cfg, k_score_long<T, MASKED, TOP, NT>, q, o, parts);
 }
 
 template <typename F>
@@ -169,8 +384,6 @@ int by_type(int dtype, F &&f)
     default: return f(__nv_bfloat16{});
     }
 }
-
-uint32_t row_blocks(uint64_t rows) { return (uint32_t)(rows < 0x7FFFFFFFull ? rows : 0x7FFFFFFFull); }
 
 }  // namespace
 
@@ -187,7 +400,7 @@ int vl_logit_rows(const vl_logits *x, LogitRows *q)
     if (((uintptr_t)x->occupied | (uintptr_t)x->mask_rows) & 3) return VL_ERR_INVALID_ARG;
     if (x->mask_rows && !x->occupied) return VL_ERR_INVALID_ARG;
     if (x->occupied && !x->mask_rows && x->n_masks < x->n_rows) return VL_ERR_INVALID_ARG;
-    if (!(x->scale > 0.0f) || x->scale > 3.0e38f) return VL_ERR_INVALID_ARG;
+    if (!(x->scale >= 1e-20f && x->scale <= 1e20f)) return VL_ERR_INVALID_ARG;
     q->x = x->logits; q->n_rows = x->n_rows; q->stride = x->row_stride;
     q->V = x->n_vocab; q->W = (x->n_vocab + 31) / 32;
     q->tokens = x->tokens; q->token_bytes = x->token_bytes;
@@ -210,35 +423,12 @@ extern "C" int vl_token_logprobs(int device, const vl_logits *x, float *d_logpro
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
     const ScoreOut o{d_logprob, d_entropy, d_row_stats, top, d_top_ids, d_top_logprobs};
+    const bool masked = q.occupied || q.widths;
     return by_type(x->dtype, [&](auto type) {
-        k_score<decltype(type)><<<row_blocks(q.n_rows), LP_THREADS, 0, (cudaStream_t)stream>>>(q, o);
-        g_vl_launches.fetch_add(1);
-        return cudaGetLastError() == cudaSuccess ? VL_OK : VL_ERR_CUDA;
-    });
-}
-
-extern "C" int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_row_stats, const float *d_entropy,
-                                          const float *d_g_logprob, const float *d_g_entropy, void *d_dlogits, uint64_t out_stride,
-                                          void *stream)
-{
-    LogitRows q;
-    const int rc = vl_logit_rows(x, &q);
-    if (rc != VL_OK) return rc;
-    if (((uintptr_t)d_entropy | (uintptr_t)d_g_logprob | (uintptr_t)d_g_entropy) & 3) return VL_ERR_INVALID_ARG;
-    if ((uintptr_t)d_row_stats & 7) return VL_ERR_INVALID_ARG;
-    if (d_g_entropy && !d_entropy) return VL_ERR_INVALID_ARG;
-    if (d_g_logprob && !q.tokens) return VL_ERR_INVALID_ARG;
-    if (q.n_rows > 1 && out_stride < q.V) return VL_ERR_INVALID_ARG;
-    if (out_stride > (1ull << 40)) return VL_ERR_INVALID_ARG;
-    if (q.n_rows && (!d_row_stats || !d_dlogits || (uintptr_t)d_dlogits % (x->dtype == VL_F32 ? 4 : 2))) return VL_ERR_INVALID_ARG;
-    if (d_dlogits == x->logits && q.n_rows > 1 && out_stride != q.stride) return VL_ERR_INVALID_ARG;
-    if (q.n_rows == 0) return VL_OK;
-    const DeviceScope scope(device);
-    if (scope.error != cudaSuccess) return VL_ERR_CUDA;
-    const GradIn p{d_row_stats, d_entropy, d_g_logprob, d_g_entropy, d_dlogits, out_stride};
-    return by_type(x->dtype, [&](auto type) {
-        k_score_grad<decltype(type)><<<row_blocks(q.n_rows), LP_THREADS, 0, (cudaStream_t)stream>>>(q, p);
-        g_vl_launches.fetch_add(1);
-        return cudaGetLastError() == cudaSuccess ? VL_OK : VL_ERR_CUDA;
+        using T = decltype(type);
+        cudaStream_t st = (cudaStream_t)stream;
+        const cudaError_t e = masked ? (top ? launch_long<T, true, true>(q, o, device, st) : launch_long<T, true, false>(q, o, device, st))
+                                     : (top ? launch_long<T, false, true>(q, o, device, st) : launch_long<T, false, false>(q, o, device, st));
+        return e == cudaSuccess ? VL_OK : VL_ERR_CUDA;
     });
 }
