@@ -132,6 +132,39 @@ struct RowVectors {
     }
 };
 
+// Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of word g.
+// (A lane holds at most 32 entries, so a row has no more words than its group has lanes.)
+template <typename T, int G, int NV>
+__device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t g, bool aligned)
+{
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const uint32_t v = g + G * j;
+        raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+        if (v < x.n && (aligned || x.whole(v))) raw[j] = *x.at(v);
+    }
+    if (!aligned) {
+#pragma unroll 1
+        for (uint32_t b = 0; b < 2; ++b) {  // the first vector and the last one
+            const uint32_t v = b ? x.n - 1 : 0;
+            if (v % G != g || x.whole(v) || (b && v == 0)) continue;
+            const uint4 r = x.part(v);
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (v / G == j) raw[j] = r;
+        }
+    }
+}
+// Closed entries of the lane's vector v, from the words that the group's lanes hold.  Every lane of the warp calls it.
+template <typename T, int G>
+__device__ __forceinline__ uint32_t group_closed(uint32_t word, int first, bool aligned)
+{
+    const int w = first >> 5, s = first & 31;
+    const uint32_t a = __shfl_sync(0xffffffffu, word, w & (G - 1), G);
+    const uint32_t b = aligned ? 0u : __shfl_sync(0xffffffffu, word, (w + 1) & (G - 1), G);
+    return __funnelshift_r(a, b, s) & ((1u << EPV<T>) - 1);
+}
+
 // Entries whose bit is set to minus infinity.
 template <typename T>
 __device__ __forceinline__ void close_entries(uint4 &r, uint32_t bits)
@@ -265,6 +298,15 @@ __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
 }
 
 }  // namespace
+
+// Largest number of 16-byte vectors that a row of the descriptor spans, and whether rows start and end on them.
+static inline uint32_t row_vectors(const LogitRows &q, uint32_t size, bool *aligned)
+{
+    const uint32_t n = 16 / size;
+    const bool starts = ((uintptr_t)q.x & 15) == 0 && (q.n_rows <= 1 || q.stride % n == 0);
+    *aligned = starts && q.V % n == 0;
+    return starts ? (q.V + n - 1) / n : (q.V + 2 * (n - 1)) / n;
+}
 
 // Makes `device` current and puts the caller's device back at the end of the call.
 struct DeviceScope {

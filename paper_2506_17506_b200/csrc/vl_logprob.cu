@@ -102,6 +102,18 @@ __device__ __forceinline__ void warp_join(Sums &a, float c)
     a.t = warp_sum(a.t);
 }
 
+// Two more entries; low: minus the largest one, twice; c2: scale log2 e, twice.
+__device__ __forceinline__ void sum_two(float x0, float x1, f32x2 low, f32x2 c2, f32x2 &s, f32x2 &t)
+{
+    float d0, d1, y0, y1;
+    apart(add2(both(x0, x1), low), d0, d1);
+    const f32x2 d = both(max_nan(d0, FAR_BELOW), max_nan(d1, FAR_BELOW));
+    apart(mul2(d, c2), y0, y1);
+    const f32x2 e = both(ex2(y0), ex2(y1));
+    s = add2(s, e);
+    t = fma2(e, d, t);
+}
+
 // A thread's state over the vectors of its stripe.
 struct Run {
     float m;
@@ -135,15 +147,7 @@ __device__ __forceinline__ void take(Run &a, const uint4 (&raw)[N], uint32_t v, 
         float x[EPV<T>];
         unpack(raw[u], x, T{});
 #pragma unroll
-        for (int j = 0; j < EPV<T>; j += 2) {
-            float d0, d1, y0, y1;
-            apart(add2(both(x[j], x[j + 1]), low), d0, d1);
-            const f32x2 d = both(max_nan(d0, FAR_BELOW), max_nan(d1, FAR_BELOW));
-            apart(mul2(d, c2), y0, y1);
-            const f32x2 e = both(ex2(y0), ex2(y1));
-            a.s = add2(a.s, e);
-            a.t = fma2(e, d, a.t);
-        }
+        for (int j = 0; j < EPV<T>; j += 2) sum_two(x[j], x[j + 1], low, c2, a.s, a.t);
     }
 }
 
@@ -194,7 +198,7 @@ __device__ __noinline__ void alternatives_one_by_one(const T *row, uint32_t V, c
     for (uint32_t j = 0; j < top; ++j) {
         key_t64 best = 0;
         for (uint32_t v = v0 + threadIdx.x; v < v1; v += NT)
-            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), best, [&](key_t64 k) { if (k < last) best = k; });
+            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), best, [&](key_t64 k) { if (k < last && k > best) best = k; });
         for (int d = 16; d; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
         __syncthreads();
         if (lane == 0) lists[0][warp] = best;
@@ -375,6 +379,165 @@ cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaS
     return cudaLaunchKernelEx(&cfg, k_score_long<T, MASKED, TOP, NT>, q, o, parts);
 }
 
+// Short rows: a group of lanes per row, every logit read once into registers.
+constexpr uint32_t SHORT_WARPS = 8, SHORT_CAND = 128;
+
+// The best entries of a row that the whole warp holds (G = 32), as in the long rows: the k-th of the lanes' best bounds the k-th of all.
+template <typename T, int NV>
+__device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t lane, uint32_t top, key_t64 *cand,
+                                                     uint32_t *n_cand)
+{
+    key_t64 mine = 0;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) each_key<T>(raw[j], x.first(lane + 32 * j), mine, [&](key_t64 k) { if (k > mine) mine = k; });
+    const key_t64 least = __shfl_sync(0xffffffffu, sort32(mine, lane), top - 1);
+    if (lane == 0) *n_cand = 0;
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+        each_key<T>(raw[j], x.first(lane + 32 * j), least, [&](key_t64 k) {
+            const uint32_t at = atomicAdd(n_cand, 1u);
+            if (at < SHORT_CAND) cand[at] = k;
+        });
+    __syncwarp();
+    const uint32_t n = *n_cand;
+    key_t64 best = 0;
+    if (n <= SHORT_CAND) {
+        best = sort32(lane < n ? cand[lane] : 0ull, lane);
+        for (uint32_t b = 32; b < n; b += 32) best = merge32(best, sort32(b + lane < n ? cand[b + lane] : 0ull, lane), lane);
+    } else {  // one by one
+        key_t64 last = ~0ull;
+        for (uint32_t i = 0; i < top; ++i) {
+            key_t64 b = 0;
+#pragma unroll 1
+            for (int j = 0; j < NV; ++j) {
+                uint4 r = raw[0];
+#pragma unroll
+                for (int l = 1; l < NV; ++l)
+                    if (j == l) r = raw[l];
+                each_key<T>(r, x.first(lane + 32 * j), b, [&](key_t64 k) { if (k < last && k > b) b = k; });
+            }
+            for (int d = 16; d; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
+            if (lane == i) best = b;
+            last = b;
+        }
+    }
+    __syncwarp();
+    return best;
+}
+
+template <typename T, bool MASKED, bool TOP, int G, int NV>
+__global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRows q, const ScoreOut o, bool aligned)
+{
+    static_assert(NV * EPV<T> <= 32, "a lane's entries");
+    static_assert(!TOP || G == 32, "alternatives take the whole warp");
+    __shared__ key_t64 s_cand[TOP ? SHORT_WARPS : 1][TOP ? SHORT_CAND : 1];
+    __shared__ uint32_t s_n[SHORT_WARPS];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
+    const float c = q.scale * 1.44269504088896341f, inf = __int_as_float(0x7f800000);
+    const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
+    for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
+        const uint64_t r = min(r0 + lane / G, q.n_rows - 1);
+        const bool there = r0 + lane / G < q.n_rows;  // (the warp's last rows may not be: it works on the last one instead)
+        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
+        uint4 raw[NV];
+        fetch_row<T, G, NV>(raw, x, g, aligned);
+        const int64_t tok = row_token(q, r);
+        uint32_t word = 0;
+        if (MASKED) {
+            word = row_mask(q, r).closed(g);
+#pragma unroll
+            for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
+        }
+        float x_tok = 0.0f;
+        if (g == 0 && o.logprob && tok >= 0) x_tok = to_f32(x.row[tok]);
+
+        float m = vector_max(raw[0], T{});
+#pragma unroll
+        for (int j = 1; j < NV; ++j) m = fmaxf(m, vector_max(raw[j], T{}));
+#pragma unroll
+        for (int d = G / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        const float base = fmaxf(m, LOWEST);
+        f32x2 s2 = 0ull, t2 = 0ull;
+        const f32x2 low = both(-base, -base), c2 = both(c, c);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float e[EPV<T>];
+            unpack(raw[j], e, T{});
+#pragma unroll
+            for (int i = 0; i < EPV<T>; i += 2) sum_two(e[i], e[i + 1], low, c2, s2, t2);
+        }
+        float s, t, b;
+        apart(s2, s, b);
+        s += b;
+        apart(t2, t, b);
+        t += b;
+#pragma unroll
+        for (int d = G / 2; d; d >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, d);
+            t += __shfl_xor_sync(0xffffffffu, t, d);
+        }
+        const float L = logf(s);
+        const bool left = tok < 0, empty = s == 0.0f;
+        bool shut = false;
+        if (MASKED) shut = (__shfl_sync(0xffffffffu, word, left ? 0 : (int)((uint32_t)tok >> 5) & (G - 1), G) >> (tok & 31)) & 1;
+        if (g == 0 && there) {
+            if (o.logprob) o.logprob[r] = left ? 0.0f : (empty || shut ? -inf : (x_tok - m) * q.scale - L);
+            if (o.entropy) o.entropy[r] = left || empty ? 0.0f : L - q.scale * (t / s);
+            if (o.stats)
+                *reinterpret_cast<float2 *>(o.stats + 2 * r) = left ? make_float2(0.0f, 0.0f) : make_float2(empty ? -inf : m, L);
+        }
+        if (TOP) {
+            const key_t64 k = warp_alternatives<T, NV>(raw, x, lane, o.top, s_cand[warp], &s_n[warp]);
+            if (lane < o.top) {
+                const bool one = k != 0 && !left;
+                o.ids[r * o.top + lane] = one ? (int32_t)key_place(k) : -1;
+                o.lps[r * o.top + lane] = one ? (key_value(k) - m) * q.scale - L : -inf;
+            }
+        }
+    }
+}
+
+template <typename T, bool MASKED, bool TOP, int G, int NV>
+cudaError_t run_short(const LogitRows &q, const ScoreOut &o, bool aligned, cudaStream_t st)
+{
+    const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
+    k_score_short<T, MASKED, TOP, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, o, aligned);
+    g_vl_launches.fetch_add(1);
+    return cudaGetLastError();
+}
+
+// Whether the rows are short, and if so the launch.
+template <typename T, bool MASKED, bool TOP>
+bool launch_short(const LogitRows &q, const ScoreOut &o, cudaStream_t st, cudaError_t *e)
+{
+    bool aligned;
+    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
+    if constexpr (TOP) {
+        if (n <= 32) *e = run_short<T, MASKED, true, 32, 1>(q, o, aligned, st);
+        else if (n <= 64) *e = run_short<T, MASKED, true, 32, 2>(q, o, aligned, st);
+        else if (n <= 128) *e = run_short<T, MASKED, true, 32, 4>(q, o, aligned, st);
+        else if (n <= 256 && sizeof(T) == 4) *e = run_short<T, MASKED, true, 32, 32 / EPV<T>>(q, o, aligned, st);
+        else return false;
+    } else {
+        if (n <= 4) *e = run_short<T, MASKED, false, 4, 1>(q, o, aligned, st);
+        else if (n <= 16) *e = run_short<T, MASKED, false, 4, 4>(q, o, aligned, st);
+        else if (n <= 32) *e = run_short<T, MASKED, false, 8, 4>(q, o, aligned, st);
+        else if (n <= 64) *e = run_short<T, MASKED, false, 16, 4>(q, o, aligned, st);
+        else if (n <= 128) *e = run_short<T, MASKED, false, 32, 4>(q, o, aligned, st);
+        else if (n <= 256 && sizeof(T) == 4) *e = run_short<T, MASKED, false, 32, 32 / EPV<T>>(q, o, aligned, st);
+        else return false;
+    }
+    return true;
+}
+
+template <typename T, bool MASKED, bool TOP>
+cudaError_t launch(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st)
+{
+    cudaError_t e;
+    return launch_short<T, MASKED, TOP>(q, o, st, &e) ? e : launch_long<T, MASKED, TOP>(q, o, device, st);
+}
+
 template <typename F>
 int by_type(int dtype, F &&f)
 {
@@ -427,8 +590,8 @@ extern "C" int vl_token_logprobs(int device, const vl_logits *x, float *d_logpro
     return by_type(x->dtype, [&](auto type) {
         using T = decltype(type);
         cudaStream_t st = (cudaStream_t)stream;
-        const cudaError_t e = masked ? (top ? launch_long<T, true, true>(q, o, device, st) : launch_long<T, true, false>(q, o, device, st))
-                                     : (top ? launch_long<T, false, true>(q, o, device, st) : launch_long<T, false, false>(q, o, device, st));
+        const cudaError_t e = masked ? (top ? launch<T, true, true>(q, o, device, st) : launch<T, true, false>(q, o, device, st))
+                                     : (top ? launch<T, false, true>(q, o, device, st) : launch<T, false, false>(q, o, device, st));
         return e == cudaSuccess ? VL_OK : VL_ERR_CUDA;
     });
 }
