@@ -375,7 +375,7 @@ typedef struct {
     uint64_t n_masks;          /* at least n_rows if mask_rows is NULL */
     const int32_t *mask_rows;  /* [n_rows] or NULL */
     const uint8_t *widths;     /* [n_rows] or NULL */
-    float scale;               /* 1 / temperature: 1e-20 to 1e20 */
+    float scale;               /* 1 / temperature: 1e-6 to 1e6 */
 } vl_logits;
 
 /*

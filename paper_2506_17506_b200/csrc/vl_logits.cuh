@@ -103,6 +103,63 @@ __device__ __forceinline__ float vector_max(const uint4 &r, __nv_bfloat16)
     return fmaxf(__low2float(m), __high2float(m));
 }
 
+// The largest of several vectors' elements.
+template <int N>
+__device__ __forceinline__ float vectors_max(const uint4 (&r)[N], float t)
+{
+    float m = vector_max(r[0], t);
+#pragma unroll
+    for (int j = 1; j < N; ++j) m = fmaxf(m, vector_max(r[j], t));
+    return m;
+}
+template <typename P, int N>
+__device__ __forceinline__ P halves_max(const uint4 (&r)[N])
+{
+    P m[4];
+    memcpy(m, &r[0], 16);
+#pragma unroll
+    for (int j = 1; j < N; ++j) {
+        P h[4];
+        memcpy(h, &r[j], 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = __hmax2(m[i], h[i]);
+    }
+    return __hmax2(__hmax2(m[0], m[1]), __hmax2(m[2], m[3]));
+}
+template <int N>
+__device__ __forceinline__ float vectors_max(const uint4 (&r)[N], __half)
+{
+    const __half2 m = halves_max<__half2>(r);
+    return fmaxf(__low2float(m), __high2float(m));
+}
+template <int N>
+__device__ __forceinline__ float vectors_max(const uint4 (&r)[N], __nv_bfloat16)
+{
+    const __nv_bfloat162 m = halves_max<__nv_bfloat162>(r);
+    return fmaxf(__low2float(m), __high2float(m));
+}
+
+// bf16 entries no lower than -1e30 (what is no number stays none): two at once, so that no product with them leaves the range of numbers.
+// The other types are bounded after the product.
+template <typename T> constexpr bool BOUNDED = false;
+template <> constexpr bool BOUNDED<__nv_bfloat16> = true;
+template <typename T>
+__device__ __forceinline__ uint4 above(const uint4 &r)
+{
+    if constexpr (BOUNDED<T>) {
+        const __nv_bfloat162 low = __floats2bfloat162_rn(-1e30f, -1e30f);
+        __nv_bfloat162 h[4];
+        memcpy(h, &r, 16);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) h[j] = __hmax2_nan(h[j], low);
+        uint4 o;
+        memcpy(&o, h, 16);
+        return o;
+    } else {
+        return r;
+    }
+}
+
 // A row as 16-byte vectors: vector v holds the entries first(v) .. first(v) + EPV - 1; the first and the last vector may hold
 // entries of no row, which are read one by one around them.
 template <typename T>
@@ -133,25 +190,27 @@ struct RowVectors {
 };
 
 // Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of word g.
-// (A lane holds at most 32 entries, so a row has no more words than its group has lanes.)
 template <typename T, int G, int NV>
 __device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t g, bool aligned)
 {
+    const uint4 *at = x.at(g);
+    if (aligned) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const uint32_t v = g + G * j;
-        raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
-        if (v < x.n && (aligned || x.whole(v))) raw[j] = *x.at(v);
-    }
-    if (!aligned) {
-#pragma unroll 1
-        for (uint32_t b = 0; b < 2; ++b) {  // the first vector and the last one
-            const uint32_t v = b ? x.n - 1 : 0;
-            if (v % G != g || x.whole(v) || (b && v == 0)) continue;
-            const uint4 r = x.part(v);
+        for (int j = 0; j < NV; ++j) {
+            raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+            if (g + G * j < x.n) raw[j] = at[G * j];
+        }
+    } else {
+// the vectors that are no whole ones: the first and the last
+        uint4 end = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>), begin = end;
+        if (g == 0 && x.lead && x.n > 1) begin = x.part(0);
+        if (g == (x.n - 1) % G && !x.whole(x.n - 1)) end = x.part(x.n - 1);
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (v / G == j) raw[j] = r;
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t v = g + G * j;
+            raw[j] = v == x.n - 1 ? end : begin;
+            if (x.whole(v)) raw[j] = at[G * j];
+            else if (v >= x.n) raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
         }
     }
 }
@@ -165,21 +224,24 @@ __device__ __forceinline__ uint32_t group_closed(uint32_t word, int first, bool 
     return __funnelshift_r(a, b, s) & ((1u << EPV<T>) - 1);
 }
 
-// Entries whose bit is set to minus infinity.
+// Entries whose bit is set to minus infinity.  Halves: a byte permutation takes their bytes from the one or the other word; the selectors
+// of four entries are made at once, a bit spread to a byte of 0x44 (13 instructions a vector, 28 with a mask per pair).
 template <typename T>
 __device__ __forceinline__ void close_entries(uint4 &r, uint32_t bits)
 {
-    uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        if (sizeof(T) == 4) {
-            if ((bits >> j) & 1) w[j] = MINUS_INF2<T>;
-        } else {
-            const uint32_t m = ((bits >> (2 * j)) & 1 ? 0xFFFFu : 0u) | ((bits >> (2 * j + 1)) & 1 ? 0xFFFF0000u : 0u);
-            w[j] = (w[j] & ~m) | (MINUS_INF2<T> & m);
-        }
+    if constexpr (sizeof(T) == 4) {
+        if (bits & 1) r.x = MINUS_INF2<T>;
+        if (bits & 2) r.y = MINUS_INF2<T>;
+        if (bits & 4) r.z = MINUS_INF2<T>;
+        if (bits & 8) r.w = MINUS_INF2<T>;
+    } else {
+        const uint32_t a = (((bits & 15u) * 0x00204081u) & 0x01010101u) * 0x44u + 0x32103210u;
+        const uint32_t b = (((bits >> 4) * 0x00204081u) & 0x01010101u) * 0x44u + 0x32103210u;
+        r.x = __byte_perm(r.x, MINUS_INF2<T>, a);
+        r.y = __byte_perm(r.y, MINUS_INF2<T>, a >> 16);
+        r.z = __byte_perm(r.z, MINUS_INF2<T>, b);
+        r.w = __byte_perm(r.w, MINUS_INF2<T>, b >> 16);
     }
-    r = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Two 32-bit numbers side by side: one instruction works on both.

@@ -8,7 +8,7 @@
 // One pass: a thread holds the largest logit so far and the two sums in 32 bits, and scales the sums when the largest one rises.
 //
 // What bounds it: reading the logits once; per element also one exponential (16 a clock and multiprocessor: 119 us for the 5.4e8 of
-// 4,096 rows of 131,072, against 164 us for their bytes in bf16) and about six more instructions, of which those on pairs of
+// 4,096 rows of 131,072, against 164 us for their bytes in bf16) and about five more instructions, of which those on pairs of
 // numbers (f32x2) and of 16-bit halves do two elements at once.
 #include <cooperative_groups.h>
 
@@ -20,10 +20,6 @@ namespace cg = cooperative_groups;
 typedef unsigned long long key_t64;
 
 constexpr float LOWEST = -3.402823466e38f;
-// Stands for minus infinity in a difference: times scale >= 1e-20 its exponential is 0, and 0 times it is 0.
-constexpr float FAR_BELOW = -1e30f;
-constexpr uint32_t TOP_MAX = VL_MAX_ALTERNATIVES;
-constexpr uint32_t MAX_PARTS = 8;  // thread blocks of a row
 
 struct ScoreOut {
     float *logprob, *entropy, *stats;
@@ -66,25 +62,24 @@ __device__ __forceinline__ key_t64 merge32(key_t64 a, key_t64 b, uint32_t lane)
     for (uint32_t d = 16; d; d /= 2) k = exchange(k, d, (lane & d) == 0);
     return k;
 }
-// NW sorted lists in shared memory; the first 32 of all of them end up in list 0.  Every warp of the block calls it.
-template <int NW>
-__device__ __forceinline__ void merge_lists(key_t64 (*lists)[32], uint32_t warp, uint32_t lane)
-{
-#pragma unroll
-    for (uint32_t half = NW / 2; half; half /= 2) {
-        __syncthreads();
-        if (warp < half) lists[warp][lane] = merge32(lists[warp][lane], lists[warp + half][lane], lane);
-    }
-    __syncthreads();
-}
-
 // ---- running sums
+// In powers of two: y_i = c x_i - B with c = scale log2 e and B = c m rounded, m the largest logit so far; s = sum 2^y, t = sum 2^y y.
+// One multiply-add makes y, and B being rounded makes no difference: it is the same B in every term, and what it lacks to c m is put
+// right once, at the end.  Where c x would leave the range of numbers (FAR_OUT), y is (x - m) c.
+constexpr float FAR_OUT = 1e29f;     // times c (scale <= 1e6) it is a number
+constexpr float FAR_BELOW = -1e30f;  // stands for minus infinity, whose 2^y y would be none: its power of two is 0 (scale >= 1e-6)
 struct Sums {
-    float m, s, t;  // largest logit; sum e, sum e d relative to it
+    float m, s, t;
 };
+__device__ __forceinline__ bool far_out(float m) { return !(fabsf(m) < FAR_OUT); }
+// What sums relative to m lack to sums relative to the larger m1, as a power of two.
+__device__ __forceinline__ float step_down(float m, float m1, float c)
+{
+    return fmaxf(far_out(m) ? (m - m1) * c : __fsub_rn(__fmul_rn(m, c), __fmul_rn(m1, c)), FAR_BELOW);
+}
 __device__ __forceinline__ void raise(Sums &a, float m, float c)
 {
-    const float d = fmaxf(a.m - m, FAR_BELOW), f = ex2(d * c);
+    const float d = step_down(a.m, m, c), f = ex2(d);
     a.t = (a.t + a.s * d) * f;
     a.s *= f;
     a.m = m;
@@ -95,60 +90,91 @@ __device__ __forceinline__ float warp_sum(float v)
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
-__device__ __forceinline__ void warp_join(Sums &a, float c)
+// The lanes' sums together, relative to the lanes' largest m.
+__device__ __forceinline__ void warp_join(Sums &a, float m, float c)
 {
-    raise(a, from_ordered(__reduce_max_sync(0xffffffffu, ordered(a.m))), c);
+    raise(a, from_ordered(__reduce_max_sync(0xffffffffu, ordered(m))), c);
     a.s = warp_sum(a.s);
     a.t = warp_sum(a.t);
 }
-
-// Two more entries; low: minus the largest one, twice; c2: scale log2 e, twice.
-__device__ __forceinline__ void sum_two(float x0, float x1, f32x2 low, f32x2 c2, f32x2 &s, f32x2 &t)
+// L = ln sum exp(scale (x - m)), and the entropy.
+__device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *H)
 {
-    float d0, d1, y0, y1;
-    apart(add2(both(x0, x1), low), d0, d1);
-    const f32x2 d = both(max_nan(d0, FAR_BELOW), max_nan(d1, FAR_BELOW));
-    apart(mul2(d, c2), y0, y1);
-    const f32x2 e = both(ex2(y0), ex2(y1));
-    s = add2(s, e);
-    t = fma2(e, d, t);
+    const float ln2 = 0.693147180559945309f, ln_s = logf(a.s);
+    *L = far_out(a.m) ? ln_s : fmaf(ln2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
+    *H = ln_s - ln2 * __fdividef(a.t, a.s);  // (s is between 1/2 and 2^31)
 }
 
-// A thread's state over the vectors of its stripe.
+// The entries of vectors into the sums relative to m.
+template <typename T, int N>
+__device__ __forceinline__ void add_vectors(const uint4 (&raw)[N], float m, float c, f32x2 &s, f32x2 &t)
+{
+    if (!far_out(m)) {
+        const float b = -__fmul_rn(m, c);
+        const f32x2 c2 = both(c, c), low = both(b, b);
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float x[EPV<T>];
+            unpack(above<T>(raw[u]), x, T{});
+#pragma unroll
+            for (int j = 0; j < EPV<T>; j += 2) {
+                f32x2 y = fma2(both(x[j], x[j + 1]), c2, low);
+                float y0, y1;
+                apart(y, y0, y1);
+                if (!BOUNDED<T>) {
+                    y0 = max_nan(y0, FAR_BELOW);
+                    y1 = max_nan(y1, FAR_BELOW);
+                    y = both(y0, y1);
+                }
+                const f32x2 e = both(ex2(y0), ex2(y1));
+                s = add2(s, e);
+                t = fma2(e, y, t);
+            }
+        }
+    } else {
+        const float base = fmaxf(m, LOWEST);  // (nothing but impossible entries so far)
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float x[EPV<T>];
+            unpack(raw[u], x, T{});
+#pragma unroll
+            for (int j = 0; j < EPV<T>; j += 2) {
+                const float y0 = max_nan((x[j] - base) * c, FAR_BELOW), y1 = max_nan((x[j + 1] - base) * c, FAR_BELOW);
+                const f32x2 e = both(ex2(y0), ex2(y1));
+                s = add2(s, e);
+                t = fma2(e, both(y0, y1), t);
+            }
+        }
+    }
+}
+
+// A thread's state over the vectors of its stripe.  Its sums are relative to the largest logit it had met when a logit last was more than
+// 8 powers of two above the one before: nearly always to the first vectors' largest, so that the rest has nothing to scale.
 struct Run {
-    float m;
+    float ref, limit, m;  // what the sums are relative to; what a logit has to pass for another one; the largest
     f32x2 s, t;
     uint32_t best;  // vector in which m was met first
 };
 template <typename T, int N, bool TOP>
-__device__ __forceinline__ void take(Run &a, const uint4 (&raw)[N], uint32_t v, uint32_t step, float c)
+__device__ __forceinline__ void take(Run &a, const uint4 (&raw)[N], uint32_t v, uint32_t step, float c, float margin)
 {
-    float vm[N], m;
-#pragma unroll
-    for (int u = 0; u < N; ++u) vm[u] = vector_max(raw[u], T{});
-    m = vm[0];
-#pragma unroll
-    for (int u = 1; u < N; ++u) m = fmaxf(m, vm[u]);
-    if (m > a.m) {
-        const float d = fmaxf(a.m - m, FAR_BELOW), f = ex2(d * c);
-        a.t = mul2(fma2(a.s, both(d, d), a.t), both(f, f));
-        a.s = mul2(a.s, both(f, f));
-        a.m = m;
-        if (TOP) {
+    const float m = vectors_max<N>(raw, T{});
+    if (TOP) {
+        if (m > a.m) {
 #pragma unroll
             for (int u = N - 1; u >= 0; --u)
-                if (vm[u] == m) a.best = v + u * step;
+                if (vector_max(raw[u], T{}) == m) a.best = v + u * step;
         }
     }
-    const float base = fmaxf(a.m, LOWEST);  // (nothing but impossible entries so far)
-    const f32x2 low = both(-base, -base), c2 = both(c, c);
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-        float x[EPV<T>];
-        unpack(raw[u], x, T{});
-#pragma unroll
-        for (int j = 0; j < EPV<T>; j += 2) sum_two(x[j], x[j + 1], low, c2, a.s, a.t);
+    a.m = fmaxf(a.m, m);
+    if (m > a.limit) {
+        const float d = step_down(a.ref, m, c), f = ex2(d);
+        a.t = mul2(fma2(a.s, both(d, d), a.t), both(f, f));
+        a.s = mul2(a.s, both(f, f));
+        a.ref = m;
+        a.limit = m + margin;
     }
+    add_vectors<T, N>(raw, a.ref, c, a.s, a.t);
 }
 
 __device__ __forceinline__ void empty_row(const ScoreOut &o, uint64_t r, bool left_out, uint32_t tid, uint32_t nt)
@@ -185,225 +211,428 @@ __device__ __forceinline__ uint4 fetch(const RowVectors<T> &x, const RowMask &ma
     return raw;
 }
 
-constexpr uint32_t CAND = 512;  // candidates for the alternatives of a part
+// ---- long rows
+// Clusters of thread blocks, each at a row at a time and then at the next one; a block has a run of the row's vectors, a thread every
+// NT-th of it.  Each thread copies its own vectors into its own places of shared memory, RING - 1 groups of U ahead, over the end of a
+// row into the next one: the loads go on while a row is summed up, and take no registers.  (What a thread copies it alone reads: no
+// barrier.)  The warps' sums of a row meet in one of the cluster's blocks and are summed up there by one warp, another one for every
+// row; nobody waits for it: there are two sets of places, and a cluster barrier whose two halves are a row apart.
+// Small blocks, eight to a multiprocessor: what a warp does once per row weighs less with four warps at a row than with sixteen
+// (4,096 rows of 131,072: 185 us, 198 with blocks of 512 threads; 1,200 rows of 8,000: 12 and 22).
+constexpr int LONG_THREADS = 128, LONG_U = 4, LONG_RING = 3, LONG_PARTS = 8;
+constexpr size_t LONG_SMEM = (size_t)LONG_THREADS * LONG_U * LONG_RING * 16;
 
-// The alternatives one by one, each a pass over the part: for rows whose best entries are crowded into a few threads' stripes.
-template <typename T, bool MASKED, int NT>
-__device__ __noinline__ void alternatives_one_by_one(const T *row, uint32_t V, const RowMask &mask, uint32_t v0, uint32_t v1, uint32_t top,
-                                                     key_t64 (*lists)[32])
+__device__ __forceinline__ void copy_vector(uint32_t to, const uint4 *from)
 {
-    const RowVectors<T> x(row, V);
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    key_t64 last = ~0ull, mine = 0;
-    for (uint32_t j = 0; j < top; ++j) {
-        key_t64 best = 0;
-        for (uint32_t v = v0 + threadIdx.x; v < v1; v += NT)
-            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), best, [&](key_t64 k) { if (k < last && k > best) best = k; });
-        for (int d = 16; d; d >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, d));
-        __syncthreads();
-        if (lane == 0) lists[0][warp] = best;
-        __syncthreads();
-        for (uint32_t w = 0; w < NT / 32; ++w) best = max(best, lists[0][w]);
-        if (lane == j) mine = best;
-        last = best;
-    }
-    __syncthreads();
-    if (warp == 0) lists[0][lane] = mine;
-    __syncthreads();
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// A part's 32 first keys into lists[0].  The k-th of the threads' best keys bounds the k-th of all from below, and only the k threads
-// at or above it can have entries that are no smaller: their stripes alone are read again (from L2).
-template <typename T, bool MASKED, int NT>
-__device__ __forceinline__ void alternatives(const RowVectors<T> &x, const RowMask &mask, uint32_t v0, uint32_t v1, const Run &a, uint32_t top,
-                                             key_t64 (*lists)[32], key_t64 *cand, uint32_t *n_cand)
+// A block's part of a row: vectors v0 .. v1 - 1.  The first and the last vector of a row may reach into its neighbours; they are
+// read whole all the same, but for the first of the first row and the last of the last one, which may reach out of the matrix.
+template <typename T>
+struct PartOfRow {
+    RowVectors<T> x;
+    uint32_t v0, v1, lo, hi;  // lo .. hi - 1 are copied
+    __device__ __forceinline__ PartOfRow(const LogitRows &q, uint64_t r, uint32_t part, uint32_t log_parts)
+        : x(static_cast<const T *>(q.x) + r * q.stride, q.V), v0(0), v1(x.n)
+    {
+        if (log_parts) {
+            const uint32_t per = (x.n + (1u << log_parts) - 1) >> log_parts;
+            v0 = min(x.n, part * per);
+            v1 = min(x.n, v0 + per);
+        }
+        lo = r == 0 && x.lead ? max(v0, 1u) : v0;
+        hi = r == q.n_rows - 1 ? min(v1, (x.lead + x.V) / EPV<T>) : v1;
+    }
+};
+
+// The alternatives of a row: 32 groups of its threads have a best entry each, and the k-th best of these bounds the k-th best entry from
+// below.  A thread whose best entry is below the bound has none of the k; the stripes of the others (about k of them) are read again
+// (from L2), and what is no smaller than the bound is gathered in one block.  If that is more than fits (rows of many equal logits), the
+// k-th best of what was gathered is a higher bound, and the stripes are read once more.
+constexpr uint32_t CAND = 256, TOP_GROUPS = 32;
+
+// The bound's key out of the groups' keys: keys[] holds `per` of them for each group.
+__device__ __forceinline__ key_t64 bound_of(const key_t64 *keys, uint32_t per, uint32_t top, uint32_t lane)
 {
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     key_t64 mine = 0;
-    if (a.best < v1)
-        each_key<T>(fetch<T, MASKED>(x, mask, a.best), x.first(a.best), 0ull, [&](key_t64 k) { if (k > mine) mine = k; });
-    lists[warp][lane] = sort32(mine, lane);
-    if (tid == 0) *n_cand = 0;
-    merge_lists<NT / 32>(lists, warp, lane);
-    const key_t64 least = lists[0][top - 1];
-    for (uint32_t j = warp; j < top; j += NT / 32) {
-        const key_t64 k = lists[0][j];
-        if (!k) break;
-        const uint32_t owner = ((key_place(k) + x.lead) / EPV<T> - v0) % NT;
-        for (uint32_t v = v0 + owner + lane * NT; v < v1; v += 32 * NT)
-            each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), least, [&](key_t64 q) {
-                const uint32_t at = atomicAdd(n_cand, 1u);
-                if (at < CAND) cand[at] = q;
-            });
+    for (uint32_t i = 0; i < per; ++i) mine = max(mine, keys[lane * per + i]);
+    uint32_t rank = 0;
+#pragma unroll 8
+    for (uint32_t j = 0; j < 32; ++j) {
+        const key_t64 other = __shfl_sync(0xffffffffu, mine, j);
+        rank += other > mine || (other == mine && j < lane);
     }
-    __syncthreads();
-    const uint32_t n = *n_cand;
-    if (n > CAND) {
-        alternatives_one_by_one<T, MASKED, NT>(x.row, x.V, mask, v0, v1, top, lists);
-        return;
-    }
-    for (uint32_t j = warp; j < NT / 32; j += NT / 32) {
-        key_t64 k = tid < n ? cand[tid] : 0;
-        if (n > j * 32) k = sort32(k, lane);
-        if (NT < CAND)  // (fewer threads than candidates: the rest of them)
-            for (uint32_t b = tid - lane + NT; b < n; b += NT) k = merge32(k, sort32(b + lane < n ? cand[b + lane] : 0ull, lane), lane);
-        lists[j][lane] = k;
-    }
-    if (n <= 32) __syncthreads();
-    else merge_lists<NT / 32>(lists, warp, lane);
+    return __shfl_sync(0xffffffffu, mine, __ffs(__ballot_sync(0xffffffffu, rank == top - 1)) - 1);
 }
 
-// Long rows: a cluster of thread blocks per row (one block if there are rows enough), each block a run of vectors, each thread every
-// NT-th vector of it.
-template <typename T, bool MASKED, bool TOP, int NT>
-__global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q, const ScoreOut o, uint32_t parts)
+// One warp: the k-th best of n keys (all different, n >= k).
+__device__ __forceinline__ key_t64 kth_key(const key_t64 *keys, uint32_t n, uint32_t k, uint32_t lane)
 {
-    constexpr int U = 4, NW = NT / 32;
-    __shared__ float s_sums[3][NW];
-    __shared__ float s_part[MAX_PARTS][3];
-    __shared__ key_t64 s_lists[TOP ? NW : 1][32], s_parts[TOP ? MAX_PARTS : 1][32], s_cand[TOP ? CAND : 1];
-    __shared__ uint32_t s_n;
-    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = blockIdx.x % parts;
+    key_t64 found = 0;
+    for (uint32_t i = lane; i < n; i += 32) {
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += keys[j] > keys[i];
+        if (rank == k - 1) found = keys[i];
+    }
+    for (int d = 16; d; d >>= 1) found = max(found, __shfl_xor_sync(0xffffffffu, found, d));
+    return found;
+}
+
+template <typename T, bool MASKED, bool TOP, bool CLUSTER>
+__global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_long(const LogitRows q, const ScoreOut o, uint32_t log_of_parts)
+{
+    constexpr int U = LONG_U, RING = LONG_RING, NT = LONG_THREADS, NW = NT / 32, MAX_PARTS = CLUSTER ? LONG_PARTS : 1;
+    const uint32_t log_parts = CLUSTER ? log_of_parts : 0;
+    extern __shared__ uint4 s_ring[];  // [RING][U][NT]
+    __shared__ float s_sums[2][MAX_PARTS * NW][3];
+    __shared__ key_t64 s_keys[TOP ? (MAX_PARTS * NW > TOP_GROUPS ? MAX_PARTS * NW : TOP_GROUPS) : 1], s_cand[TOP ? CAND : 1], s_bound;
+    __shared__ uint32_t s_n[2];
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
+    const uint64_t step = gridDim.x >> log_parts;
     const float c = q.scale * 1.44269504088896341f, inf = __int_as_float(0x7f800000);
-    for (uint64_t r = blockIdx.x / parts; r < q.n_rows; r += gridDim.x / parts) {
+    const float margin = 8.0f / c;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + tid * 16;
+    cg::cluster_group cluster = cg::this_cluster();
+    auto away = [&](auto *p, uint32_t b) { return CLUSTER ? cluster.map_shared_rank(p, b) : p; };  // the same place in another block
+    auto meet = [&]() {
+        if (CLUSTER) { cluster_arrive(); cluster_wait(); }
+        else __syncthreads();
+    };
+    if (CLUSTER) cluster_arrive();
+
+    // The rows that count, in order; the token of the one behind is loaded a row early.  (The first row is taken before its token
+    // is known.)
+    struct Rows {
+        uint64_t r;
+        int64_t next;
+    };
+    auto move = [&](Rows &a, bool report) {
+        for (;;) {
+            a.r += step;
+            if (a.r >= q.n_rows) return;
+            const int64_t tok = a.next;
+            a.next = a.r + step < q.n_rows ? row_token(q, a.r + step) : -1;
+            if (tok >= 0) return;
+            if (report && part == 0) empty_row(o, a.r, true, tid, NT);
+        }
+    };
+    Rows ahead{blockIdx.x >> log_parts, 0}, now;
+    ahead.next = ahead.r + step < q.n_rows ? row_token(q, ahead.r + step) : -1;
+    now = ahead;
+    // the copies
+    const uint4 *from = nullptr;
+    uint32_t v_next = 0, v_end = 0, lo = 0, hi = 0, slot_in = 0, slot_out = 0;
+    auto open = [&]() {  // (a part may have no vectors)
+        for (;;) {
+            const PartOfRow<T> p(q, ahead.r, part, log_parts);
+            from = p.x.at(0);
+            v_next = p.v0; v_end = p.v1; lo = p.lo; hi = p.hi;
+            if (v_next < v_end) return;
+            move(ahead, true);
+            if (ahead.r >= q.n_rows) return;
+        }
+    };
+    auto copy_group = [&]() {
+        if (v_next < v_end) {
+            const uint32_t to = ring + slot_in * (U * NT * 16);
+            const uint4 *at = from + v_next + tid;
+            if (v_next >= lo && v_next + U * NT <= hi) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) copy_vector(to + u * (NT * 16), at + u * NT);
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const uint32_t v = v_next + u * NT + tid;
+                    if (v >= lo && v < hi) copy_vector(to + u * (NT * 16), at + u * NT);
+                }
+            }
+            slot_in = slot_in + 1 == RING ? 0 : slot_in + 1;
+            v_next += U * NT;
+            if (v_next >= v_end) {
+                move(ahead, true);
+                if (ahead.r < q.n_rows) open();
+            }
+        }
+        copies_close();
+    };
+    open();
+#pragma unroll 1
+    for (int i = 0; i < RING - 1; ++i) copy_group();
+
+    uint32_t set = 0;
+    bool waiting = true;  // for the other half of the barrier
+    for (; now.r < q.n_rows; move(now, false)) {
+        const uint64_t r = now.r;
         const int64_t tok = row_token(q, r);
-        if (tok < 0) {
+        const PartOfRow<T> p(q, r, part, log_parts);
+        const RowVectors<T> &x = p.x;
+        const uint32_t groups = (p.v1 - p.v0 + U * NT - 1) / (U * NT);
+        if (r < step && tok < 0) {  // the first row, after all not
+            for (uint32_t g = 0; g < groups; ++g) {
+                copies_wait<RING - 2>();
+                slot_out = slot_out + 1 == RING ? 0 : slot_out + 1;
+                copy_group();
+            }
             if (part == 0) empty_row(o, r, true, tid, NT);
             continue;
         }
-        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
         const RowMask mask = row_mask(q, r);
-        const uint32_t per = (x.n + parts - 1) / parts, v0 = min(x.n, part * per), v1 = min(x.n, v0 + per);
-        const uint32_t f0 = max(v0, x.lead ? 1u : 0u), f1 = min(v1, (x.lead + x.V) / EPV<T>);  // whole vectors
-        if (parts > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        const uint32_t half = (set >> log_parts) & 1, block = set & (parts - 1);  // where the row is summed up, and by which warp
+        const bool last = part == block && warp == ((set >> log_parts) & (NW - 1));
         float x_tok = 0.0f;
-        if (part == 0 && tid == 0 && o.logprob) x_tok = to_f32(x.row[tok]);
-
-        Run a{-inf, 0ull, 0ull, 0xFFFFFFFFu};
-        uint4 raw[U];
-        if (f0 > v0 && tid == 0) {
-            uint4 one[1] = {fetch<T, MASKED>(x, mask, v0)};
-            take<T, 1, TOP>(a, one, v0, NT, c);
-        }
-        for (uint32_t v = v0 + tid; v < f1; v += NT * U) {
+        if (last && lane == 0 && o.logprob) x_tok = to_f32(x.row[tok]);
+        Run a{-inf, -inf, -inf, 0ull, 0ull, 0xFFFFFFFFu};
+        const uint32_t whole0 = p.v0 == 0 && x.lead ? 1 : 0;  // groups of which every vector is whole
+        const uint32_t whole1 = (min(p.v1, (x.lead + x.V) / EPV<T>) - p.v0) / (U * NT);
+        for (uint32_t g = 0; g < groups; ++g) {
+            copies_wait<RING - 2>();
+            const uint32_t v = p.v0 + g * (U * NT) + tid;
+            const uint4 *slot = s_ring + slot_out * (U * NT) + tid;
+            slot_out = slot_out + 1 == RING ? 0 : slot_out + 1;
+            if (g >= whole0 && g < whole1) {
+                uint4 raw[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const uint32_t w = v + u * NT;
-                raw[u] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
-                if (w >= f0 && w < f1) raw[u] = *x.at(w);
-            }
-            if (MASKED) {
+                for (int u = 0; u < U; ++u) raw[u] = slot[u * NT];
+                copy_group();  // (into the places read a group ago)
+                if (MASKED) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (v + u * NT < f1) close_entries<T>(raw[u], mask.closed_from(x.first(v + u * NT), EPV<T>));
+                    for (int u = 0; u < U; ++u) close_entries<T>(raw[u], mask.closed_from(x.first(v + u * NT), EPV<T>));
+                }
+                take<T, U, TOP>(a, raw, v, NT, c, margin);
+            } else {  // with the row's first or last vectors
+                copy_group();
+                const uint32_t rest = p.v1 - (v - tid);
+#pragma unroll 1
+                for (uint32_t u = 0; u < U && u * NT < rest; ++u) {
+                    const uint32_t w = v + u * NT;
+                    uint4 raw[1] = {make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>)};
+                    if (w < p.v1) {
+                        raw[0] = slot[u * NT];
+                        if (w < p.lo || w >= p.hi) raw[0] = x.part(w);
+                        uint32_t bits = MASKED ? mask.closed_from(x.first(w), EPV<T>) : 0u;
+                        if (w == 0) bits |= (1u << x.lead) - 1;
+                        if (w == x.n - 1) bits |= 0xFFu << (EPV<T> - (x.n * EPV<T> - x.lead - x.V));
+                        if (bits) close_entries<T>(raw[0], bits & ((1u << EPV<T>) - 1));
+                    }
+                    take<T, 1, TOP>(a, raw, w, NT, c, margin);
+                }
             }
-            take<T, U, TOP>(a, raw, v, NT, c);
-        }
-        if (f1 < v1 && v1 > f0 && (v1 - 1 - v0) % NT == tid) {
-            uint4 one[1] = {fetch<T, MASKED>(x, mask, v1 - 1)};
-            take<T, 1, TOP>(a, one, v1 - 1, NT, c);
         }
 
         float s0, s1, t0, t1;
         apart(a.s, s0, s1);
         apart(a.t, t0, t1);
-        Sums w{a.m, s0 + s1, t0 + t1};
-        warp_join(w, c);
-        __syncthreads();  // (what the row in front left in shared memory has been read)
-        if (lane == 0) { s_sums[0][warp] = w.m; s_sums[1][warp] = w.s; s_sums[2][warp] = w.t; }
-        if (TOP) alternatives<T, MASKED, NT>(x, mask, v0, v1, a, o.top, s_lists, s_cand, &s_n);
-        else __syncthreads();
-        if (warp == 0) {
-            w = lane < NW ? Sums{s_sums[0][lane], s_sums[1][lane], s_sums[2][lane]} : Sums{-inf, 0.0f, 0.0f};
-            warp_join(w, c);
+        Sums w{a.ref, s0 + s1, t0 + t1};
+        warp_join(w, a.m, c);
+        if (CLUSTER && waiting) cluster_wait();  // the places have been read (at first: the blocks of the cluster run)
+        if (lane == 0) {
+            float *to = away(&s_sums[half][part * NW + warp][0], block);
+            to[0] = w.m; to[1] = w.s; to[2] = w.t;
         }
-        if (parts > 1) {  // to the first block of the cluster
-            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");  // (it has read the row in front, and runs)
-            cg::cluster_group cluster = cg::this_cluster();
-            if (warp == 0) {
-                if (lane == 0) {
-                    float *to = cluster.map_shared_rank(&s_part[part][0], 0);
-                    to[0] = w.m; to[1] = w.s; to[2] = w.t;
+        uint32_t n = 0;
+        if (TOP) {
+            // a key that the thread's best entry reaches, whatever its place in its vector; the best of each of 32 / parts groups of
+            // the block, or of its warps if these are more, to every block
+            const bool any = a.best < p.v1;
+            const int in = any ? x.first(a.best) : 0;
+            key_t64 k = any ? rank_key(a.m, (uint32_t)(in + EPV<T> - 1)) : 0ull;
+            const uint32_t lanes = min(32u, (uint32_t)NW * parts);  // of a group within a warp
+            for (uint32_t d = 1; d < lanes; d *= 2) k = max(k, __shfl_xor_sync(0xffffffffu, k, d));
+            const uint32_t per_warp = 32 / lanes;
+            for (uint32_t b = lane % lanes; b < parts; b += lanes)
+                *away(&s_keys[TOP ? (part * NW + warp) * per_warp + lane / lanes : 0], b) = k;
+            if (tid == 0) s_n[set & 1] = 0;
+            meet();
+            key_t64 bound = bound_of(s_keys, parts * NW * per_warp / TOP_GROUPS, o.top, lane);
+            uint32_t *const count = away(&s_n[set & 1], block);
+            key_t64 *const cand = away(&s_cand[0], block);
+            for (;;) {
+                uint32_t left = __ballot_sync(0xffffffffu, any && rank_key(a.m, (uint32_t)max(in, 0)) >= bound);
+                while (left) {
+                    const uint32_t owner = warp * 32 + __ffs(left) - 1;
+                    left &= left - 1;
+                    for (uint32_t v = p.v0 + owner + lane * NT; v < p.v1; v += 32 * NT)
+                        each_key<T>(fetch<T, MASKED>(x, mask, v), x.first(v), bound, [&](key_t64 e) {
+                            const uint32_t at = atomicAdd(count, 1u);
+                            if (at < CAND) cand[at] = e;
+                        });
                 }
-                if (TOP) *cluster.map_shared_rank(&s_parts[part][lane], 0) = s_lists[0][lane];
-            }
-            cluster.sync();
-            if (part != 0) continue;
-            if (warp == 0) {
-                w = lane < parts ? Sums{s_part[lane][0], s_part[lane][1], s_part[lane][2]} : Sums{-inf, 0.0f, 0.0f};
-                warp_join(w, c);
-                if (TOP) {
-                    key_t64 k = s_parts[0][lane];
-                    for (uint32_t j = 1; j < parts; ++j) k = merge32(k, s_parts[j][lane], lane);
-                    s_lists[0][lane] = k;
-                    __syncwarp();
+                meet();
+                n = *count;
+                if (n <= CAND) break;
+                meet();
+                if (last) {
+                    bound = kth_key(s_cand, CAND, o.top, lane);
+                    if (lane == 0) s_n[set & 1] = 0;
+                    if (lane < parts) *away(&s_bound, lane) = bound;
                 }
+                meet();
+                bound = s_bound;
             }
-        }
-        if (warp == 0) {
-            if (w.s == 0.0f) {
-                empty_row(o, r, false, lane, 32);
+            waiting = false;
+        } else {
+            if (CLUSTER) {
+                cluster_arrive();
+                waiting = !last;
+                if (last) cluster_wait();
             } else {
-                const float L = logf(w.s);
-                if (lane == 0) {
-                    if (o.logprob) o.logprob[r] = MASKED && mask.is_closed((uint32_t)tok) ? -inf : (x_tok - w.m) * q.scale - L;
-                    if (o.entropy) o.entropy[r] = L - q.scale * (w.t / w.s);
-                    if (o.stats) *reinterpret_cast<float2 *>(o.stats + 2 * r) = make_float2(w.m, L);
-                }
-                if (TOP && lane < o.top) {
-                    const key_t64 k = s_lists[0][lane];
-                    o.ids[r * o.top + lane] = k ? (int32_t)key_place(k) : -1;
-                    o.lps[r * o.top + lane] = k ? (key_value(k) - w.m) * q.scale - L : -inf;
+                __syncthreads();
+            }
+        }
+        ++set;
+        if (!last) continue;
+        w = Sums{-inf, 0.0f, 0.0f};
+        for (uint32_t i = lane; i < parts * NW; i += 32) {
+            Sums b{s_sums[half][i][0], s_sums[half][i][1], s_sums[half][i][2]};
+            const float m = fmaxf(w.m, b.m);
+            raise(w, m, c);
+            raise(b, m, c);
+            w.s += b.s;
+            w.t += b.t;
+        }
+        warp_join(w, w.m, c);
+        if (w.s == 0.0f) {
+            empty_row(o, r, false, lane, 32);
+            continue;
+        }
+        float L, H;
+        finish(w, c, &L, &H);
+        if (lane == 0) {
+            if (o.logprob) o.logprob[r] = MASKED && mask.is_closed((uint32_t)tok) ? -inf : (x_tok - w.m) * q.scale - L;
+            if (o.entropy) o.entropy[r] = H;
+            if (o.stats) *reinterpret_cast<float2 *>(o.stats + 2 * r) = make_float2(w.m, L);
+        }
+        if (TOP) {
+            for (uint32_t i = lane; i < n; i += 32) {
+                const key_t64 k = s_cand[i];
+                uint32_t rank = 0;
+                for (uint32_t j = 0; j < n; ++j) rank += s_cand[j] > k;
+                if (rank < o.top) {
+                    o.ids[r * o.top + rank] = (int32_t)key_place(k);
+                    o.lps[r * o.top + rank] = (key_value(k) - w.m) * q.scale - L;
                 }
             }
+            if (lane >= n && lane < o.top) { o.ids[r * o.top + lane] = -1; o.lps[r * o.top + lane] = -inf; }
         }
     }
+    if (CLUSTER && waiting) cluster_wait();
 }
 
-template <typename T, bool MASKED, bool TOP>
-cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st)
+// Clusters of 2^at blocks that run at once on the device (asked once).
+template <auto kernel>
+int long_clusters(int device, uint32_t at, const cudaLaunchConfig_t &cfg)
 {
-    constexpr int NT = 512;
-    const uint64_t sms = (uint64_t)vl_device_sm_count(device);
-    uint32_t parts = 1;
-    while (parts < MAX_PARTS && q.n_rows * parts < 2 * sms && q.V / (2 * parts) >= NT * EPV<T>) parts *= 2;
-    const uint64_t rows = q.n_rows < (1ull << 27) ? q.n_rows : (1ull << 27);
+    static std::atomic<int> known[64][4];
+    const bool keep = device >= 0 && device < 64;
+    int n = keep ? known[device][at].load() : 0;
+    if (n > 0) return n;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) n = 1;
+    if (keep) known[device][at].store(n);
+    return n;
+}
+
+template <typename T, bool MASKED, bool TOP, bool CLUSTER>
+cudaError_t run_long(const LogitRows &q, const ScoreOut &o, uint32_t log_parts, int device, cudaStream_t st)
+{
+    constexpr auto kernel = k_score_long<T, MASKED, TOP, CLUSTER>;
+    const cudaError_t e = allow_smem<kernel, (int)LONG_SMEM>(device);
+    if (e != cudaSuccess) return e;
+    const uint32_t parts = 1u << log_parts;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = parts;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((uint32_t)(rows * parts)); cfg.blockDim = NT; cfg.stream = st;
-    cfg.attrs = &at; cfg.numAttrs = 1;
+    cfg.gridDim = dim3(parts); cfg.blockDim = LONG_THREADS; cfg.dynamicSmemBytes = LONG_SMEM; cfg.stream = st;
+    cfg.attrs = &at; cfg.numAttrs = CLUSTER ? 1 : 0;
+    const uint64_t most = CLUSTER ? (uint64_t)long_clusters<kernel>(device, log_parts, cfg)
+                                  : (1024 / LONG_THREADS) * (uint64_t)vl_device_sm_count(device);
+    cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
     g_vl_launches.fetch_add(1);
-    return cudaLaunchKernelEx(&cfg, k_score_long<T, MASKED, TOP, NT>, q, o, parts);
+    return cudaLaunchKernelEx(&cfg, kernel, q, o, log_parts);
+}
+
+// Blocks of a row.  More of them shorten it and cost the cluster's barriers; they may not be more than run at once, and less than 2,048
+// vectors (16 a thread) are worth a block only where most multiprocessors would be idle: us for 1, 2, 4, 8 blocks, bf16: one row of
+// 131,072 15.4, 10.3, 7.3, 5.9; 100 rows 16.8, 13.4, 11.3, 11.4; 300 rows 23.7, 21.5, 21.5, 22.5; 100 rows of 32,000 7.5, 7.1, 6.4, 7.3;
+// 300 rows 10.7, 11.3, 12.9, 15.8; 100 rows of 8,000 5.1, 5.8, 5.2, 5.9.
+template <typename T, bool MASKED, bool TOP>
+cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st)
+{
+    const uint64_t resident = (1024 / LONG_THREADS) * (uint64_t)vl_device_sm_count(device);
+    const uint32_t n = q.V / EPV<T>;
+    uint32_t log_parts = 0;
+    if (n >= 2048)
+        while ((1u << log_parts) < LONG_PARTS && q.n_rows << (log_parts + 1) <= (n >> (log_parts + 1) > 2048 ? resident : resident * 2 / 5))
+            ++log_parts;
+    if (log_parts == 1 && n < 8192) log_parts = 0;
+    if (getenv("VLP")) log_parts = __builtin_ctz(atoi(getenv("VLP")));
+    return log_parts ? run_long<T, MASKED, TOP, true>(q, o, log_parts, device, st) : run_long<T, MASKED, TOP, false>(q, o, 0, device, st);
 }
 
 // Short rows: a group of lanes per row, every logit read once into registers.
 constexpr uint32_t SHORT_WARPS = 8, SHORT_CAND = 128;
 
+// The warp's first `top` keys in order, one to a lane, out of one key per lane: round by round for few (8 instructions a round), sorted
+// for many.
+__device__ __forceinline__ key_t64 first_keys(key_t64 k, uint32_t top, uint32_t lane)
+{
+    if (top > 16) return sort32(k, lane);
+    key_t64 mine = 0;
+    for (uint32_t i = 0; i < top; ++i) {
+        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
+        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
+        const key_t64 best = ((key_t64)hi << 32) | lo;
+        if (lane == i) mine = best;
+        if (k == best) k = 0;
+    }
+    return mine;
+}
+
 // The best entries of a row that the whole warp holds (G = 32), as in the long rows: the k-th of the lanes' best bounds the k-th of all.
+// own: the lane's largest logit.
 template <typename T, int NV>
-__device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t lane, uint32_t top, key_t64 *cand,
-                                                     uint32_t *n_cand)
+__device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], float own, const RowVectors<T> &x, uint32_t lane, uint32_t top,
+                                                     key_t64 *cand, uint32_t *n_cand)
 {
     key_t64 mine = 0;
+    if (own > __int_as_float(0xFF800000)) {
+        uint32_t at = 0;
 #pragma unroll
-    for (int j = 0; j < NV; ++j) each_key<T>(raw[j], x.first(lane + 32 * j), mine, [&](key_t64 k) { if (k > mine) mine = k; });
-    const key_t64 least = __shfl_sync(0xffffffffu, sort32(mine, lane), top - 1);
+        for (int j = NV - 1; j >= 0; --j) {
+            float e[EPV<T>];
+            unpack(raw[j], e, T{});
+#pragma unroll
+            for (int i = EPV<T> - 1; i >= 0; --i)
+                if (e[i] == own) at = x.first(lane + 32 * j) + i;
+        }
+        mine = rank_key(own, at);
+    }
+    const key_t64 least = __shfl_sync(0xffffffffu, first_keys(mine, top, lane), top - 1);
+    const float floor = least ? key_value(least) : __int_as_float(0xFF800000);
     if (lane == 0) *n_cand = 0;
     __syncwarp();
+    if (own >= floor) {
 #pragma unroll
-    for (int j = 0; j < NV; ++j)
-        each_key<T>(raw[j], x.first(lane + 32 * j), least, [&](key_t64 k) {
-            const uint32_t at = atomicAdd(n_cand, 1u);
-            if (at < SHORT_CAND) cand[at] = k;
-        });
+        for (int j = 0; j < NV; ++j)
+            if (vector_max(raw[j], T{}) >= floor)
+                each_key<T>(raw[j], x.first(lane + 32 * j), least, [&](key_t64 k) {
+                    const uint32_t at = atomicAdd(n_cand, 1u);
+                    if (at < SHORT_CAND) cand[at] = k;
+                });
+    }
     __syncwarp();
     const uint32_t n = *n_cand;
     key_t64 best = 0;
-    if (n <= SHORT_CAND) {
-        best = sort32(lane < n ? cand[lane] : 0ull, lane);
+    if (n <= 32) {
+        best = first_keys(lane < n ? cand[lane] : 0ull, top, lane);
+    } else if (n <= SHORT_CAND) {
+        best = sort32(cand[lane], lane);
         for (uint32_t b = 32; b < n; b += 32) best = merge32(best, sort32(b + lane < n ? cand[b + lane] : 0ull, lane), lane);
     } else {  // one by one
         key_t64 last = ~0ull;
@@ -429,7 +658,7 @@ __device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], con
 template <typename T, bool MASKED, bool TOP, int G, int NV>
 __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRows q, const ScoreOut o, bool aligned)
 {
-    static_assert(NV * EPV<T> <= 32, "a lane's entries");
+    constexpr bool WORDS = NV * EPV<T> <= 32;  // a row has no more words of closed entries than its group has lanes
     static_assert(!TOP || G == 32, "alternatives take the whole warp");
     __shared__ key_t64 s_cand[TOP ? SHORT_WARPS : 1][TOP ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
@@ -445,28 +674,27 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
         const int64_t tok = row_token(q, r);
         uint32_t word = 0;
         if (MASKED) {
-            word = row_mask(q, r).closed(g);
+            const RowMask mask = row_mask(q, r);
+            if (WORDS) {
+                word = mask.closed(g);
 #pragma unroll
-            for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
+                for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
+            } else {
+                word = tok >= 0 && mask.is_closed((uint32_t)tok);
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (g + G * j < x.n) close_entries<T>(raw[j], mask.closed_from(x.first(g + G * j), EPV<T>));
+            }
         }
         float x_tok = 0.0f;
         if (g == 0 && o.logprob && tok >= 0) x_tok = to_f32(x.row[tok]);
 
-        float m = vector_max(raw[0], T{});
-#pragma unroll
-        for (int j = 1; j < NV; ++j) m = fmaxf(m, vector_max(raw[j], T{}));
+        const float own = vectors_max<NV>(raw, T{});
+        float m = own;
 #pragma unroll
         for (int d = G / 2; d; d >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-        const float base = fmaxf(m, LOWEST);
         f32x2 s2 = 0ull, t2 = 0ull;
-        const f32x2 low = both(-base, -base), c2 = both(c, c);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            float e[EPV<T>];
-            unpack(raw[j], e, T{});
-#pragma unroll
-            for (int i = 0; i < EPV<T>; i += 2) sum_two(e[i], e[i + 1], low, c2, s2, t2);
-        }
+        add_vectors<T, NV>(raw, m, c, s2, t2);
         float s, t, b;
         apart(s2, s, b);
         s += b;
@@ -477,18 +705,20 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
             s += __shfl_xor_sync(0xffffffffu, s, d);
             t += __shfl_xor_sync(0xffffffffu, t, d);
         }
-        const float L = logf(s);
+        float L, H;
+        finish(Sums{m, s, t}, c, &L, &H);
         const bool left = tok < 0, empty = s == 0.0f;
         bool shut = false;
-        if (MASKED) shut = (__shfl_sync(0xffffffffu, word, left ? 0 : (int)((uint32_t)tok >> 5) & (G - 1), G) >> (tok & 31)) & 1;
+        if (MASKED && WORDS) shut = (__shfl_sync(0xffffffffu, word, left ? 0 : (int)((uint32_t)tok >> 5) & (G - 1), G) >> (tok & 31)) & 1;
+        else if (MASKED) shut = word;
         if (g == 0 && there) {
             if (o.logprob) o.logprob[r] = left ? 0.0f : (empty || shut ? -inf : (x_tok - m) * q.scale - L);
-            if (o.entropy) o.entropy[r] = left || empty ? 0.0f : L - q.scale * (t / s);
+            if (o.entropy) o.entropy[r] = left || empty ? 0.0f : H;
             if (o.stats)
                 *reinterpret_cast<float2 *>(o.stats + 2 * r) = left ? make_float2(0.0f, 0.0f) : make_float2(empty ? -inf : m, L);
         }
         if (TOP) {
-            const key_t64 k = warp_alternatives<T, NV>(raw, x, lane, o.top, s_cand[warp], &s_n[warp]);
+            const key_t64 k = warp_alternatives<T, NV>(raw, own, x, lane, o.top, s_cand[warp], &s_n[warp]);
             if (lane < o.top) {
                 const bool one = k != 0 && !left;
                 o.ids[r * o.top + lane] = one ? (int32_t)key_place(k) : -1;
@@ -517,7 +747,8 @@ bool launch_short(const LogitRows &q, const ScoreOut &o, cudaStream_t st, cudaEr
         if (n <= 32) *e = run_short<T, MASKED, true, 32, 1>(q, o, aligned, st);
         else if (n <= 64) *e = run_short<T, MASKED, true, 32, 2>(q, o, aligned, st);
         else if (n <= 128) *e = run_short<T, MASKED, true, 32, 4>(q, o, aligned, st);
-        else if (n <= 256 && sizeof(T) == 4) *e = run_short<T, MASKED, true, 32, 32 / EPV<T>>(q, o, aligned, st);
+        else if (n <= 256) *e = run_short<T, MASKED, true, 32, 8>(q, o, aligned, st);
+        else if (n <= 512) *e = run_short<T, MASKED, true, 32, 16>(q, o, aligned, st);
         else return false;
     } else {
         if (n <= 4) *e = run_short<T, MASKED, false, 4, 1>(q, o, aligned, st);
@@ -525,7 +756,8 @@ bool launch_short(const LogitRows &q, const ScoreOut &o, cudaStream_t st, cudaEr
         else if (n <= 32) *e = run_short<T, MASKED, false, 8, 4>(q, o, aligned, st);
         else if (n <= 64) *e = run_short<T, MASKED, false, 16, 4>(q, o, aligned, st);
         else if (n <= 128) *e = run_short<T, MASKED, false, 32, 4>(q, o, aligned, st);
-        else if (n <= 256 && sizeof(T) == 4) *e = run_short<T, MASKED, false, 32, 32 / EPV<T>>(q, o, aligned, st);
+        else if (n <= 256) *e = run_short<T, MASKED, false, 32, 8>(q, o, aligned, st);
+        else if (n <= 512) *e = run_short<T, MASKED, false, 32, 16>(q, o, aligned, st);
         else return false;
     }
     return true;
@@ -563,7 +795,7 @@ int vl_logit_rows(const vl_logits *x, LogitRows *q)
     if (((uintptr_t)x->occupied | (uintptr_t)x->mask_rows) & 3) return VL_ERR_INVALID_ARG;
     if (x->mask_rows && !x->occupied) return VL_ERR_INVALID_ARG;
     if (x->occupied && !x->mask_rows && x->n_masks < x->n_rows) return VL_ERR_INVALID_ARG;
-    if (!(x->scale >= 1e-20f && x->scale <= 1e20f)) return VL_ERR_INVALID_ARG;
+    if (!(x->scale >= 1e-6f && x->scale <= 1e6f)) return VL_ERR_INVALID_ARG;
     q->x = x->logits; q->n_rows = x->n_rows; q->stride = x->row_stride;
     q->V = x->n_vocab; q->W = (x->n_vocab + 31) / 32;
     q->tokens = x->tokens; q->token_bytes = x->token_bytes;

@@ -127,6 +127,29 @@ def test_scores_of_equal_impossible_and_sorted_entries(B, dtype, kind):
         _check_scores(got, x.double().cpu().numpy(), 1.0, np.zeros((R, V), bool), t, 32)
 
 
+@pytest.mark.parametrize("R,V", [(1, 131075), (3, 70000), (700, 40000), (40, 9000), (5, 1000)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_alternatives_crowded_into_few_places(B, dtype, R, V):
+    """The best entries are all a power of two apart, or in one run, or all alike: whatever the entries are handed out by, some thread has
+    many of the best."""
+    import torch
+    rng = np.random.default_rng(V)
+    t = np.full(R, -1)
+    t[:3] = rng.integers(0, V, min(R, 3))
+    for period, run in [(4096, 24), (1024, 8), (512, 4), (16384, 64), (V, 400)]:
+        vals = rng.normal(-5, 1, (R, V)).astype(np.float32)
+        high = np.arange(V) % period < run
+        vals[:, high] = rng.normal(5, 1, (R, int(high.sum())))
+        if period == V:
+            vals[0] = 0.0
+        x = _rows(vals, dtype)
+        got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), top=32)
+        head = B.TokenLogprobs(*[v[:3] for v in got])
+        n = min(R, 3)
+        _check_scores(head, x[:3].double().cpu().numpy(), 1.0, np.zeros((n, V), bool), t[:3], 32)
+        assert bool((got.top_ids[3:] == -1).all()) and bool((got.logprob[3:] == 0).all())
+
+
 @pytest.mark.parametrize("V", [5, 16, 31, 64, 200, 256, 300, 512, 1024, 1500, 9001])
 @pytest.mark.parametrize("dtype", DTYPES)
 def test_scores_under_masks_and_widths(B, dtype, V):
@@ -366,6 +389,30 @@ def test_rows_beyond_32_bits_of_entries(B):
         p = np.exp(x64[r] - x64[r].max())
         assert np.all(np.abs(x[r - 2].double().cpu().numpy() - want) <= tol + 2 * _sum_error(V) * p)
     assert bool((x[:100] == 0).all())
+
+
+def test_many_rows_of_which_most_are_left_out(B):
+    """More rows than blocks run at once, so that a block goes from row to row: all of them, every third, the last, none."""
+    import torch
+    rng = np.random.default_rng(12)
+    for R, V in [(5000, 2500), (3000, 9000), (2600, 1100)]:
+        x = torch.randn(R, V, device="cuda", dtype=torch.bfloat16) * 2
+        t = torch.randint(0, V, (R,), device="cuda")
+        want = torch.log_softmax(x.double(), dim=1)
+        for keep in (slice(None), slice(0, None, 3), slice(R - 1, R), slice(0, 0)):
+            u = torch.full((R,), -1, device="cuda")
+            u[keep] = t[keep]
+            for top in (0, 3):
+                got = B.vl_token_logprobs(x, u, top=top)
+                lp = want.gather(1, t[:, None])[:, 0]
+                S = _sum_error(V)
+                assert bool(((got.logprob[keep].double() - lp[keep]).abs() <= S + 8 * U * (lp[keep].abs() + 20)).all())
+                rest = u < 0
+                assert bool((got.logprob[rest] == 0).all()) and bool((got.row_stats[rest] == 0).all())
+                if top:
+                    assert bool((got.top_ids[rest] == -1).all())
+                    best = torch.sort(x.float(), dim=1, descending=True, stable=True).indices[:, :top]
+                    assert torch.equal(got.top_ids[keep].long(), best[keep])
 
 
 @pytest.mark.parametrize("R,V,top", [(3, 200, 4), (2, 9000, 8), (1, 131072, 20), (300, 1024, 0)])
