@@ -19,7 +19,6 @@ namespace {
 namespace cg = cooperative_groups;
 typedef unsigned long long key_t64;
 
-constexpr float LOWEST = -3.402823466e38f;
 
 struct ScoreOut {
     float *logprob, *entropy, *stats;
@@ -66,12 +65,10 @@ __device__ __forceinline__ key_t64 merge32(key_t64 a, key_t64 b, uint32_t lane)
 // In powers of two: y_i = c x_i - B with c = scale log2 e and B = c m rounded, m the largest logit so far; s = sum 2^y, t = sum 2^y y.
 // One multiply-add makes y, and B being rounded makes no difference: it is the same B in every term, and what it lacks to c m is put
 // right once, at the end.  Where c x would leave the range of numbers (FAR_OUT), y is (x - m) c.
-constexpr float FAR_OUT = 1e29f;     // times c (scale <= 1e6) it is a number
 constexpr float FAR_BELOW = -1e30f;  // stands for minus infinity, whose 2^y y would be none: its power of two is 0 (scale >= 1e-6)
 struct Sums {
     float m, s, t;
 };
-__device__ __forceinline__ bool far_out(float m) { return !(fabsf(m) < FAR_OUT); }
 // What sums relative to m lack to sums relative to the larger m1, as a power of two.
 __device__ __forceinline__ float step_down(float m, float m1, float c)
 {
@@ -100,9 +97,9 @@ __device__ __forceinline__ void warp_join(Sums &a, float m, float c)
 // L = ln sum exp(scale (x - m)), and the entropy.
 __device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *H)
 {
-    const float ln2 = 0.693147180559945309f, ln_s = logf(a.s);
-    *L = far_out(a.m) ? ln_s : fmaf(ln2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
-    *H = ln_s - ln2 * __fdividef(a.t, a.s);  // (s is between 1/2 and 2^31)
+    const float ln_s = logf(a.s);
+    *L = far_out(a.m) ? ln_s : fmaf(LN2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
+    *H = ln_s - LN2 * __fdividef(a.t, a.s);  // (s is between 1/2 and 2^31)
 }
 
 // The entries of vectors into the sums relative to m.
@@ -294,7 +291,7 @@ __global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_lon
     __shared__ uint32_t s_n[2];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
     const uint64_t step = gridDim.x >> log_parts;
-    const float c = q.scale * 1.44269504088896341f, inf = __int_as_float(0x7f800000);
+    const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000);
     const float margin = 8.0f / c;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + tid * 16;
     cg::cluster_group cluster = cg::this_cluster();
@@ -663,7 +660,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
     __shared__ key_t64 s_cand[TOP ? SHORT_WARPS : 1][TOP ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
-    const float c = q.scale * 1.44269504088896341f, inf = __int_as_float(0x7f800000);
+    const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000);
     const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
     for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
         const uint64_t r = min(r0 + lane / G, q.n_rows - 1);

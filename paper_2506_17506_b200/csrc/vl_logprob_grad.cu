@@ -1,11 +1,15 @@
 // The gradient of vl_token_logprobs to the logits.  With l_i = log p_i = scale (x_i - M) - L:
 //   d logprob / d x_i = scale ([i = token] - p_i),   d entropy / d x_i = -scale p_i (l_i + entropy)
 // p is recomputed from the logits and the row's two statistics: nothing but these is kept from the forward pass.
+//
+// In powers of two, with y = log2 p: d_i = 2^y (a + b y), a = -scale (g + h entropy), b = -scale h ln 2, and scale g more at the token.
+// y = c x - K, c = scale log2 e, K = c M + L log2 e, is one multiply-add; K is rounded, and what it lacks, the same in the whole row,
+// goes into a and b.  Each value is rounded once.
+//
+// What bounds it: the logits read and the gradient written, once each, and per element an exponential and about five more instructions.
 #include "vl_logits.cuh"
 
 namespace {
-
-constexpr uint32_t GRAD_THREADS = 256;
 
 struct GradIn {
     const float *stats, *entropy, *g, *h;
@@ -13,31 +17,186 @@ struct GradIn {
     uint64_t stride;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(GRAD_THREADS) k_score_grad(const LogitRows q, const GradIn p)
+// What a row's entries have in common.
+struct GradRow {
+    float c, K, a, b, at_token;
+    float M, L2;  // for rows far out
+    bool far, dead;
+    int tok;
+};
+__device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p, uint64_t r, const RowMask &mask, bool masked)
 {
-    const float inf = __int_as_float(0x7f800000);
-    for (uint64_t r = blockIdx.x; r < q.n_rows; r += gridDim.x) {
-        const int64_t tok = row_token(q, r);
-        const float M = p.stats[2 * r], L = p.stats[2 * r + 1];
-        const T *x = static_cast<const T *>(q.x) + r * q.stride;
-        T *dx = static_cast<T *>(p.dx) + r * p.stride;
+    GradRow w;
+    const int64_t tok = row_token(q, r);
+    const float2 st = *reinterpret_cast<const float2 *>(p.stats + 2 * r);
+    float g = p.g ? p.g[r] : 0.0f;
+    const float h = p.h ? p.h[r] : 0.0f, H = p.h ? p.entropy[r] : 0.0f;
+    w.tok = (int)tok;
+    w.dead = tok < 0 || st.y == __int_as_float(0xFF800000);
+    if (masked && p.g && !w.dead && mask.is_closed((uint32_t)tok)) g = 0.0f;
+    w.c = q.scale * LOG2E;
+    w.M = st.x;
+    w.far = far_out(st.x);
+    w.L2 = st.y * LOG2E;
+    const float B = __fmul_rn(st.x, w.c), K = __fadd_rn(B, w.L2), k = __fsub_rn(K, B);
+    // what K lacks: the rounded bits of the sum and of both products
+    const float lacks = __fadd_rn(__fsub_rn(B, __fsub_rn(K, k)), __fsub_rn(w.L2, k)) + __fmaf_rn(st.x, w.c, -B) + __fmaf_rn(st.y, LOG2E, -w.L2);
+    const float a = -q.scale * fmaf(h, H, g), b = -q.scale * h * LN2;
+    w.K = K;
+    const float f = w.far ? 1.0f : ex2(-lacks);
+    w.a = w.far ? a : f * fmaf(-b, lacks, a);
+    w.b = f * b;
+    w.at_token = q.scale * g;
+    return w;
+}
+
+constexpr float FLOOR = -300.0f;  // 2^-300 is 0, and 0 (a + b y) too
+
+// The gradient of a vector that begins at entry `first`.
+template <typename T>
+__device__ __forceinline__ uint4 grad_vector(const uint4 &raw, int first, const GradRow &w)
+{
+    float x[EPV<T>], d[EPV<T>];
+    unpack(raw, x, T{});
+    const f32x2 c2 = both(w.c, w.c), K2 = both(-w.K, -w.K), a2 = both(w.a, w.a), b2 = both(w.b, w.b);
+#pragma unroll
+    for (int j = 0; j < EPV<T>; j += 2) {
+        float y0, y1;
+        if (!w.far) {
+            apart(fma2(both(x[j], x[j + 1]), c2, K2), y0, y1);
+        } else {
+            y0 = (x[j] - w.M) * w.c - w.L2;
+            y1 = (x[j + 1] - w.M) * w.c - w.L2;
+        }
+        y0 = max_nan(y0, FLOOR);
+        y1 = max_nan(y1, FLOOR);
+        apart(mul2(both(ex2(y0), ex2(y1)), fma2(b2, both(y0, y1), a2)), d[j], d[j + 1]);
+    }
+    const uint32_t at = (uint32_t)(w.tok - first);
+    if (at < (uint32_t)EPV<T>) {
+#pragma unroll
+        for (int j = 0; j < EPV<T>; ++j)
+            if ((uint32_t)j == at) d[j] += w.at_token;
+    }
+    return pack(d, T{});
+}
+
+// A vector's entries one by one, those that are in the row.
+template <typename T>
+__device__ __forceinline__ void store_entries(T *row, int first, uint32_t V, const uint4 &d)
+{
+    T e[EPV<T>];
+    memcpy(e, &d, 16);
+#pragma unroll
+    for (int j = 0; j < EPV<T>; ++j)
+        if ((uint32_t)(first + j) < V) row[first + j] = e[j];
+}
+
+// Long rows: a block per row and run of GRAD_TILE vectors.
+constexpr int GRAD_THREADS = 256, GRAD_U = 4, GRAD_TILE = GRAD_THREADS * GRAD_U;
+
+template <typename T, bool MASKED>
+__global__ void __launch_bounds__(GRAD_THREADS) k_grad_long(const LogitRows q, const GradIn p)
+{
+    const uint64_t step = (uint64_t)gridDim.y * gridDim.z;
+    for (uint64_t r = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z; r < q.n_rows; r += step) {
+        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
+        T *const dx = static_cast<T *>(p.dx) + r * p.stride;
+        const bool alike = ((uintptr_t)dx & 15) == x.lead * sizeof(T);  // vectors of one are vectors of the other
+        uint4 *const to = reinterpret_cast<uint4 *>(reinterpret_cast<uintptr_t>(dx) & ~(uintptr_t)15);
+        const uint32_t v0 = blockIdx.x * GRAD_TILE + threadIdx.x;
+        uint4 raw[GRAD_U];
+#pragma unroll
+        for (int u = 0; u < GRAD_U; ++u) {
+            const uint32_t v = v0 + u * GRAD_THREADS;
+            raw[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (v < x.n && x.whole(v)) raw[u] = __ldcs(x.at(v));
+        }
         const RowMask mask = row_mask(q, r);
-        const bool masked = mask.any(), dead = tok < 0 || L == -inf;
-        const float H = p.h && !dead ? p.entropy[r] : 0.0f, h = p.h && !dead ? p.h[r] : 0.0f;
-        const float g = !p.g || dead || (masked && mask.is_closed((uint32_t)tok)) ? 0.0f : p.g[r];
-        for (uint32_t i = threadIdx.x; i < q.V; i += GRAD_THREADS) {
-            float d = 0.0f;
-            if (!dead && !(masked && mask.is_closed(i))) {
-                const float l = (to_f32(x[i]) - M) * q.scale - L;
-                const float e = expf(l);
-                d = e == 0.0f ? 0.0f : -e * (g + h * (l + H));
-                if ((int64_t)i == tok) d += g;
-                d *= q.scale;
-            }
-            from_f32(dx[i], d);
+        const GradRow w = grad_row(q, p, r, mask, MASKED);
+#pragma unroll
+        for (int u = 0; u < GRAD_U; ++u) {
+            const uint32_t v = v0 + u * GRAD_THREADS;
+            if (v >= x.n) break;
+            const bool whole = x.whole(v);
+            const int first = x.first(v);
+            if (!whole) raw[u] = x.part(v);
+            if (MASKED) close_entries<T>(raw[u], mask.closed_from(first, EPV<T>));
+            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[u], first, w);
+            if (whole && alike) __stcs(to + v, d);
+            else store_entries<T>(dx, first, q.V, d);
         }
     }
+}
+
+// Short rows: a group of lanes per row.
+constexpr uint32_t SHORT_WARPS = 8;
+
+template <typename T, bool MASKED, int G, int NV>
+__global__ void __launch_bounds__(SHORT_WARPS * 32) k_grad_short(const LogitRows q, const GradIn p, bool aligned, bool out_aligned)
+{
+    constexpr bool WORDS = NV * EPV<T> <= 32;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
+    const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
+    for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
+        const bool there = r0 + lane / G < q.n_rows;
+        const uint64_t r = there ? r0 + lane / G : q.n_rows - 1;
+        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
+        uint4 raw[NV];
+        if (there) fetch_row<T, G, NV>(raw, x, g, aligned);
+        const RowMask mask = row_mask(q, r);
+        const GradRow w = grad_row(q, p, r, mask, MASKED);
+        if (MASKED) {
+            if (WORDS) {
+                const uint32_t word = mask.closed(g);
+#pragma unroll
+                for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
+            } else {
+#pragma unroll
+                for (int j = 0; j < NV; ++j)
+                    if (g + G * j < x.n) close_entries<T>(raw[j], mask.closed_from(x.first(g + G * j), EPV<T>));
+            }
+        }
+        if (!there) continue;
+        T *const dx = static_cast<T *>(p.dx) + r * p.stride;
+        uint4 *const to = reinterpret_cast<uint4 *>(dx) + g;  // (aligned ones only)
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t v = g + G * j;
+            if (v >= x.n) break;
+            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[j], x.first(v), w);
+            if (aligned && out_aligned) to[G * j] = d;
+            else store_entries<T>(dx, x.first(v), q.V, d);
+        }
+    }
+}
+
+template <typename T, bool MASKED, int G, int NV>
+void run_short(const LogitRows &q, const GradIn &p, bool aligned, cudaStream_t st)
+{
+    const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
+    const bool out_aligned = ((uintptr_t)p.dx & 15) == 0 && (q.n_rows <= 1 || p.stride % EPV<T> == 0);
+    k_grad_short<T, MASKED, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, p, aligned, out_aligned);
+}
+
+template <typename T, bool MASKED>
+cudaError_t launch(const LogitRows &q, const GradIn &p, cudaStream_t st)
+{
+    bool aligned;
+    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
+    if (n <= 4) run_short<T, MASKED, 4, 1>(q, p, aligned, st);
+    else if (n <= 16) run_short<T, MASKED, 4, 4>(q, p, aligned, st);
+    else if (n <= 32) run_short<T, MASKED, 8, 4>(q, p, aligned, st);
+    else if (n <= 64) run_short<T, MASKED, 16, 4>(q, p, aligned, st);
+    else if (n <= 128) run_short<T, MASKED, 32, 4>(q, p, aligned, st);
+    else if (n <= 256) run_short<T, MASKED, 32, 8>(q, p, aligned, st);
+    else {
+        const uint32_t y = (uint32_t)(q.n_rows < 65535 ? q.n_rows : 65535);
+        const uint64_t z = (q.n_rows + y - 1) / y;
+        k_grad_long<T, MASKED><<<dim3((n + GRAD_TILE - 1) / GRAD_TILE, y, (uint32_t)(z < 65535 ? z : 65535)), GRAD_THREADS, 0, st>>>(q, p);
+    }
+    g_vl_launches.fetch_add(1);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -61,11 +220,11 @@ extern "C" int vl_token_logprobs_backward(int device, const vl_logits *x, const 
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
     const GradIn p{d_row_stats, d_entropy, d_g_logprob, d_g_entropy, d_dlogits, out_stride};
-    const uint32_t blocks = (uint32_t)(q.n_rows < 0x7FFFFFFFull ? q.n_rows : 0x7FFFFFFFull);
     cudaStream_t st = (cudaStream_t)stream;
-    if (x->dtype == VL_F32) k_score_grad<float><<<blocks, GRAD_THREADS, 0, st>>>(q, p);
-    else if (x->dtype == VL_F16) k_score_grad<__half><<<blocks, GRAD_THREADS, 0, st>>>(q, p);
-    else k_score_grad<__nv_bfloat16><<<blocks, GRAD_THREADS, 0, st>>>(q, p);
-    g_vl_launches.fetch_add(1);
-    return cudaGetLastError() == cudaSuccess ? VL_OK : VL_ERR_CUDA;
+    const bool masked = q.occupied || q.widths;
+    cudaError_t e;
+    if (x->dtype == VL_F32) e = masked ? launch<float, true>(q, p, st) : launch<float, false>(q, p, st);
+    else if (x->dtype == VL_F16) e = masked ? launch<__half, true>(q, p, st) : launch<__half, false>(q, p, st);
+    else e = masked ? launch<__nv_bfloat16, true>(q, p, st) : launch<__nv_bfloat16, false>(q, p, st);
+    return e == cudaSuccess ? VL_OK : VL_ERR_CUDA;
 }

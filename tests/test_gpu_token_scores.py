@@ -212,7 +212,8 @@ def test_rows_of_the_lowest_value_and_of_no_numbers(B, dtype, V):
     dx = B.vl_token_logprobs_backward(x[:4], torch.from_numpy(t[:4]).cuda(), got.row_stats[:4].contiguous(),
                                       torch.ones(4, device="cuda"), entropy=got.entropy[:4].contiguous(), g_entropy=torch.ones(4, device="cuda"))
     assert bool(torch.isfinite(dx.float()).all())
-    assert bool((dx[3] == 0).all()) and float(dx[1].float().abs().max()) == 0.0
+    # the token has all of the probability: g (1 - p) with p = 1 within 6 u, and a few u of the two terms' size in their sum
+    assert bool((dx[3] == 0).all()) and float(dx[1].float().abs().max()) <= 16 * U
     assert bool((dx[2, ::2] == 0).all())
 
 
