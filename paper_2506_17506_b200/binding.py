@@ -612,7 +612,7 @@ def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None,
     with scope:
         work = torch.empty(size, dtype=torch.uint8, device=dev)
         f = torch.empty(1 + N + T, dtype=torch.float32, device=dev)
-    loss, adv, g = f[0], f[1:1 + N], f[1 + N:]
+    g, adv, loss = f[:T], f[T:T + N], f[T + N]        # (the derivative on 16 bytes)
     rc = _lib.vl_policy_loss(dev.index, n, op, Ks, off, T, lp, old, ref, C.byref(rules), loss.data_ptr(), adv.data_ptr(), g.data_ptr(),
                              work.data_ptr(), size, ptr)
     if rc != VL_OK:

@@ -3,25 +3,35 @@
 //
 //   reward = [pass] - pair_cost conflict_pairs - bank_cost bank_conflicts,   A = reward - mean  (/ (std + eps))
 //   d = logprob - old, rho = exp d,  token loss = -min(rho A, clip(rho) A) + kl (exp q - q - 1),  q = ref - logprob
-// The sign of a token loss's sum rests on small differences (A sums to nothing within a program, rho is near 1): rewards,
-// advantages and sums are held in 64 bits, rho - 1 comes from expm1, and the clip's borders are compared as logarithms in 64 bits.
+// The loss rests on small differences (A sums to nothing within a program, rho is near 1): rewards, advantages and sums are held in 64
+// bits, rho - 1 comes from expm1, and on which side of a border of the clip a token lies is decided as in exact arithmetic.
+//
+// Three kernels: k_advantages, a cluster or a block per program, leaves each candidate's weight and weighted advantage; k_policy_tokens
+// streams the tokens, which is what bounds it (12 to 16 bytes a token), each warp a run of them, finding candidates by their
+// offsets; k_policy_sum adds the blocks' sums in order.
+#include <cooperative_groups.h>
 #include <math.h>
 
 #include "vl_logits.cuh"
 
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr uint32_t PL_GROUPS = 96;    // programs per launch (their pointers travel as kernel arguments)
-constexpr uint32_t PL_THREADS = 256;
-constexpr uint32_t PL_TILE = 2048;    // tokens of a block
+constexpr uint32_t PL_THREADS = 256, PL_WARPS = PL_THREADS / 32;
+constexpr uint32_t PL_STEP = 128;     // tokens of a warp at a time, four to a lane
+constexpr uint32_t PL_MAX_BLOCKS = 2048;
 
 struct GroupParams {
     const uint4 *out[PL_GROUPS];
     uint64_t K[PL_GROUPS], first[PL_GROUPS];  // first: candidate number of its first row
     double pair_cost, bank_cost, eps;
-    double *adv;
+    const int64_t *off;
+    uint64_t N, T;
+    double2 *weights;  // [N] weight of a token of the candidate, and times the advantage
     float *advantage;
-    int normalise;
+    int normalise, per_token;
 };
 
 __device__ __forceinline__ double reward_of(const uint4 &v, double pair_cost, double bank_cost)
@@ -42,102 +52,256 @@ __device__ __forceinline__ double block_sum(double v, double *s)
     return v;
 }
 
-// One block per program.
-__global__ void __launch_bounds__(PL_THREADS) k_advantages(const GroupParams q)
+__device__ __forceinline__ int64_t inside(int64_t t, uint64_t T) { return min(max(t, (int64_t)0), (int64_t)T); }
+
+// A cluster of blocks per program.  A thread's first rewards stay in registers.
+constexpr uint32_t ADV_THREADS = 512, ADV_KEEP = 4;
+__global__ void __launch_bounds__(ADV_THREADS) k_advantages(const __grid_constant__ GroupParams q)
 {
-    __shared__ double s[PL_THREADS / 32];
-    const uint32_t j = blockIdx.x;
-    const uint64_t K = q.K[j];
+    __shared__ double s[ADV_THREADS / 32], s_all[2][8];
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
+    const uint32_t j = blockIdx.x / parts;
+    const uint64_t K = q.K[j], step = (uint64_t)parts * ADV_THREADS, k0 = (uint64_t)part * ADV_THREADS + threadIdx.x;
     const uint4 *out = q.out[j];
+    pdl_go();
+    pdl_wait();
     // taken from the first one's: equal rewards leave exactly nothing, which a division by their deviation would blow up
     const double base = reward_of(__ldg(out), q.pair_cost, q.bank_cost);
+    double keep[ADV_KEEP];
+#pragma unroll
+    for (uint32_t i = 0; i < ADV_KEEP; ++i)
+        keep[i] = k0 + i * step < K ? reward_of(__ldg(out + k0 + i * step), q.pair_cost, q.bank_cost) - base : 0.0;
+    auto each = [&](auto &&f) {
+#pragma unroll
+        for (uint32_t i = 0; i < ADV_KEEP; ++i)
+            if (k0 + i * step < K) f(k0 + i * step, keep[i]);
+        for (uint64_t k = k0 + ADV_KEEP * step; k < K; k += step) f(k, reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base);
+    };
+    auto total = [&](double v, uint32_t at) {  // over the cluster, in the blocks' order
+        v = block_sum(v, s);
+        if (parts == 1) return v;
+        if (threadIdx.x < parts) *cluster.map_shared_rank(&s_all[at][part], threadIdx.x) = v;
+        cluster.sync();
+        v = 0.0;
+        for (uint32_t b = 0; b < parts; ++b) v += s_all[at][b];
+        return v;
+    };
+    if (parts > 1) cluster.sync();  // (all of them run)
     double sum = 0.0;
-    for (uint64_t k = threadIdx.x; k < K; k += PL_THREADS) sum += reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base;
-    const double mean = block_sum(sum, s) / (double)K;
+    each([&](uint64_t, double c) { sum += c; });
+    const double mean = total(sum, 0) / (double)K;
     double by = 1.0;
     if (q.normalise) {
         double var = 0.0;
-        for (uint64_t k = threadIdx.x; k < K; k += PL_THREADS) {
-            const double c = reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base - mean;
-            var += c * c;
-        }
-        by = 1.0 / (sqrt(block_sum(var, s) / (double)K) + q.eps);
+        each([&](uint64_t, double c) { var += (c - mean) * (c - mean); });
+        by = 1.0 / (sqrt(total(var, 1) / (double)K) + q.eps);
     }
-    for (uint64_t k = threadIdx.x; k < K; k += PL_THREADS) {
-        const double a = (reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base - mean) * by;
-        q.adv[q.first[j] + k] = a;
-        if (q.advantage) q.advantage[q.first[j] + k] = (float)a;
-    }
+    const double per_token = 1.0 / (double)max(inside(q.off[q.N], q.T) - inside(q.off[0], q.T), (int64_t)1);
+    each([&](uint64_t k, double c) {
+        const double a = (c - mean) * by;
+        const uint64_t at = q.first[j] + k;
+        const double w = q.per_token ? per_token : 1.0 / ((double)q.N * (double)max(q.off[at + 1] - q.off[at], (int64_t)1));
+        q.weights[at] = make_double2(w, w * a);
+        if (q.advantage) q.advantage[at] = (float)a;
+    });
 }
 
 struct TokenParams {
-    const double *adv;
+    const double2 *weights;
     const int64_t *off;
-    uint64_t N, T;
+    uint64_t N, T, per_warp;  // per_warp: tokens of a warp, a multiple of PL_STEP
     const float *lp, *old, *ref;
-    double log_lo, log_hi, at_lo, at_hi, kl;
-    int per_token;
+    float hi, hi_rest, lo, lo_rest;  // the clip's borders as logarithms, in two parts
+    double at_lo, at_hi, kl;
+    int vectors;                     // every array on 16 bytes
     float *g;
     double *part;
 };
 
-__global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams q)
+// First of off[0 .. n) that is above t (n if none).  Every lane of the warp calls it with the same t: 31 places at a time.
+__device__ __forceinline__ uint64_t first_above(const int64_t *off, uint64_t n, int64_t t, uint32_t lane)
 {
-    __shared__ double s[PL_THREADS / 32];
-    const double inf = __longlong_as_double(0x7ff0000000000000ll);
-    const int64_t span = min(max(q.off[q.N], (int64_t)0), (int64_t)q.T) - min(max(q.off[0], (int64_t)0), (int64_t)q.T);
-    double loss = 0.0;
-    for (uint32_t j = 0; j < PL_TILE / PL_THREADS; ++j) {
-        const uint64_t t = (uint64_t)blockIdx.x * PL_TILE + j * PL_THREADS + threadIdx.x;
-        if (t >= q.T) break;
-        uint64_t a = 0, b = q.N + 1;  // the first offset above t
-        while (a < b) {
-            const uint64_t mid = (a + b) >> 1;
-            if (q.off[mid] <= (int64_t)t) a = mid + 1; else b = mid;
-        }
-        float grad = 0.0f;
-        if (a > 0 && a <= q.N) {
-            const uint64_t k = a - 1;
-            const double A = q.adv[k], lp = q.lp[t], old = q.old ? (double)q.old[t] : lp, ref = q.kl != 0.0 ? (double)q.ref[t] : lp;
-            if (lp != -inf && old != -inf && ref != -inf) {
-                const double w = 1.0 / (q.per_token ? (double)max(span, (int64_t)1)
-                                                    : (double)q.N * (double)max(q.off[k + 1] - q.off[k], (int64_t)1));
-                const double d = lp - old;
-                const double Am = A * (double)expm1f((float)d);
-                const bool outside = A > 0.0 ? d > q.log_hi : d < q.log_lo;
-                double term = outside ? -A * (A > 0.0 ? q.at_hi : q.at_lo) : -(A + Am);
-                double slope = outside ? 0.0 : -(A + Am);
-                if (q.kl != 0.0) {
-                    const double e = ref - lp, em = (double)expm1f((float)e);
-                    term += q.kl * (em - e);
-                    slope -= q.kl * em;
-                }
-                loss += w * term;
-                grad = (float)(w * slope);
-            }
-        }
-        if (q.g) q.g[t] = grad;
+    uint64_t a = 0, b = n;  // off[a - 1] <= t < off[b]
+    while (a < b) {
+        const uint64_t step = (b - a + 31) / 32;  // places a + step - 1, a + 2 step - 1, ... below b
+        const uint64_t at = a + (lane + 1) * step - 1;
+        const uint32_t above = __ballot_sync(0xffffffffu, at >= b || off[at] > t);
+        const uint32_t f = above ? __ffs(above) - 1 : 32;
+        const uint64_t from = a + f * step;
+        b = min(b, from + step - 1);
+        a = min(from, b);
     }
-    loss = block_sum(loss, s);
-    if (threadIdx.x == 0) q.part[blockIdx.x] = loss;
+    return a;
 }
 
-__global__ void __launch_bounds__(PL_THREADS) k_policy_sum(const double *part, uint64_t n, float *loss)
+// rho - 1 in 32 bits.
+struct Token {
+    float lp, old, ref;
+};
+// A token's derivative per weight and, per weight, what it adds to the loss: wA (count_in + in) and so on, summed by the caller.
+struct Part {
+    float in;         // sum of rho - 1 of the tokens that are not clipped
+    float kl;         // sum of exp q - q - 1
+    int n_in, n_hi, n_lo;
+};
+__device__ __forceinline__ float token(const TokenParams &q, const Token &x, bool up, float wA, float wk, Part &p)
 {
-    __shared__ double s[PL_THREADS / 32];
+    const float minus_inf = __int_as_float(0xFF800000);
+    if (x.lp == minus_inf || x.old == minus_inf || x.ref == minus_inf) return 0.0f;
+    const float d = __fsub_rn(x.lp, x.old);
+    // what d lost to rounding (exact: the difference's error is a 32-bit number)
+    const float back = __fsub_rn(d, x.lp), lost = __fsub_rn(__fsub_rn(x.lp, __fsub_rn(d, back)), __fadd_rn(x.old, back));
+    const bool above = d > q.hi || (d == q.hi && lost > q.hi_rest), below = d < q.lo || (d == q.lo && lost < q.lo_rest);
+    float g = 0.0f;
+    if (up ? above : below) {
+        p.n_hi += up;
+        p.n_lo += !up;
+    } else {
+        const float m = expm1f(d);
+        p.in += m;
+        ++p.n_in;
+        g = -fmaf(wA, m, wA);
+    }
+    if (q.kl != 0.0) {
+        const float e = __fsub_rn(x.ref, x.lp), m = expm1f(e);
+        p.kl += m - e;
+        g = fmaf(-wk, m, g);
+    }
+    return g;
+}
+
+__global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams q)
+{
+    __shared__ double s[PL_WARPS];
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint64_t begin = ((uint64_t)blockIdx.x * PL_WARPS + warp) * q.per_warp, end = min(begin + q.per_warp, q.T);
+    const bool has_ref = q.kl != 0.0;
+    pdl_go();
+    double loss = 0.0;
+    uint64_t k0 = 0;  // the first offset above the warp's first token belongs to candidate k0 - 1
+    if (begin < end) k0 = first_above(q.off, q.N + 1, (int64_t)begin, lane);
+    pdl_wait();
+    for (uint64_t t0 = begin; t0 < end; t0 += PL_STEP) {
+        const uint64_t t = t0 + lane * 4;
+        Token x[4];
+        if (q.vectors && t + 4 <= end) {
+            const float4 a = __ldcs(reinterpret_cast<const float4 *>(q.lp + t));
+            const float4 b = q.old ? __ldcs(reinterpret_cast<const float4 *>(q.old + t)) : a;
+            const float4 c = has_ref ? __ldcs(reinterpret_cast<const float4 *>(q.ref + t)) : a;
+            x[0] = {a.x, b.x, c.x}; x[1] = {a.y, b.y, c.y}; x[2] = {a.z, b.z, c.z}; x[3] = {a.w, b.w, c.w};
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[j] = {0.0f, 0.0f, 0.0f};
+                if (t + j < end) {
+                    x[j].lp = q.lp[t + j];
+                    x[j].old = q.old ? q.old[t + j] : x[j].lp;
+                    x[j].ref = has_ref ? q.ref[t + j] : x[j].lp;
+                }
+            }
+        }
+        // the next 32 offsets, from the warp's first token on
+        const int64_t mine = k0 + lane <= q.N ? q.off[k0 + lane] - (int64_t)t0 : (int64_t)PL_STEP;
+        const int near = (int)min(max(mine, (int64_t)0), (int64_t)PL_STEP);
+        const bool many = __shfl_sync(0xffffffffu, near, 31) < (int)PL_STEP;  // candidates end faster than 32 in 128 tokens
+        // offsets at or below the lane's first token: the candidate's number
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t d = 16; d; d /= 2)
+            if (__shfl_sync(0xffffffffu, near, n + d - 1) <= (int)(lane * 4)) n += d;
+        int next = __shfl_sync(0xffffffffu, near, n);
+        float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        uint64_t k = k0 + n;  // first offset above the token
+        if (!many && next >= (int)(lane * 4 + 4)) {  // the four belong to one candidate
+            if (k > 0 && k <= q.N && t < end) {
+                const double2 w = q.weights[k - 1];
+                const float wA = (float)w.y, wk = (float)(q.kl * w.x);
+                Part p{0.0f, 0.0f, 0, 0, 0};
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (t + j < end) g[j] = token(q, x[j], w.y > 0.0, wA, wk, p);
+                loss += q.kl * w.x * (double)p.kl - w.y * ((double)p.in + (double)p.n_in + p.n_hi * q.at_hi + p.n_lo * q.at_lo);
+            }
+        } else {
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j) {
+                if (t + j >= end) break;
+                uint64_t a = k0, b = q.N + 1;  // first offset above the token
+                while (a < b) {
+                    const uint64_t mid = (a + b) >> 1;
+                    if (q.off[mid] <= (int64_t)(t + j)) a = mid + 1; else b = mid;
+                }
+                if (a == 0 || a > q.N) continue;
+                const double2 w = q.weights[a - 1];
+                Part p{0.0f, 0.0f, 0, 0, 0};
+                const float v = token(q, j == 0 ? x[0] : j == 1 ? x[1] : j == 2 ? x[2] : x[3], w.y > 0.0, (float)w.y, (float)(q.kl * w.x), p);
+                if (j == 0) g[0] = v; else if (j == 1) g[1] = v; else if (j == 2) g[2] = v; else g[3] = v;
+                loss += q.kl * w.x * (double)p.kl - w.y * ((double)p.in + (double)p.n_in + p.n_hi * q.at_hi + p.n_lo * q.at_lo);
+            }
+        }
+        if (q.g) {
+            if (q.vectors && t + 4 <= end) {
+                __stcs(reinterpret_cast<float4 *>(q.g + t), make_float4(g[0], g[1], g[2], g[3]));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (t + j < end) q.g[t + j] = g[j];
+            }
+        }
+        // offsets at or below the next step's first token
+        if (many) {
+            uint64_t a = k0, b = q.N + 1;
+            while (a < b) {
+                const uint64_t mid = (a + b) >> 1;
+                if (q.off[mid] <= (int64_t)(t0 + PL_STEP)) a = mid + 1; else b = mid;
+            }
+            k0 = a;
+        } else {
+            k0 += __popc(__ballot_sync(0xffffffffu, mine <= (int64_t)PL_STEP && k0 + lane <= q.N));
+        }
+    }
+    // fixed order: lanes, warps, blocks
+#pragma unroll
+    for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
+    if (lane == 0) s[warp] = loss;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        loss = 0.0;
+        for (uint32_t w = 0; w < PL_WARPS; ++w) loss += s[w];
+        q.part[blockIdx.x] = loss;
+    }
+}
+
+__global__ void __launch_bounds__(PL_THREADS) k_policy_sum(const double *part, uint32_t n, float *loss)
+{
+    __shared__ double s[PL_WARPS];
+    pdl_wait();
     double v = 0.0;
-    for (uint64_t i = threadIdx.x; i < n; i += PL_THREADS) v += part[i];
+    for (uint32_t i = threadIdx.x; i < n; i += PL_THREADS) v += part[i];
     v = block_sum(v, s);
     if (threadIdx.x == 0) *loss = (float)v;
 }
 
-uint64_t policy_tiles(uint64_t n_tokens) { return (n_tokens + PL_TILE - 1) / PL_TILE; }
+cudaError_t launch_advantages(const GroupParams &q, uint32_t groups, uint32_t parts, cudaStream_t st)
+{
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = parts;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(groups * parts); cfg.blockDim = ADV_THREADS; cfg.stream = st;
+    cfg.attrs = &at; cfg.numAttrs = 1;
+    g_vl_launches.fetch_add(1);
+    return cudaLaunchKernelEx(&cfg, k_advantages, q);
+}
 
 }  // namespace
 
 extern "C" uint64_t vl_policy_work(uint64_t n_candidates, uint64_t n_tokens)
 {
-    return 8 * (n_candidates + policy_tiles(n_tokens) + 1);
+    const uint64_t blocks = (n_tokens + PL_STEP * PL_WARPS - 1) / (PL_STEP * PL_WARPS);
+    return 16 * n_candidates + 8 * (blocks < PL_MAX_BLOCKS ? blocks : PL_MAX_BLOCKS) + 16;
 }
 
 extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d_out, const uint64_t *K, const int64_t *d_token_off,
@@ -146,7 +310,7 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
                               uint64_t work_bytes, void *stream)
 {
     if (!rules || !d_loss || !d_token_off || (n && (!d_out || !K)) || (n_tokens && !d_logprob)) return VL_ERR_INVALID_ARG;
-    if (((uintptr_t)d_token_off & 7) || ((uintptr_t)d_work & 7)) return VL_ERR_INVALID_ARG;
+    if (((uintptr_t)d_token_off & 7) || ((uintptr_t)d_work & 15)) return VL_ERR_INVALID_ARG;
     if (((uintptr_t)d_logprob | (uintptr_t)d_old_logprob | (uintptr_t)d_ref_logprob | (uintptr_t)d_loss | (uintptr_t)d_advantage |
          (uintptr_t)d_g_logprob) & 3)
         return VL_ERR_INVALID_ARG;
@@ -163,39 +327,49 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
     cudaStream_t st = (cudaStream_t)stream;
-    double *adv = static_cast<double *>(d_work), *part = adv + N;
     GroupParams q;
     q.pair_cost = rules->pair_cost; q.bank_cost = rules->bank_cost; q.eps = rules->eps; q.normalise = rules->normalise;
-    q.adv = adv; q.advantage = d_advantage;
+    q.off = d_token_off; q.N = N; q.T = n_tokens;
+    q.weights = static_cast<double2 *>(d_work); q.advantage = d_advantage; q.per_token = rules->per_token;
+    double *const part = reinterpret_cast<double *>(q.weights + N);
     uint64_t first = 0;
     for (uint32_t j = 0; j < n;) {
         uint32_t m = 0;
+        uint64_t most = 0;
         for (; j < n && m < PL_GROUPS; ++j) {
             if (!K[j]) continue;
             q.out[m] = reinterpret_cast<const uint4 *>(d_out[j]);
             q.K[m] = K[j];
             q.first[m++] = first;
             first += K[j];
+            most = K[j] > most ? K[j] : most;
         }
         if (!m) break;
-        k_advantages<<<m, PL_THREADS, 0, st>>>(q);
-        g_vl_launches.fetch_add(1);
+        // (no overlap with a launch in front that it does not know)
+        if (launch_advantages(q, m, most > ADV_THREADS * 2 ? 8 : 1, st) != cudaSuccess) return VL_ERR_CUDA;
     }
     TokenParams t;
-    t.adv = adv; t.off = d_token_off; t.N = N; t.T = n_tokens;
+    t.weights = q.weights; t.off = d_token_off; t.N = N; t.T = n_tokens;
     t.lp = d_logprob; t.old = d_old_logprob; t.ref = d_ref_logprob;
     t.at_lo = rules->clip_lo < 1.0 ? 1.0 - rules->clip_lo : 0.0;
     t.at_hi = 1.0 + rules->clip_hi;
-    t.log_lo = rules->clip_lo < 1.0 ? log1p(-rules->clip_lo) : -HUGE_VAL;
-    t.log_hi = log1p(rules->clip_hi);
-    t.kl = rules->kl; t.per_token = rules->per_token;
+    const double lo = rules->clip_lo < 1.0 ? log1p(-rules->clip_lo) : -HUGE_VAL, hi = log1p(rules->clip_hi);
+    t.lo = (float)lo; t.lo_rest = isfinite(lo) ? (float)(lo - t.lo) : 0.0f;
+    t.hi = (float)hi; t.hi_rest = isfinite(hi) ? (float)(hi - t.hi) : 0.0f;
+    if (!isfinite(t.at_hi)) t.at_hi = 0.0;  // (never taken)
+    t.kl = rules->kl;
     t.g = d_g_logprob; t.part = part;
-    const uint64_t tiles = policy_tiles(n_tokens);
-    if (tiles) {
-        k_policy_tokens<<<(uint32_t)tiles, PL_THREADS, 0, st>>>(t);
-        g_vl_launches.fetch_add(1);
+    t.vectors = !(((uintptr_t)d_logprob | (uintptr_t)d_old_logprob | (uintptr_t)(rules->kl != 0.0 ? d_ref_logprob : nullptr) | (uintptr_t)d_g_logprob) & 15);
+    const uint64_t steps = (n_tokens + PL_STEP - 1) / PL_STEP;
+    uint64_t blocks = (steps + PL_WARPS - 1) / PL_WARPS;
+    const uint64_t resident = 8 * (uint64_t)vl_device_sm_count(device);
+    const uint64_t at_most = resident < PL_MAX_BLOCKS ? resident : PL_MAX_BLOCKS;
+    if (blocks > at_most) blocks = at_most;
+    if (blocks) {
+        t.per_warp = (steps + blocks * PL_WARPS - 1) / (blocks * PL_WARPS) * PL_STEP;
+        if (launch_overlap(k_policy_tokens, dim3((uint32_t)blocks), PL_THREADS, 0, st, N != 0, t) != cudaSuccess) return VL_ERR_CUDA;
     }
-    k_policy_sum<<<1, PL_THREADS, 0, st>>>(part, tiles, d_loss);
-    g_vl_launches.fetch_add(1);
-    return cudaGetLastError() == cudaSuccess ? VL_OK : VL_ERR_CUDA;
+    if (launch_overlap(k_policy_sum, dim3(1), PL_THREADS, 0, st, blocks != 0, (const double *)part, (uint32_t)blocks, d_loss) != cudaSuccess)
+        return VL_ERR_CUDA;
+    return VL_OK;
 }
