@@ -54,15 +54,15 @@ __device__ __forceinline__ double block_sum(double v, double *s)
 
 __device__ __forceinline__ int64_t inside(int64_t t, uint64_t T) { return min(max(t, (int64_t)0), (int64_t)T); }
 
-// A cluster of blocks per program.  A thread's first rewards stay in registers.
-constexpr uint32_t ADV_THREADS = 512, ADV_KEEP = 4;
+// A block or a cluster of eight per program.  A thread's first rewards stay in registers.
+constexpr uint32_t ADV_THREADS = 1024, ADV_KEEP = 8;
 __global__ void __launch_bounds__(ADV_THREADS) k_advantages(const __grid_constant__ GroupParams q)
 {
     __shared__ double s[ADV_THREADS / 32], s_all[2][8];
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
     const uint32_t j = blockIdx.x / parts;
-    const uint64_t K = q.K[j], step = (uint64_t)parts * ADV_THREADS, k0 = (uint64_t)part * ADV_THREADS + threadIdx.x;
+    const uint64_t K = q.K[j], step = (uint64_t)parts * blockDim.x, k0 = (uint64_t)part * blockDim.x + threadIdx.x;
     const uint4 *out = q.out[j];
     pdl_go();
     pdl_wait();
@@ -135,130 +135,168 @@ __device__ __forceinline__ uint64_t first_above(const int64_t *off, uint64_t n, 
     return a;
 }
 
-// rho - 1 in 32 bits.
-struct Token {
-    float lp, old, ref;
-};
-// A token's derivative per weight and, per weight, what it adds to the loss: wA (count_in + in) and so on, summed by the caller.
-struct Part {
-    float in;         // sum of rho - 1 of the tokens that are not clipped
-    float kl;         // sum of exp q - q - 1
-    int n_in, n_hi, n_lo;
-};
-__device__ __forceinline__ float token(const TokenParams &q, const Token &x, bool up, float wA, float wk, Part &p)
+// exp d - 1 and exp d - 1 - d.  Near 0 from the exponential series (|d| < 0.35: its terms from the ninth on are below 2^-26 of the
+// first), elsewhere from the exponential itself, where nothing cancels: within 4 u exp d.
+__device__ __forceinline__ void exp_less(float d, float *m1, float *m2)
 {
-    const float minus_inf = __int_as_float(0xFF800000);
-    if (x.lp == minus_inf || x.old == minus_inf || x.ref == minus_inf) return 0.0f;
-    const float d = __fsub_rn(x.lp, x.old);
-    // what d lost to rounding (exact: the difference's error is a 32-bit number)
-    const float back = __fsub_rn(d, x.lp), lost = __fsub_rn(__fsub_rn(x.lp, __fsub_rn(d, back)), __fadd_rn(x.old, back));
-    const bool above = d > q.hi || (d == q.hi && lost > q.hi_rest), below = d < q.lo || (d == q.lo && lost < q.lo_rest);
-    float g = 0.0f;
-    if (up ? above : below) {
-        p.n_hi += up;
-        p.n_lo += !up;
-    } else {
-        const float m = expm1f(d);
-        p.in += m;
-        ++p.n_in;
-        g = -fmaf(wA, m, wA);
+    float p = 1.0f / 40320.0f;
+    p = fmaf(p, d, 1.0f / 5040.0f);
+    p = fmaf(p, d, 1.0f / 720.0f);
+    p = fmaf(p, d, 1.0f / 120.0f);
+    p = fmaf(p, d, 1.0f / 24.0f);
+    p = fmaf(p, d, 1.0f / 6.0f);
+    p = fmaf(p, d, 0.5f);
+    const float near2 = d * d * p, far1 = ex2(d * LOG2E) - 1.0f;
+    const bool near = fabsf(d) < 0.35f;
+    *m1 = near ? d + near2 : far1;
+    *m2 = near ? near2 : far1 - d;
+}
+
+// What tokens add to the loss of their candidate, of weight w and w times advantage wA: -wA (in + n_in + n_cut border) + kl w sum.
+struct Part {
+    float in, kl;  // sums of rho - 1 of the tokens that are not clipped, and of exp q - q - 1
+    int n_in, n_cut;
+};
+struct Weight {
+    double w, wA;
+    float wA32, wk32;  // and kl w
+    bool up;           // a positive advantage: clipped above
+};
+__device__ __forceinline__ Weight weight_of(const TokenParams &q, uint64_t k)  // of candidate k - 1, or of none
+{
+    const double2 w = k > 0 && k <= q.N ? q.weights[k - 1] : make_double2(0.0, 0.0);
+    return {w.x, w.y, (float)w.y, (float)(q.kl * w.x), w.y > 0.0};
+}
+template <bool REF>
+__device__ __forceinline__ float token(const TokenParams &q, float lp, float old, float ref, const Weight &w, bool owned, Part &p)
+{
+    const bool counts = owned && fminf(fminf(lp, old), ref) != __int_as_float(0xFF800000);
+    const float d = __fsub_rn(lp, old), border = w.up ? q.hi : q.lo;
+    bool cut = w.up ? d > border : d < border;
+    if (d == border) {  // what d lost to rounding decides (it is a 32-bit number, and so found exactly)
+        const float back = __fsub_rn(d, lp), lost = __fsub_rn(__fsub_rn(lp, __fsub_rn(d, back)), __fadd_rn(old, back));
+        cut = w.up ? lost > q.hi_rest : lost < q.lo_rest;
     }
-    if (q.kl != 0.0) {
-        const float e = __fsub_rn(x.ref, x.lp), m = expm1f(e);
-        p.kl += m - e;
-        g = fmaf(-wk, m, g);
+    float m, m2;
+    exp_less(d, &m, &m2);
+    const bool in = counts && !cut;
+    p.in += in ? m : 0.0f;
+    p.n_in += in;
+    p.n_cut += counts && cut;
+    float g = in ? -fmaf(w.wA32, m, w.wA32) : 0.0f;
+    if (REF) {
+        exp_less(__fsub_rn(ref, lp), &m, &m2);
+        p.kl += counts ? m2 : 0.0f;
+        g = counts ? fmaf(-w.wk32, m, g) : 0.0f;
     }
     return g;
 }
+template <bool REF>
+__device__ __forceinline__ double part_loss(const TokenParams &q, const Part &p, const Weight &w)
+{
+    const double in = (double)p.in + (double)p.n_in + (double)p.n_cut * (w.up ? q.at_hi : q.at_lo);
+    return REF ? fma(q.kl * w.w, (double)p.kl, -w.wA * in) : -w.wA * in;
+}
 
+template <bool REF>
 __global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams q)
 {
     __shared__ double s[PL_WARPS];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint64_t begin = ((uint64_t)blockIdx.x * PL_WARPS + warp) * q.per_warp, end = min(begin + q.per_warp, q.T);
-    const bool has_ref = q.kl != 0.0;
+    const uint64_t begin = ((uint64_t)blockIdx.x * PL_WARPS + warp) * q.per_warp;
+    const uint32_t len = begin < q.T ? (uint32_t)min(q.per_warp, q.T - begin) : 0;  // tokens of the warp; from here on counted from its first
+    const float *const lp = q.lp + begin, *const old = (q.old ? q.old : q.lp) + begin, *const ref = (REF ? q.ref : q.lp) + begin;
+    constexpr int FAR = 0x7FFFFFFF;
+    auto offset = [&](uint64_t k) -> int {
+        return k <= q.N ? (int)min(max(q.off[k] - (int64_t)begin, (int64_t)0), (int64_t)FAR) : FAR;
+    };
+    float4 nx, ny, nz;
+    auto fetch = [&](uint32_t t) {
+        if (q.vectors && t + 4 <= len) {
+            nx = __ldcs(reinterpret_cast<const float4 *>(lp + t));
+            ny = __ldcs(reinterpret_cast<const float4 *>(old + t));
+            if (REF) nz = __ldcs(reinterpret_cast<const float4 *>(ref + t));
+            else nz = nx;
+        } else {
+            auto one = [&](const float *a, uint32_t j) { return t + j < len ? a[t + j] : 0.0f; };
+            nx = make_float4(one(lp, 0), one(lp, 1), one(lp, 2), one(lp, 3));
+            ny = make_float4(one(old, 0), one(old, 1), one(old, 2), one(old, 3));
+            nz = make_float4(one(ref, 0), one(ref, 1), one(ref, 2), one(ref, 3));
+        }
+    };
     pdl_go();
     double loss = 0.0;
-    uint64_t k0 = 0;  // the first offset above the warp's first token belongs to candidate k0 - 1
-    if (begin < end) k0 = first_above(q.off, q.N + 1, (int64_t)begin, lane);
-    pdl_wait();
-    for (uint64_t t0 = begin; t0 < end; t0 += PL_STEP) {
-        const uint64_t t = t0 + lane * 4;
-        Token x[4];
-        if (q.vectors && t + 4 <= end) {
-            const float4 a = __ldcs(reinterpret_cast<const float4 *>(q.lp + t));
-            const float4 b = q.old ? __ldcs(reinterpret_cast<const float4 *>(q.old + t)) : a;
-            const float4 c = has_ref ? __ldcs(reinterpret_cast<const float4 *>(q.ref + t)) : a;
-            x[0] = {a.x, b.x, c.x}; x[1] = {a.y, b.y, c.y}; x[2] = {a.z, b.z, c.z}; x[3] = {a.w, b.w, c.w};
+    uint64_t k0 = 0;  // first offset above the step's first token
+    if (len) {
+        fetch(lane * 4);
+        k0 = first_above(q.off, q.N + 1, (int64_t)begin, lane);
+    }
+    pdl_wait();       // for the weights
+    int end0 = offset(k0);
+    Weight w0 = weight_of(q, k0);
+    bool owned0 = k0 > 0 && k0 <= q.N;
+    for (uint32_t t0 = 0; t0 < len; t0 += PL_STEP) {
+        const uint32_t t = t0 + lane * 4;
+        const float x[4] = {nx.x, nx.y, nx.z, nx.w}, y[4] = {ny.x, ny.y, ny.z, ny.w}, z[4] = {nz.x, nz.y, nz.z, nz.w};
+        if (t0 + PL_STEP < len) fetch(t + PL_STEP);
+        float g[4];
+        if (end0 >= (int)min(t0 + PL_STEP, len)) {  // one candidate's tokens, or nobody's
+            Part p{0.0f, 0.0f, 0, 0};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) g[j] = token<REF>(q, x[j], y[j], z[j], w0, owned0 && t + j < len, p);
+            loss += part_loss<REF>(q, p, w0);
         } else {
+            // the next 32 offsets; each lane walks to its tokens' from the last one at or below the first of them
+            const int near = offset(k0 + lane);
+            const bool many = __shfl_sync(0xffffffffu, near, 31) <= (int)(t0 + PL_STEP);  // they may end before the step does
+            uint32_t n = 0;
+#pragma unroll
+            for (uint32_t d = 16; d; d /= 2)
+                if (__shfl_sync(0xffffffffu, near, n + d - 1) <= (int)t) n += d;
+            uint64_t k = k0 + n;
+            Weight w = weight_of(q, k);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                x[j] = {0.0f, 0.0f, 0.0f};
-                if (t + j < end) {
-                    x[j].lp = q.lp[t + j];
-                    x[j].old = q.old ? q.old[t + j] : x[j].lp;
-                    x[j].ref = has_ref ? q.ref[t + j] : x[j].lp;
+                if (many) {
+                    uint64_t a = k0, b = q.N + 1;
+                    while (a < b) {
+                        const uint64_t mid = (a + b) >> 1;
+                        if (offset(mid) <= (int)(t + j)) a = mid + 1; else b = mid;
+                    }
+                    k = a;
+                    w = weight_of(q, k);
+                } else {
+                    for (;;) {
+                        const int next = __shfl_sync(0xffffffffu, near, n);
+                        const bool on = n < 31 && next <= (int)(t + j);
+                        if (!__any_sync(0xffffffffu, on)) break;
+                        n += on;
+                    }
+                    if (k != k0 + n) {
+                        k = k0 + n;
+                        w = weight_of(q, k);
+                    }
                 }
+                Part p{0.0f, 0.0f, 0, 0};
+                g[j] = token<REF>(q, x[j], y[j], z[j], w, k > 0 && k <= q.N && t + j < len, p);
+                loss += part_loss<REF>(q, p, w);
             }
-        }
-        // the next 32 offsets, from the warp's first token on
-        const int64_t mine = k0 + lane <= q.N ? q.off[k0 + lane] - (int64_t)t0 : (int64_t)PL_STEP;
-        const int near = (int)min(max(mine, (int64_t)0), (int64_t)PL_STEP);
-        const bool many = __shfl_sync(0xffffffffu, near, 31) < (int)PL_STEP;  // candidates end faster than 32 in 128 tokens
-        // offsets at or below the lane's first token: the candidate's number
-        uint32_t n = 0;
-#pragma unroll
-        for (uint32_t d = 16; d; d /= 2)
-            if (__shfl_sync(0xffffffffu, near, n + d - 1) <= (int)(lane * 4)) n += d;
-        int next = __shfl_sync(0xffffffffu, near, n);
-        float g[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        uint64_t k = k0 + n;  // first offset above the token
-        if (!many && next >= (int)(lane * 4 + 4)) {  // the four belong to one candidate
-            if (k > 0 && k <= q.N && t < end) {
-                const double2 w = q.weights[k - 1];
-                const float wA = (float)w.y, wk = (float)(q.kl * w.x);
-                Part p{0.0f, 0.0f, 0, 0, 0};
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (t + j < end) g[j] = token(q, x[j], w.y > 0.0, wA, wk, p);
-                loss += q.kl * w.x * (double)p.kl - w.y * ((double)p.in + (double)p.n_in + p.n_hi * q.at_hi + p.n_lo * q.at_lo);
-            }
-        } else {
-#pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
-                if (t + j >= end) break;
-                uint64_t a = k0, b = q.N + 1;  // first offset above the token
-                while (a < b) {
-                    const uint64_t mid = (a + b) >> 1;
-                    if (q.off[mid] <= (int64_t)(t + j)) a = mid + 1; else b = mid;
-                }
-                if (a == 0 || a > q.N) continue;
-                const double2 w = q.weights[a - 1];
-                Part p{0.0f, 0.0f, 0, 0, 0};
-                const float v = token(q, j == 0 ? x[0] : j == 1 ? x[1] : j == 2 ? x[2] : x[3], w.y > 0.0, (float)w.y, (float)(q.kl * w.x), p);
-                if (j == 0) g[0] = v; else if (j == 1) g[1] = v; else if (j == 2) g[2] = v; else g[3] = v;
-                loss += q.kl * w.x * (double)p.kl - w.y * ((double)p.in + (double)p.n_in + p.n_hi * q.at_hi + p.n_lo * q.at_lo);
-            }
+            // first offset above the next step's first token
+            if (many) k0 = first_above(q.off, q.N + 1, (int64_t)(begin + t0 + PL_STEP), lane);
+            else k0 += __popc(__ballot_sync(0xffffffffu, near <= (int)(t0 + PL_STEP)));
+            end0 = offset(k0);
+            w0 = weight_of(q, k0);
+            owned0 = k0 > 0 && k0 <= q.N;
         }
         if (q.g) {
-            if (q.vectors && t + 4 <= end) {
-                __stcs(reinterpret_cast<float4 *>(q.g + t), make_float4(g[0], g[1], g[2], g[3]));
+            float *const to = q.g + begin + t;
+            if (q.vectors && t + 4 <= len) {
+                __stcs(reinterpret_cast<float4 *>(to), make_float4(g[0], g[1], g[2], g[3]));
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (t + j < end) q.g[t + j] = g[j];
+                    if (t + j < len) to[j] = g[j];
             }
-        }
-        // offsets at or below the next step's first token
-        if (many) {
-            uint64_t a = k0, b = q.N + 1;
-            while (a < b) {
-                const uint64_t mid = (a + b) >> 1;
-                if (q.off[mid] <= (int64_t)(t0 + PL_STEP)) a = mid + 1; else b = mid;
-            }
-            k0 = a;
-        } else {
-            k0 += __popc(__ballot_sync(0xffffffffu, mine <= (int64_t)PL_STEP && k0 + lane <= q.N));
         }
     }
     // fixed order: lanes, warps, blocks
@@ -283,14 +321,16 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_sum(const double *part, u
     if (threadIdx.x == 0) *loss = (float)v;
 }
 
-cudaError_t launch_advantages(const GroupParams &q, uint32_t groups, uint32_t parts, cudaStream_t st)
+cudaError_t launch_advantages(const GroupParams &q, uint32_t groups, uint64_t most, cudaStream_t st)
 {
+    const uint32_t parts = most > 2 * ADV_THREADS ? 8 : 1;  // most: candidates of the largest program
+    const uint64_t threads = (most / parts + 31) / 32 * 32;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = parts;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(groups * parts); cfg.blockDim = ADV_THREADS; cfg.stream = st;
+    cfg.gridDim = dim3(groups * parts); cfg.blockDim = (uint32_t)(threads < 64 ? 64 : threads < ADV_THREADS ? threads : ADV_THREADS); cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = 1;
     g_vl_launches.fetch_add(1);
     return cudaLaunchKernelEx(&cfg, k_advantages, q);
@@ -346,7 +386,7 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
         }
         if (!m) break;
         // (no overlap with a launch in front that it does not know)
-        if (launch_advantages(q, m, most > ADV_THREADS * 2 ? 8 : 1, st) != cudaSuccess) return VL_ERR_CUDA;
+        if (launch_advantages(q, m, most, st) != cudaSuccess) return VL_ERR_CUDA;
     }
     TokenParams t;
     t.weights = q.weights; t.off = d_token_off; t.N = N; t.T = n_tokens;
@@ -367,7 +407,9 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
     if (blocks > at_most) blocks = at_most;
     if (blocks) {
         t.per_warp = (steps + blocks * PL_WARPS - 1) / (blocks * PL_WARPS) * PL_STEP;
-        if (launch_overlap(k_policy_tokens, dim3((uint32_t)blocks), PL_THREADS, 0, st, N != 0, t) != cudaSuccess) return VL_ERR_CUDA;
+        if (launch_overlap(t.kl != 0.0 ? k_policy_tokens<true> : k_policy_tokens<false>, dim3((uint32_t)blocks), PL_THREADS, 0, st, N != 0, t) !=
+            cudaSuccess)
+            return VL_ERR_CUDA;
     }
     if (launch_overlap(k_policy_sum, dim3(1), PL_THREADS, 0, st, blocks != 0, (const double *)part, (uint32_t)blocks, d_loss) != cudaSuccess)
         return VL_ERR_CUDA;
