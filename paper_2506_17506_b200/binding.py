@@ -11,6 +11,7 @@ import collections
 import contextlib
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -465,57 +466,83 @@ def vl_resample_stats(outs, ks=(1, 10, 100), device: int = 0, stream=None):
 
 
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy row_stats top_ids top_logprobs")
+_LOGITS = struct.Struct("@PiQIQPIPQPPf0P")     # vl_logits
+_RULES = struct.Struct("@6d2i")                # vl_policy_rules
 
 
-def _need(ok: bool, where: str, what: str):
-    if not ok:
-        raise VlError(VL_ERR_INVALID_ARG, f"{where}: {what}")
+class _Torch:
+    """What the functions below need of torch on every call, looked up once (torch is imported when it is first needed)."""
+    torch = None
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.logits = {torch.float32: (VL_F32, 4), torch.float16: (VL_F16, 2), torch.bfloat16: (VL_BF16, 2)}
+        cls.tokens = {torch.uint16: 2, torch.int16: 2, torch.int32: 4, torch.int64: 8}
+        cls.words = (torch.int32, torch.uint32)
+        cls.f32, cls.i32, cls.i64, cls.u8 = (torch.float32,), (torch.int32,), (torch.int64,), (torch.uint8,)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        cls.current = raw if raw else staticmethod(lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        cls.torch = torch
+        return torch
 
 
-def _on(stream, device):
-    """(the stream's pointer, a context in which torch's allocations belong to it); None: the device's current stream."""
-    import torch
-    if stream is None:
-        return C.c_void_p(torch.cuda.current_stream(device).cuda_stream), contextlib.nullcontext()
+def _refuse(where: str, what: str):
+    raise VlError(VL_ERR_INVALID_ARG, f"{where}: {what}")
+
+
+def _on(stream, dev: int):
+    """(the stream's pointer, a context in which torch's allocations belong to it) for a stream that was given."""
+    torch = _Torch.torch
     ptr = int(getattr(stream, "cuda_stream", stream))
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(ptr, device=device) if ptr else torch.cuda.default_stream(device)
-    return C.c_void_p(ptr), torch.cuda.stream(stream)
+        stream = torch.cuda.ExternalStream(ptr, device=dev) if ptr else torch.cuda.default_stream(dev)
+    return ptr, torch.cuda.stream(stream)
 
 
-def _vector(t, name, where, like, n, dtypes):
-    """Address of a contiguous vector of n entries on the device of `like`; None for None."""
+def _vector(t, name, where, dev, n, dtypes):
+    """Address of a contiguous vector of n entries on device `dev`; 0 for None."""
     if t is None:
-        return None
-    _need(t.device == like.device and t.dtype in dtypes and t.dim() == 1 and t.shape[0] == n and t.is_contiguous(), where,
-          f"{name}: a contiguous vector of {n} entries of {' or '.join(str(d)[6:] for d in dtypes)} on {like.device}")
-    return t.data_ptr() or None
+        return 0
+    if t.get_device() == dev and t.dtype in dtypes and t.dim() == 1 and t.shape[0] == n and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(where, f"{name}: a contiguous vector of {n} entries of {' or '.join(str(d)[6:] for d in dtypes)} on cuda:{dev}")
 
 
 def _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale):
-    import torch
-    types = {torch.float32: VL_F32, torch.float16: VL_F16, torch.bfloat16: VL_BF16}
-    _need(logits.is_cuda and logits.dtype in types and logits.dim() == 2, where, "logits: a CUDA matrix of float32, float16 or bfloat16")
+    """(vl_logits as bytes, rows, entries, device number)."""
+    torch = _Torch.torch or _Torch.load()
+    kind = _Torch.logits.get(logits.dtype)
+    if kind is None or not logits.is_cuda or logits.dim() != 2:
+        _refuse(where, "logits: a CUDA matrix of float32, float16 or bfloat16")
+    dev = logits.get_device()
     R, V = logits.shape
-    _need(1 <= V <= VL_MAX_VOCAB, where, f"logits: 1 to {VL_MAX_VOCAB} entries per row")
-    _need(V == 1 or logits.stride(1) == 1, where, "logits: entries of a row side by side")
-    _need(R <= 1 or logits.stride(0) >= V, where, "logits: rows that do not overlap")
-    x = vl_logits(logits=logits.data_ptr(), dtype=types[logits.dtype], n_rows=R, n_vocab=V, row_stride=logits.stride(0) if R > 1 else V,
-                  scale=scale)
-    x.tokens = _vector(tokens, "tokens", where, logits, R, (torch.uint16, torch.int16, torch.int32, torch.int64))
-    x.token_bytes = tokens.element_size() if tokens is not None else 0
-    x.mask_rows = _vector(mask_rows, "mask_rows", where, logits, R, (torch.int32,))
-    x.widths = _vector(widths, "widths", where, logits, R, (torch.uint8,))
+    apart, step = logits.stride()
+    if not 1 <= V <= VL_MAX_VOCAB:
+        _refuse(where, f"logits: 1 to {VL_MAX_VOCAB} entries per row")
+    if step != 1 and V != 1:
+        _refuse(where, "logits: entries of a row side by side")
+    if R <= 1:
+        apart = V
+    elif apart < V:
+        _refuse(where, "logits: rows that do not overlap")
+    t = _vector(tokens, "tokens", where, dev, R, _Torch.tokens)
+    words = n_masks = which = 0
     if occupied is not None:
         W = (V + 31) // 32
-        _need(occupied.device == logits.device and occupied.dtype in (torch.int32, torch.uint32) and occupied.dim() == 2 and
-              occupied.shape[1] == W and occupied.is_contiguous(), where,
-              f"occupied: a contiguous int32 matrix with {W} words per mask on {logits.device}")
-        _need(mask_rows is not None or occupied.shape[0] >= R, where, "occupied: a mask for every row, or mask_rows")
-        _need(occupied.shape[0] > 0 or R == 0, where, "occupied: at least one mask")
-        x.occupied, x.n_masks = occupied.data_ptr(), occupied.shape[0]
-    _need(occupied is not None or mask_rows is None, where, "mask_rows: the numbers of which masks?")
-    return x
+        if not (occupied.get_device() == dev and occupied.dtype in _Torch.words and occupied.dim() == 2 and occupied.shape[1] == W and
+                occupied.is_contiguous()):
+            _refuse(where, f"occupied: a contiguous int32 matrix with {W} words per mask on cuda:{dev}")
+        n_masks = occupied.shape[0]
+        if n_masks < (R if mask_rows is None else min(R, 1)):
+            _refuse(where, "occupied: a mask for every row, or mask_rows")
+        words = occupied.data_ptr()
+        which = _vector(mask_rows, "mask_rows", where, dev, R, _Torch.i32)
+    elif mask_rows is not None:
+        _refuse(where, "mask_rows: the numbers of which masks?")
+    w = _vector(widths, "widths", where, dev, R, _Torch.u8)
+    return _LOGITS.pack(logits.data_ptr(), kind[0], R, V, apart, t, _Torch.tokens[tokens.dtype] if t else 0, words, n_masks, which, w,
+                        scale), R, V, dev
 
 
 def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths=None, scale: float = 1.0, top: int = 0, stream=None):
@@ -523,62 +550,74 @@ def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths
     probability of the given token of every row (``tokens``: uint16, int32 or int64; a row whose token is no entry is
     left out), the entropy, what the backward call takes, and the ``top`` best entries with their log probabilities.
     ``occupied``: masks as ``vl_occupied_masks(..., words=True)`` gives them, mask ``mask_rows[r]`` for row r (or mask r);
-    ``widths``: registers of the tuple that row r places; ``scale``: 1 / temperature.  No wait.
+    ``widths``: registers of the tuple that row r places; ``scale``: 1 / temperature.  On ``stream`` (default: the current
+    one of the logits' device), without waiting.
     Returns TokenLogprobs(logprob, entropy, row_stats [rows, 2], top_ids, top_logprobs); what was not asked for is None."""
-    import torch
     where = "vl_token_logprobs"
-    x = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
-    _need(0 <= top <= VL_MAX_ALTERNATIVES, where, f"top: at most {VL_MAX_ALTERNATIVES} alternatives")
-    R, dev = logits.shape[0], logits.device
-    ptr, scope = _on(stream, dev)
-    with scope:
-        f = torch.empty(R * ((4 if tokens is not None else 3) + 2 * top), dtype=torch.float32, device=dev)   # one allocation
-    stats, rest = f[:2 * R].view(R, 2), f[2 * R:]
-    ent, rest = rest[:R], rest[R:]
-    lp = ids = lps = None
-    if tokens is not None:
-        lp, rest = rest[:R], rest[R:]
-    if top:
-        ids, lps = rest[:R * top].view(torch.int32).view(R, top), rest[R * top:].view(R, top)
-    rc = _lib.vl_token_logprobs(dev.index, C.byref(x), lp.data_ptr() if lp is not None else None, ent.data_ptr(), stats.data_ptr(), top,
-                                ids.data_ptr() if top else None, lps.data_ptr() if top else None, ptr)
+    x, R, _, dev = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
+    torch = _Torch.torch
+    if not 0 <= top <= VL_MAX_ALTERNATIVES:
+        _refuse(where, f"top: at most {VL_MAX_ALTERNATIVES} alternatives")
+    sizes = [2 * R, R, R] + [R * top, R * top] * (top > 0)      # one allocation
+    if stream is None:
+        ptr = _Torch.current(dev)
+        f = torch.empty(sum(sizes), dtype=torch.float32, device=logits.device)
+    else:
+        ptr, scope = _on(stream, dev)
+        with scope:
+            f = torch.empty(sum(sizes), dtype=torch.float32, device=logits.device)
+    at = f.data_ptr()
+    rc = _lib.vl_token_logprobs(dev, x, at + 12 * R if tokens is not None else 0, at + 8 * R, at, top, at + 16 * R if top else 0,
+                                at + (16 + 4 * top) * R if top else 0, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
-    return TokenLogprobs(lp, ent, stats, ids, lps)
+    out = f.split_with_sizes(sizes)
+    return TokenLogprobs(out[2] if tokens is not None else None, out[1], out[0].view(R, 2),
+                         out[3].view(torch.int32).view(R, top) if top else None, out[4].view(R, top) if top else None)
 
 
 def vl_token_logprobs_backward(logits, tokens, row_stats, g_logprob=None, entropy=None, g_entropy=None, occupied=None, mask_rows=None,
                                widths=None, scale: float = 1.0, out=None, stream=None):
     """Gradient to the logits of a loss whose derivatives to the log probabilities and entropies of ``vl_token_logprobs`` are
-    ``g_logprob`` and ``g_entropy`` (float32 [rows]; a single number in a tensor of stride 0 has to be made contiguous).
-    ``row_stats`` and ``entropy`` come from that call, the other arguments are the ones it had.  ``out``: where to (the logits
-    themselves, or a matrix of their shape and type that does not overlap them); a new matrix without it."""
-    import torch
+    ``g_logprob`` and ``g_entropy`` (contiguous float32 [rows]).  ``row_stats`` and ``entropy`` come from that call, the other
+    arguments are the ones it had.  ``out``: where to (the logits themselves, or a matrix of their shape and type that does not
+    overlap them); a new matrix without it."""
     where = "vl_token_logprobs_backward"
-    x = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
-    R, V = logits.shape
-    f32 = (torch.float32,)
-    _need(row_stats.device == logits.device and row_stats.dtype == torch.float32 and tuple(row_stats.shape) == (R, 2) and
-          row_stats.is_contiguous(), where, "row_stats: the contiguous float32 [rows, 2] of vl_token_logprobs")
-    g = _vector(g_logprob, "g_logprob", where, logits, R, f32)
-    h = _vector(g_entropy, "g_entropy", where, logits, R, f32)
-    ent = _vector(entropy, "entropy", where, logits, R, f32)
-    _need(g_logprob is None or tokens is not None, where, "g_logprob: the log probabilities of which tokens?")
-    _need(g_entropy is None or entropy is not None, where, "entropy: needed with g_entropy")
-    ptr, scope = _on(stream, logits.device)
+    x, R, V, dev = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
+    torch = _Torch.torch
+    if not (row_stats.get_device() == dev and row_stats.dtype == torch.float32 and row_stats.dim() == 2 and
+            tuple(row_stats.shape) == (R, 2) and row_stats.is_contiguous()):
+        _refuse(where, "row_stats: the contiguous float32 [rows, 2] of vl_token_logprobs")
+    g = _vector(g_logprob, "g_logprob", where, dev, R, _Torch.f32)
+    h = _vector(g_entropy, "g_entropy", where, dev, R, _Torch.f32)
+    ent = _vector(entropy, "entropy", where, dev, R, _Torch.f32)
+    if g_logprob is not None and tokens is None:
+        _refuse(where, "g_logprob: the log probabilities of which tokens?")
+    if g_entropy is not None and entropy is None:
+        _refuse(where, "entropy: needed with g_entropy")
+    scope = None
+    if stream is None:
+        ptr = _Torch.current(dev)
+    else:
+        ptr, scope = _on(stream, dev)
     if out is None:
-        with scope:
+        with scope or contextlib.nullcontext():
             out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
-    _need(out.device == logits.device and out.dtype == logits.dtype and out.shape == logits.shape and (V == 1 or out.stride(1) == 1) and
-          (R <= 1 or out.stride(0) >= V), where, "out: a matrix of the logits' shape and type, entries of a row side by side")
-    if out.data_ptr() == logits.data_ptr():
-        _need(R <= 1 or out.stride(0) == logits.stride(0), where, "out: the logits themselves have the logits' stride")
-    elif R:
-        size = logits.element_size()
-        ends = [t.data_ptr() + ((R - 1) * t.stride(0) + V) * size for t in (logits, out)]
-        _need(out.data_ptr() >= ends[0] or logits.data_ptr() >= ends[1], where, "out: overlaps the logits")
-    rc = _lib.vl_token_logprobs_backward(logits.device.index, C.byref(x), row_stats.data_ptr(), ent, g, h, out.data_ptr(),
-                                         out.stride(0) if R > 1 else V, ptr)
+        apart = V
+    else:
+        apart = out.stride(0) if out.dim() == 2 and R > 1 else V
+        if not (out.get_device() == dev and out.dtype == logits.dtype and out.shape == logits.shape and (V == 1 or out.stride(1) == 1) and
+                apart >= V):
+            _refuse(where, "out: a matrix of the logits' shape and type, entries of a row side by side")
+        if out.data_ptr() == logits.data_ptr():
+            if R > 1 and apart != logits.stride(0):
+                _refuse(where, "out: the logits themselves have the logits' stride")
+        elif R:
+            size = logits.element_size()
+            ends = [t.data_ptr() + ((R - 1) * (t.stride(0) if R > 1 else 0) + V) * size for t in (logits, out)]
+            if out.data_ptr() < ends[0] and logits.data_ptr() < ends[1]:
+                _refuse(where, "out: overlaps the logits")
+    rc = _lib.vl_token_logprobs_backward(dev, x, row_stats.data_ptr(), ent, g, h, out.data_ptr(), apart, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
     return out
@@ -591,33 +630,39 @@ def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None,
     them); ``token_off``: CUDA int64, candidate c (over all programs) owns the tokens token_off[c] .. token_off[c + 1] - 1 of
     ``logprob`` (float32), of ``old_logprob`` (under the model that sampled; None: the same) and ``ref_logprob`` (with ``kl``).
     Returns (loss, a float32 scalar tensor; advantages of the candidates; derivative of the loss to ``logprob``).  No wait."""
-    import torch
     where = "vl_policy_loss"
-    n = len(outs)
-    _need(logprob.is_cuda and logprob.dim() == 1, where, "logprob: a CUDA vector")
-    for o in outs:
-        _need(o.device == logprob.device and o.dtype == torch.int32 and o.dim() == 2 and o.shape[1] == 4 and o.is_contiguous(), where,
-              f"outs: contiguous int32 verdicts [samples, 4] on {logprob.device}")
-    N, T, dev = sum(o.shape[0] for o in outs), logprob.shape[0], logprob.device
-    f32 = (torch.float32,)
-    lp = _vector(logprob, "logprob", where, logprob, T, f32)
-    old = _vector(old_logprob, "old_logprob", where, logprob, T, f32)
-    ref = _vector(ref_logprob, "ref_logprob", where, logprob, T, f32)
-    off = _vector(token_off, "token_off", where, logprob, N + 1, (torch.int64,))
-    rules = vl_policy_rules(pair_cost, bank_cost, eps, clip_lo, clip_hi, kl, int(normalise), int(per_token))
-    op = (C.c_void_p * max(n, 1))(*[o.data_ptr() or None for o in outs])
-    Ks = (C.c_uint64 * max(n, 1))(*[o.shape[0] for o in outs])
-    size = int(_lib.vl_policy_work(N, T))
-    ptr, scope = _on(stream, dev)
-    with scope:
-        work = torch.empty(size, dtype=torch.uint8, device=dev)
-        f = torch.empty(1 + N + T, dtype=torch.float32, device=dev)
-    g, adv, loss = f[:T], f[T:T + N], f[T + N]        # (the derivative on 16 bytes)
-    rc = _lib.vl_policy_loss(dev.index, n, op, Ks, off, T, lp, old, ref, C.byref(rules), loss.data_ptr(), adv.data_ptr(), g.data_ptr(),
-                             work.data_ptr(), size, ptr)
+    torch = _Torch.torch or _Torch.load()
+    if not logprob.is_cuda or logprob.dim() != 1:
+        _refuse(where, "logprob: a CUDA vector")
+    dev, T, n = logprob.get_device(), logprob.shape[0], len(outs)
+    i32 = torch.int32
+    shapes = [o.shape for o in outs]
+    for o, s in zip(outs, shapes):
+        if not (o.get_device() == dev and o.dtype is i32 and len(s) == 2 and s[1] == 4 and o.is_contiguous()):
+            _refuse(where, f"outs: contiguous int32 verdicts [samples, 4] on cuda:{dev}")
+    sizes = [s[0] for s in shapes]
+    N = sum(sizes)
+    lp = _vector(logprob, "logprob", where, dev, T, _Torch.f32)
+    old = _vector(old_logprob, "old_logprob", where, dev, T, _Torch.f32)
+    ref = _vector(ref_logprob, "ref_logprob", where, dev, T, _Torch.f32)
+    off = _vector(token_off, "token_off", where, dev, N + 1, _Torch.i64)
+    work = (int(_lib.vl_policy_work(N, T)) + 15) // 16 * 16
+    size = work + 4 * (T + N + 1)                       # working memory, then the results: the derivative on 16 bytes
+    if stream is None:
+        ptr = _Torch.current(dev)
+        f = torch.empty(size // 4, dtype=torch.float32, device=logprob.device)
+    else:
+        ptr, scope = _on(stream, dev)
+        with scope:
+            f = torch.empty(size // 4, dtype=torch.float32, device=logprob.device)
+    at = f.data_ptr()
+    rc = _lib.vl_policy_loss(dev, n, struct.pack(f"{n}P", *[o.data_ptr() for o in outs]), struct.pack(f"{n}Q", *sizes), off, T, lp, old, ref,
+                             _RULES.pack(pair_cost, bank_cost, eps, clip_lo, clip_hi, kl, bool(normalise), bool(per_token)),
+                             at + work + 4 * (T + N), at + work + 4 * T, at + work, at, work, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
-    return loss, adv, g
+    _, g, adv, loss = f.split_with_sizes([work // 4, T, N, 1])
+    return loss[0], adv, g
 
 
 def verdicts_to_numpy(t) -> np.ndarray:

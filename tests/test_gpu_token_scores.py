@@ -467,7 +467,7 @@ def test_nothing_else_is_written(B):
         x = _rows(_make(rng, R, V), "f32")
         t = torch.from_numpy(rng.integers(0, V, R)).cuda()
         want = B.vl_token_logprobs(x, t, top=top)
-        d = B._logit_rows("test", x, t, None, None, None, 1.0)
+        d = B.vl_logits(x.data_ptr(), B.VL_F32, R, V, V, t.data_ptr(), 8, None, 0, None, None, 1.0)
         sizes = [R, R, 2 * R, R * top, R * top]
         bufs = [torch.full((n + 16,), 12345.0, device="cuda") for n in sizes]
         ptrs = [b.data_ptr() + 32 for b in bufs]
