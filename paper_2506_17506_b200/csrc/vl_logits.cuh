@@ -195,12 +195,16 @@ struct RowVectors {
     }
 };
 
-// Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of word g.
+// Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of the words g,
+// g + G, ...
 template <typename T, int G, int NV>
 __device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t g, bool aligned)
 {
     const uint4 *at = x.at(g);
-    if (aligned) {
+    if (aligned && x.n == G * NV) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) raw[j] = at[G * j];
+    } else if (aligned) {
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
@@ -220,16 +224,6 @@ __device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> 
         }
     }
 }
-// Closed entries of the lane's vector v, from the words that the group's lanes hold.  Every lane of the warp calls it.
-template <typename T, int G>
-__device__ __forceinline__ uint32_t group_closed(uint32_t word, int first, bool aligned)
-{
-    const int w = first >> 5, s = first & 31;
-    const uint32_t a = __shfl_sync(0xffffffffu, word, w & (G - 1), G);
-    const uint32_t b = aligned ? 0u : __shfl_sync(0xffffffffu, word, (w + 1) & (G - 1), G);
-    return __funnelshift_r(a, b, s) & ((1u << EPV<T>) - 1);
-}
-
 // Entries whose bit is set to minus infinity.  Halves: a byte permutation takes their bytes from the one or the other word; the selectors
 // of four entries are made at once, a bit spread to a byte of 0x44 (13 instructions a vector, 28 with a mask per pair).
 template <typename T>
@@ -363,6 +357,43 @@ __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
         if (j < q.n_masks) m.words = q.occupied + j * q.W;
     }
     return m;
+}
+
+// Sets the closed entries of a group's rows to minus infinity.  Each word of a mask is worked out by one lane and handed to those that
+// hold its entries.  Every lane of the warp calls it; the result says whether entry tok is closed (true for what is no entry).
+template <typename T, int G, int NV>
+__device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> &x, const RowMask &mask, uint32_t g, bool aligned, int64_t tok)
+{
+    constexpr int WL = NV * EPV<T> <= 32 ? 1 : NV * EPV<T> / 32;  // words of a lane
+    uint32_t word[WL];
+    if (aligned || WL == 1) {
+#pragma unroll
+        for (int k = 0; k < WL; ++k) word[k] = mask.closed(g + G * k);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        uint32_t bits;
+        if (aligned) {
+            const uint32_t first = (g + G * j) * EPV<T>;
+            bits = __shfl_sync(0xffffffffu, word[j * EPV<T> / 32], (first >> 5) & (G - 1), G) >> (first & 31);
+        } else if (WL == 1) {
+            const int first = x.first(g + G * j), w = first >> 5;
+            const uint32_t a = __shfl_sync(0xffffffffu, word[0], w & (G - 1), G), b = __shfl_sync(0xffffffffu, word[0], (w + 1) & (G - 1), G);
+            bits = __funnelshift_r(a, b, first & 31);
+        } else {
+            bits = g + G * j < x.n ? mask.closed_from(x.first(g + G * j), EPV<T>) : 0u;
+        }
+        close_entries<T>(raw[j], bits & ((1u << EPV<T>) - 1));
+    }
+    const uint32_t t = tok < 0 ? 0u : (uint32_t)tok;
+    if (!aligned && WL > 1) return tok < 0 || mask.is_closed(t);
+    uint32_t at = 0;
+#pragma unroll
+    for (int k = 0; k < WL; ++k) {
+        const uint32_t w = __shfl_sync(0xffffffffu, word[k], (t >> 5) & (G - 1), G);
+        if ((int)((t >> 5) / G) == k) at = w;
+    }
+    return (at >> (t & 31)) & 1;
 }
 
 }  // namespace

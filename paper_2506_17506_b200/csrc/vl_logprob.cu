@@ -655,7 +655,6 @@ __device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], flo
 template <typename T, bool MASKED, bool TOP, int G, int NV>
 __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRows q, const ScoreOut o, bool aligned)
 {
-    constexpr bool WORDS = NV * EPV<T> <= 32;  // a row has no more words of closed entries than its group has lanes
     static_assert(!TOP || G == 32, "alternatives take the whole warp");
     __shared__ key_t64 s_cand[TOP ? SHORT_WARPS : 1][TOP ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
@@ -669,20 +668,8 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
         uint4 raw[NV];
         fetch_row<T, G, NV>(raw, x, g, aligned);
         const int64_t tok = row_token(q, r);
-        uint32_t word = 0;
-        if (MASKED) {
-            const RowMask mask = row_mask(q, r);
-            if (WORDS) {
-                word = mask.closed(g);
-#pragma unroll
-                for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
-            } else {
-                word = tok >= 0 && mask.is_closed((uint32_t)tok);
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (g + G * j < x.n) close_entries<T>(raw[j], mask.closed_from(x.first(g + G * j), EPV<T>));
-            }
-        }
+        bool shut = false;
+        if (MASKED) shut = close_row<T, G, NV>(raw, x, row_mask(q, r), g, aligned, tok);
         float x_tok = 0.0f;
         if (g == 0 && o.logprob && tok >= 0) x_tok = to_f32(x.row[tok]);
 
@@ -705,9 +692,6 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
         float L, H;
         finish(Sums{m, s, t}, c, &L, &H);
         const bool left = tok < 0, empty = s == 0.0f;
-        bool shut = false;
-        if (MASKED && WORDS) shut = (__shfl_sync(0xffffffffu, word, left ? 0 : (int)((uint32_t)tok >> 5) & (G - 1), G) >> (tok & 31)) & 1;
-        else if (MASKED) shut = word;
         if (g == 0 && there) {
             if (o.logprob) o.logprob[r] = left ? 0.0f : (empty || shut ? -inf : (x_tok - m) * q.scale - L);
             if (o.entropy) o.entropy[r] = left || empty ? 0.0f : H;
@@ -750,9 +734,9 @@ bool launch_short(const LogitRows &q, const ScoreOut &o, cudaStream_t st, cudaEr
     } else {
         if (n <= 4) *e = run_short<T, MASKED, false, 4, 1>(q, o, aligned, st);
         else if (n <= 16) *e = run_short<T, MASKED, false, 4, 4>(q, o, aligned, st);
-        else if (n <= 32) *e = run_short<T, MASKED, false, 8, 4>(q, o, aligned, st);
-        else if (n <= 64) *e = run_short<T, MASKED, false, 16, 4>(q, o, aligned, st);
-        else if (n <= 128) *e = run_short<T, MASKED, false, 32, 4>(q, o, aligned, st);
+        else if (n <= 32) *e = run_short<T, MASKED, false, 4, 8>(q, o, aligned, st);
+        else if (n <= 64) *e = run_short<T, MASKED, false, 8, 8>(q, o, aligned, st);
+        else if (n <= 128) *e = run_short<T, MASKED, false, 16, 8>(q, o, aligned, st);
         else if (n <= 256) *e = run_short<T, MASKED, false, 32, 8>(q, o, aligned, st);
         else if (n <= 512) *e = run_short<T, MASKED, false, 32, 16>(q, o, aligned, st);
         else return false;

@@ -24,16 +24,15 @@ struct GradRow {
     bool far, dead;
     int tok;
 };
-__device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p, uint64_t r, const RowMask &mask, bool masked)
+__device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p, uint64_t r, int64_t tok, bool shut)  // shut: the token is closed
 {
     GradRow w;
-    const int64_t tok = row_token(q, r);
     const float2 st = *reinterpret_cast<const float2 *>(p.stats + 2 * r);
     float g = p.g ? p.g[r] : 0.0f;
     const float h = p.h ? p.h[r] : 0.0f, H = p.h ? p.entropy[r] : 0.0f;
     w.tok = (int)tok;
     w.dead = tok < 0 || st.y == __int_as_float(0xFF800000);
-    if (masked && p.g && !w.dead && mask.is_closed((uint32_t)tok)) g = 0.0f;
+    if (shut) g = 0.0f;
     w.c = q.scale * LOG2E;
     w.M = st.x;
     w.far = far_out(st.x);
@@ -113,7 +112,8 @@ __global__ void __launch_bounds__(GRAD_THREADS) k_grad_long(const LogitRows q, c
             if (v < x.n && x.whole(v)) raw[u] = __ldcs(x.at(v));
         }
         const RowMask mask = row_mask(q, r);
-        const GradRow w = grad_row(q, p, r, mask, MASKED);
+        const int64_t tok = row_token(q, r);
+        const GradRow w = grad_row(q, p, r, tok, MASKED && tok >= 0 && tok < (int64_t)q.V && mask.is_closed((uint32_t)tok));
 #pragma unroll
         for (int u = 0; u < GRAD_U; ++u) {
             const uint32_t v = v0 + u * GRAD_THREADS;
@@ -135,7 +135,6 @@ constexpr uint32_t SHORT_WARPS = 8;
 template <typename T, bool MASKED, int G, int NV>
 __global__ void __launch_bounds__(SHORT_WARPS * 32) k_grad_short(const LogitRows q, const GradIn p, bool aligned, bool out_aligned)
 {
-    constexpr bool WORDS = NV * EPV<T> <= 32;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
     const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
     for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
@@ -145,18 +144,10 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_grad_short(const LogitRows
         uint4 raw[NV];
         if (there) fetch_row<T, G, NV>(raw, x, g, aligned);
         const RowMask mask = row_mask(q, r);
-        const GradRow w = grad_row(q, p, r, mask, MASKED);
-        if (MASKED) {
-            if (WORDS) {
-                const uint32_t word = mask.closed(g);
-#pragma unroll
-                for (int j = 0; j < NV; ++j) close_entries<T>(raw[j], group_closed<T, G>(word, x.first(g + G * j), aligned));
-            } else {
-#pragma unroll
-                for (int j = 0; j < NV; ++j)
-                    if (g + G * j < x.n) close_entries<T>(raw[j], mask.closed_from(x.first(g + G * j), EPV<T>));
-            }
-        }
+        const int64_t tok = row_token(q, r);
+        bool shut = false;
+        if (MASKED) shut = close_row<T, G, NV>(raw, x, mask, g, aligned, tok);
+        const GradRow w = grad_row(q, p, r, tok, shut);
         if (!there) continue;
         T *const dx = static_cast<T *>(p.dx) + r * p.stride;
         uint4 *const to = reinterpret_cast<uint4 *>(dx) + g;  // (aligned ones only)
@@ -186,9 +177,9 @@ cudaError_t launch(const LogitRows &q, const GradIn &p, cudaStream_t st)
     const uint32_t n = row_vectors(q, sizeof(T), &aligned);
     if (n <= 4) run_short<T, MASKED, 4, 1>(q, p, aligned, st);
     else if (n <= 16) run_short<T, MASKED, 4, 4>(q, p, aligned, st);
-    else if (n <= 32) run_short<T, MASKED, 8, 4>(q, p, aligned, st);
-    else if (n <= 64) run_short<T, MASKED, 16, 4>(q, p, aligned, st);
-    else if (n <= 128) run_short<T, MASKED, 32, 4>(q, p, aligned, st);
+    else if (n <= 32) run_short<T, MASKED, 4, 8>(q, p, aligned, st);
+    else if (n <= 64) run_short<T, MASKED, 8, 8>(q, p, aligned, st);
+    else if (n <= 128) run_short<T, MASKED, 16, 8>(q, p, aligned, st);
     else if (n <= 256) run_short<T, MASKED, 32, 8>(q, p, aligned, st);
     else {
         const uint32_t y = (uint32_t)(q.n_rows < 65535 ? q.n_rows : 65535);
