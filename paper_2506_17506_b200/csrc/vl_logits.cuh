@@ -3,6 +3,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "vl_internal.cuh"
 
 // A checked vl_logits in the form the kernels take.
@@ -13,7 +15,7 @@ struct LogitRows {
     uint32_t token_bytes;
     const void *tokens;
     const uint32_t *occupied;
-    uint64_t n_masks;
+    uint32_t n_masks;            // that mask_rows can name: at most 2^31
     const int32_t *mask_rows;
     const uint8_t *widths;
     float scale;
@@ -195,37 +197,14 @@ struct RowVectors {
     }
 };
 
+// Blocks of 256 threads of a multiprocessor for short rows, by the vectors of a lane: what hides the loads are warps (200,000 rows of 256 bf16
+// logits in us for 2, 3, 4, 5, 6 blocks of 122, 77, 64, 48, 40 registers a thread: 27.5, 21.8, 19.3, 24.5, 32).
+constexpr int short_blocks(int NV) { return NV <= 8 ? 4 : 2; }
+
 // Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of the words g,
 // g + G, ...
-template <typename T, int G, int NV>
-__device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t g, bool aligned)
-{
-    const uint4 *at = x.at(g);
-    if (aligned && x.n == G * NV) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) raw[j] = at[G * j];
-    } else if (aligned) {
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
-            if (g + G * j < x.n) raw[j] = at[G * j];
-        }
-    } else {
-// the vectors that are no whole ones: the first and the last
-        uint4 end = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>), begin = end;
-        if (g == 0 && x.lead && x.n > 1) begin = x.part(0);
-        if (g == (x.n - 1) % G && !x.whole(x.n - 1)) end = x.part(x.n - 1);
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const uint32_t v = g + G * j;
-            raw[j] = v == x.n - 1 ? end : begin;
-            if (x.whole(v)) raw[j] = at[G * j];
-            else if (v >= x.n) raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
-        }
-    }
-}
 // Entries whose bit is set to minus infinity.  Halves: a byte permutation takes their bytes from the one or the other word; the selectors
-// of four entries are made at once, a bit spread to a byte of 0x44 (13 instructions a vector, 28 with a mask per pair).
+// of four entries are made at once, a bit spread to a byte of 0x44 (14 instructions a vector, 28 with a mask per pair).
 template <typename T>
 __device__ __forceinline__ void close_entries(uint4 &r, uint32_t bits)
 {
@@ -241,6 +220,40 @@ __device__ __forceinline__ void close_entries(uint4 &r, uint32_t bits)
         r.y = __byte_perm(r.y, MINUS_INF2<T>, a >> 16);
         r.z = __byte_perm(r.z, MINUS_INF2<T>, b);
         r.w = __byte_perm(r.w, MINUS_INF2<T>, b >> 16);
+    }
+}
+
+// ALIGNED: rows start and end on vectors.  Else, with `around`, the vectors that reach into the rows in front and behind are read whole; without
+// it (what lies there is not the matrix, or another thread's to write) their entries of the row alone.
+template <typename T, int G, int NV, bool ALIGNED>
+__device__ __forceinline__ void fetch_row(uint4 (&raw)[NV], const RowVectors<T> &x, uint32_t g, bool around)
+{
+    const uint4 *at = x.at(g);
+    if (ALIGNED && x.n == G * NV) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) raw[j] = at[G * j];
+    } else {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t v = g + G * j;
+            raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+            if (ALIGNED || around ? v < x.n : x.whole(v)) raw[j] = at[G * j];
+        }
+    }
+    if (ALIGNED) return;
+    const uint32_t last = x.n - 1, over = x.n * EPV<T> - x.lead - x.V;
+    uint4 begin, end;
+    if (!around) {
+        if (g == 0) begin = x.part(0);
+        if (g == last % G) end = x.part(last);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const uint32_t v = g + G * j;
+        if (v == last || (j == 0 && g == 0)) {
+            if (around) close_entries<T>(raw[j], ((v == 0 ? (1u << x.lead) - 1 : 0u) | (v == last ? 0xFFu << (EPV<T> - over) : 0u)) & ((1u << EPV<T>) - 1));
+            else raw[j] = v == 0 ? begin : end;
+        }
     }
 }
 
@@ -352,31 +365,34 @@ __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
     m.W = q.W;
     m.width = q.widths ? q.widths[r] : 1u;
     m.words = nullptr;
-    if (q.occupied) {
-        const uint64_t j = q.mask_rows ? (uint64_t)(int64_t)q.mask_rows[r] : r;  // (a negative one is a large one)
-        if (j < q.n_masks) m.words = q.occupied + j * q.W;
+    if (q.mask_rows) {
+        const uint32_t j = (uint32_t)q.mask_rows[r];  // (a negative one is a large one)
+        if (j < q.n_masks) m.words = q.occupied + (uint64_t)j * q.W;
+    } else if (q.occupied) {
+        m.words = q.occupied + r * q.W;
     }
     return m;
 }
 
 // Sets the closed entries of a group's rows to minus infinity.  Each word of a mask is worked out by one lane and handed to those that
 // hold its entries.  Every lane of the warp calls it; the result says whether entry tok is closed (true for what is no entry).
-template <typename T, int G, int NV>
-__device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> &x, const RowMask &mask, uint32_t g, bool aligned, int64_t tok)
+template <typename T, int G, int NV, bool ALIGNED>
+__device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> &x, const RowMask &mask, uint32_t g, int64_t tok)
 {
     constexpr int WL = NV * EPV<T> <= 32 ? 1 : NV * EPV<T> / 32;  // words of a lane
+    constexpr bool WORDS = ALIGNED || WL == 1;
     uint32_t word[WL];
-    if (aligned || WL == 1) {
+    if (WORDS) {
 #pragma unroll
         for (int k = 0; k < WL; ++k) word[k] = mask.closed(g + G * k);
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         uint32_t bits;
-        if (aligned) {
+        if (ALIGNED) {
             const uint32_t first = (g + G * j) * EPV<T>;
             bits = __shfl_sync(0xffffffffu, word[j * EPV<T> / 32], (first >> 5) & (G - 1), G) >> (first & 31);
-        } else if (WL == 1) {
+        } else if (WORDS) {
             const int first = x.first(g + G * j), w = first >> 5;
             const uint32_t a = __shfl_sync(0xffffffffu, word[0], w & (G - 1), G), b = __shfl_sync(0xffffffffu, word[0], (w + 1) & (G - 1), G);
             bits = __funnelshift_r(a, b, first & 31);
@@ -386,7 +402,7 @@ __device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> 
         close_entries<T>(raw[j], bits & ((1u << EPV<T>) - 1));
     }
     const uint32_t t = tok < 0 ? 0u : (uint32_t)tok;
-    if (!aligned && WL > 1) return tok < 0 || mask.is_closed(t);
+    if (!WORDS) return tok < 0 || mask.is_closed(t);
     uint32_t at = 0;
 #pragma unroll
     for (int k = 0; k < WL; ++k) {
@@ -394,6 +410,33 @@ __device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> 
         if ((int)((t >> 5) / G) == k) at = w;
     }
     return (at >> (t & 31)) & 1;
+}
+
+// The kernel of a row of at most n vectors: calls f with the lanes of a group and the vectors of a lane; false if the rows are long.  Lanes hold
+// more where rows are aligned (the ends of the others take registers, and their masks' words two lanes).
+template <bool WARP, bool ALIGNED, typename F>
+bool short_shape(uint32_t n, F &&f)
+{
+    auto with = [&](auto g, auto v) { f(g, v); return true; };
+    using std::integral_constant;
+    if constexpr (WARP) {  // the whole warp at a row
+        if (n <= 32) return with(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+        if (n <= 64) return with(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+    } else {
+        if (n <= 4) return with(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+        if (n <= 16) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
+        if constexpr (ALIGNED) {
+            if (n <= 32) return with(integral_constant<int, 4>{}, integral_constant<int, 8>{});
+            if (n <= 64) return with(integral_constant<int, 8>{}, integral_constant<int, 8>{});
+            if (n <= 128) return with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
+        } else {
+            if (n <= 32) return with(integral_constant<int, 8>{}, integral_constant<int, 4>{});
+            if (n <= 64) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
+        }
+    }
+    if (n <= 128) return with(integral_constant<int, 32>{}, integral_constant<int, 4>{});
+    if (n <= 256) return with(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+    return false;
 }
 
 }  // namespace

@@ -106,6 +106,7 @@ __device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *
 template <typename T, int N>
 __device__ __forceinline__ void add_vectors(const uint4 (&raw)[N], float m, float c, f32x2 &s, f32x2 &t)
 {
+    m = m == __int_as_float(0xFF800000) ? 0.0f : m;  // (nothing but impossible entries, whose powers of two are 0 relative to anything)
     if (!far_out(m)) {
         const float b = -__fmul_rn(m, c);
         const f32x2 c2 = both(c, c), low = both(b, b);
@@ -129,14 +130,13 @@ __device__ __forceinline__ void add_vectors(const uint4 (&raw)[N], float m, floa
             }
         }
     } else {
-        const float base = fmaxf(m, LOWEST);  // (nothing but impossible entries so far)
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             float x[EPV<T>];
             unpack(raw[u], x, T{});
 #pragma unroll
             for (int j = 0; j < EPV<T>; j += 2) {
-                const float y0 = max_nan((x[j] - base) * c, FAR_BELOW), y1 = max_nan((x[j + 1] - base) * c, FAR_BELOW);
+                const float y0 = max_nan((x[j] - m) * c, FAR_BELOW), y1 = max_nan((x[j + 1] - m) * c, FAR_BELOW);
                 const f32x2 e = both(ex2(y0), ex2(y1));
                 s = add2(s, e);
                 t = fma2(e, both(y0, y1), t);
@@ -652,8 +652,8 @@ __device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], flo
     return best;
 }
 
-template <typename T, bool MASKED, bool TOP, int G, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRows q, const ScoreOut o, bool aligned)
+template <typename T, bool MASKED, bool TOP, bool ALIGNED, int G, int NV>
+__global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_score_short(const LogitRows q, const ScoreOut o)
 {
     static_assert(!TOP || G == 32, "alternatives take the whole warp");
     __shared__ key_t64 s_cand[TOP ? SHORT_WARPS : 1][TOP ? SHORT_CAND : 1];
@@ -666,10 +666,10 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
         const bool there = r0 + lane / G < q.n_rows;  // (the warp's last rows may not be: it works on the last one instead)
         const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
         uint4 raw[NV];
-        fetch_row<T, G, NV>(raw, x, g, aligned);
+        fetch_row<T, G, NV, ALIGNED>(raw, x, g, r != 0 && r != q.n_rows - 1);
         const int64_t tok = row_token(q, r);
         bool shut = false;
-        if (MASKED) shut = close_row<T, G, NV>(raw, x, row_mask(q, r), g, aligned, tok);
+        if (MASKED) shut = close_row<T, G, NV, ALIGNED>(raw, x, row_mask(q, r), g, tok);
         float x_tok = 0.0f;
         if (g == 0 && o.logprob && tok >= 0) x_tok = to_f32(x.row[tok]);
 
@@ -709,46 +709,30 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_score_short(const LogitRow
     }
 }
 
-template <typename T, bool MASKED, bool TOP, int G, int NV>
-cudaError_t run_short(const LogitRows &q, const ScoreOut &o, bool aligned, cudaStream_t st)
-{
-    const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
-    k_score_short<T, MASKED, TOP, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, o, aligned);
-    g_vl_launches.fetch_add(1);
-    return cudaGetLastError();
-}
-
 // Whether the rows are short, and if so the launch.
-template <typename T, bool MASKED, bool TOP>
-bool launch_short(const LogitRows &q, const ScoreOut &o, cudaStream_t st, cudaError_t *e)
+template <typename T, bool MASKED, bool TOP, bool ALIGNED>
+bool launch_short(const LogitRows &q, const ScoreOut &o, uint32_t n, cudaStream_t st)
 {
-    bool aligned;
-    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
-    if constexpr (TOP) {
-        if (n <= 32) *e = run_short<T, MASKED, true, 32, 1>(q, o, aligned, st);
-        else if (n <= 64) *e = run_short<T, MASKED, true, 32, 2>(q, o, aligned, st);
-        else if (n <= 128) *e = run_short<T, MASKED, true, 32, 4>(q, o, aligned, st);
-        else if (n <= 256) *e = run_short<T, MASKED, true, 32, 8>(q, o, aligned, st);
-        else if (n <= 512) *e = run_short<T, MASKED, true, 32, 16>(q, o, aligned, st);
-        else return false;
-    } else {
-        if (n <= 4) *e = run_short<T, MASKED, false, 4, 1>(q, o, aligned, st);
-        else if (n <= 16) *e = run_short<T, MASKED, false, 4, 4>(q, o, aligned, st);
-        else if (n <= 32) *e = run_short<T, MASKED, false, 4, 8>(q, o, aligned, st);
-        else if (n <= 64) *e = run_short<T, MASKED, false, 8, 8>(q, o, aligned, st);
-        else if (n <= 128) *e = run_short<T, MASKED, false, 16, 8>(q, o, aligned, st);
-        else if (n <= 256) *e = run_short<T, MASKED, false, 32, 8>(q, o, aligned, st);
-        else if (n <= 512) *e = run_short<T, MASKED, false, 32, 16>(q, o, aligned, st);
-        else return false;
-    }
+    auto run = [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, NV = decltype(v)::value;
+        const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
+        k_score_short<T, MASKED, TOP, ALIGNED, G, NV>
+            <<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, o);
+        g_vl_launches.fetch_add(1);
+    };
+    if (short_shape<TOP, ALIGNED>(n, run)) return true;
+    if (n > 512) return false;
+    run(std::integral_constant<int, 32>{}, std::integral_constant<int, 16>{});
     return true;
 }
 
 template <typename T, bool MASKED, bool TOP>
 cudaError_t launch(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st)
 {
-    cudaError_t e;
-    return launch_short<T, MASKED, TOP>(q, o, st, &e) ? e : launch_long<T, MASKED, TOP>(q, o, device, st);
+    bool aligned;
+    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
+    if (aligned ? launch_short<T, MASKED, TOP, true>(q, o, n, st) : launch_short<T, MASKED, TOP, false>(q, o, n, st)) return cudaGetLastError();
+    return launch_long<T, MASKED, TOP>(q, o, device, st);
 }
 
 template <typename F>
@@ -780,7 +764,7 @@ int vl_logit_rows(const vl_logits *x, LogitRows *q)
     q->x = x->logits; q->n_rows = x->n_rows; q->stride = x->row_stride;
     q->V = x->n_vocab; q->W = (x->n_vocab + 31) / 32;
     q->tokens = x->tokens; q->token_bytes = x->token_bytes;
-    q->occupied = x->occupied; q->n_masks = x->n_masks; q->mask_rows = x->mask_rows; q->widths = x->widths;
+    q->occupied = x->occupied; q->n_masks = (uint32_t)(x->n_masks < (1ull << 31) ? x->n_masks : (1ull << 31)); q->mask_rows = x->mask_rows; q->widths = x->widths;
     q->scale = x->scale;
     return VL_OK;
 }

@@ -132,9 +132,10 @@ __global__ void __launch_bounds__(GRAD_THREADS) k_grad_long(const LogitRows q, c
 // Short rows: a group of lanes per row.
 constexpr uint32_t SHORT_WARPS = 8;
 
-template <typename T, bool MASKED, int G, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32) k_grad_short(const LogitRows q, const GradIn p, bool aligned, bool out_aligned)
+template <typename T, bool MASKED, bool ALIGNED, int G, int NV>
+__global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_grad_short(const LogitRows q, const GradIn p)
 {
+    const bool in_place = p.dx == q.x;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
     const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
     for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
@@ -142,32 +143,36 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32) k_grad_short(const LogitRows
         const uint64_t r = there ? r0 + lane / G : q.n_rows - 1;
         const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
         uint4 raw[NV];
-        if (there) fetch_row<T, G, NV>(raw, x, g, aligned);
+        if (there) fetch_row<T, G, NV, ALIGNED>(raw, x, g, !in_place && r != 0 && r != q.n_rows - 1);
         const RowMask mask = row_mask(q, r);
         const int64_t tok = row_token(q, r);
         bool shut = false;
-        if (MASKED) shut = close_row<T, G, NV>(raw, x, mask, g, aligned, tok);
+        if (MASKED) shut = close_row<T, G, NV, ALIGNED>(raw, x, mask, g, tok);
         const GradRow w = grad_row(q, p, r, tok, shut);
         if (!there) continue;
         T *const dx = static_cast<T *>(p.dx) + r * p.stride;
-        uint4 *const to = reinterpret_cast<uint4 *>(dx) + g;  // (aligned ones only)
+        const bool alike = ALIGNED || ((uintptr_t)dx & 15) == x.lead * sizeof(T);  // vectors of one are vectors of the other
+        uint4 *const to = reinterpret_cast<uint4 *>(reinterpret_cast<uintptr_t>(dx) & ~(uintptr_t)15) + g;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const uint32_t v = g + G * j;
             if (v >= x.n) break;
             const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[j], x.first(v), w);
-            if (aligned && out_aligned) to[G * j] = d;
+            if (alike && (ALIGNED || x.whole(v))) to[G * j] = d;
             else store_entries<T>(dx, x.first(v), q.V, d);
         }
     }
 }
 
-template <typename T, bool MASKED, int G, int NV>
-void run_short(const LogitRows &q, const GradIn &p, bool aligned, cudaStream_t st)
+// ALIGNED: both matrices' rows start and end on vectors.
+template <typename T, bool MASKED, bool ALIGNED>
+bool launch_short(const LogitRows &q, const GradIn &p, uint32_t n, cudaStream_t st)
 {
-    const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
-    const bool out_aligned = ((uintptr_t)p.dx & 15) == 0 && (q.n_rows <= 1 || p.stride % EPV<T> == 0);
-    k_grad_short<T, MASKED, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, p, aligned, out_aligned);
+    return short_shape<false, ALIGNED>(n, [&](auto g, auto v) {
+        constexpr int G = decltype(g)::value, NV = decltype(v)::value;
+        const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
+        k_grad_short<T, MASKED, ALIGNED, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, p);
+    });
 }
 
 template <typename T, bool MASKED>
@@ -175,13 +180,8 @@ cudaError_t launch(const LogitRows &q, const GradIn &p, cudaStream_t st)
 {
     bool aligned;
     const uint32_t n = row_vectors(q, sizeof(T), &aligned);
-    if (n <= 4) run_short<T, MASKED, 4, 1>(q, p, aligned, st);
-    else if (n <= 16) run_short<T, MASKED, 4, 4>(q, p, aligned, st);
-    else if (n <= 32) run_short<T, MASKED, 4, 8>(q, p, aligned, st);
-    else if (n <= 64) run_short<T, MASKED, 8, 8>(q, p, aligned, st);
-    else if (n <= 128) run_short<T, MASKED, 16, 8>(q, p, aligned, st);
-    else if (n <= 256) run_short<T, MASKED, 32, 8>(q, p, aligned, st);
-    else {
+    aligned = aligned && ((uintptr_t)p.dx & 15) == 0 && (q.n_rows <= 1 || p.stride % EPV<T> == 0);
+    if (!(aligned ? launch_short<T, MASKED, true>(q, p, n, st) : launch_short<T, MASKED, false>(q, p, n, st))) {
         const uint32_t y = (uint32_t)(q.n_rows < 65535 ? q.n_rows : 65535);
         const uint64_t z = (q.n_rows + y - 1) / y;
         k_grad_long<T, MASKED><<<dim3((n + GRAD_TILE - 1) / GRAD_TILE, y, (uint32_t)(z < 65535 ? z : 65535)), GRAD_THREADS, 0, st>>>(q, p);
