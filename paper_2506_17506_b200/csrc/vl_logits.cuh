@@ -412,30 +412,37 @@ __device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> 
     return (at >> (t & 31)) & 1;
 }
 
-// The kernel of a row of at most n vectors: calls f with the lanes of a group and the vectors of a lane; false if the rows are long.  Lanes hold
-// more where rows are aligned (the ends of the others take registers, and their masks' words two lanes).
+// The kernel of rows of at most n vectors and W words of a mask: calls f with the lanes of a group and the vectors of a lane; false if the
+// rows are long.  A group has a lane for every word (where a lane holds at most 32 entries it has one anyway).  Rows that are not aligned
+// have a vector more than their entries fill: a fifth one a lane takes it in.
 template <bool WARP, bool ALIGNED, typename F>
-bool short_shape(uint32_t n, F &&f)
+bool short_shape(uint32_t n, uint32_t W, F &&f)
 {
-    auto with = [&](auto g, auto v) { f(g, v); return true; };
     using std::integral_constant;
+    auto with = [&](auto g, auto v) { f(g, v); return true; };
+    constexpr integral_constant<int, 4> g4;
+    constexpr integral_constant<int, 8> g8;
+    constexpr integral_constant<int, 16> g16;
+    constexpr integral_constant<int, 32> g32;
+    constexpr integral_constant<int, 1> v1;
+    constexpr integral_constant<int, 5> v5;
     if constexpr (WARP) {  // the whole warp at a row
-        if (n <= 32) return with(integral_constant<int, 32>{}, integral_constant<int, 1>{});
-        if (n <= 64) return with(integral_constant<int, 32>{}, integral_constant<int, 2>{});
+        if (n <= 32) return with(g32, v1);
+        if (n <= 160 && W <= 32) return with(g32, v5);
+    } else if constexpr (ALIGNED) {
+        if (n <= 4) return with(g4, v1);
+        if (n <= 16) return with(g4, g4);
+        if (n <= 32) return with(g4, g8);
+        if (n <= 64) return with(g8, g8);
+        if (n <= 128) return with(g16, g8);
     } else {
-        if (n <= 4) return with(integral_constant<int, 4>{}, integral_constant<int, 1>{});
-        if (n <= 16) return with(integral_constant<int, 4>{}, integral_constant<int, 4>{});
-        if constexpr (ALIGNED) {
-            if (n <= 32) return with(integral_constant<int, 4>{}, integral_constant<int, 8>{});
-            if (n <= 64) return with(integral_constant<int, 8>{}, integral_constant<int, 8>{});
-            if (n <= 128) return with(integral_constant<int, 16>{}, integral_constant<int, 8>{});
-        } else {
-            if (n <= 32) return with(integral_constant<int, 8>{}, integral_constant<int, 4>{});
-            if (n <= 64) return with(integral_constant<int, 16>{}, integral_constant<int, 4>{});
-        }
+        if (n <= 4) return with(g4, v1);
+        if (n <= 20 && W <= 4) return with(g4, v5);
+        if (n <= 40 && W <= 8) return with(g8, v5);
+        if (n <= 80 && W <= 16) return with(g16, v5);
+        if (n <= 160 && W <= 32) return with(g32, v5);
     }
-    if (n <= 128) return with(integral_constant<int, 32>{}, integral_constant<int, 4>{});
-    if (n <= 256) return with(integral_constant<int, 32>{}, integral_constant<int, 8>{});
+    if (n <= 256) return with(g32, g8);
     return false;
 }
 

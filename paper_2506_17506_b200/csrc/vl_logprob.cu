@@ -720,7 +720,7 @@ bool launch_short(const LogitRows &q, const ScoreOut &o, uint32_t n, cudaStream_
             <<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, o);
         g_vl_launches.fetch_add(1);
     };
-    if (short_shape<TOP, ALIGNED>(n, run)) return true;
+    if (short_shape<TOP, ALIGNED>(n, q.W, run)) return true;
     if (n > 512) return false;
     run(std::integral_constant<int, 32>{}, std::integral_constant<int, 16>{});
     return true;

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_grad_sho
 template <typename T, bool MASKED, bool ALIGNED>
 bool launch_short(const LogitRows &q, const GradIn &p, uint32_t n, cudaStream_t st)
 {
-    return short_shape<false, ALIGNED>(n, [&](auto g, auto v) {
+    return short_shape<false, ALIGNED>(n, q.W, [&](auto g, auto v) {
         constexpr int G = decltype(g)::value, NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
         k_grad_short<T, MASKED, ALIGNED, G, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, p);
