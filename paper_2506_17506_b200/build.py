@@ -1,10 +1,12 @@
 """Builds ``libverilocc.so`` in-tree with nvcc for sm_100a (cross-compiles without a GPU)."""
 from __future__ import annotations
 
+import concurrent.futures
 import glob
 import os
 import subprocess
 import sys
+import tempfile
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -28,12 +30,18 @@ def build(force: bool = False, verbose: bool = False, extra=()) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"),
+           "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"),
            "-I", os.path.join(HERE, "csrc")]
     if verbose:
         cmd += ["-Xptxas", "-v"]
-    cmd += list(extra) + ["-o", LIB] + sources()
-    subprocess.check_call(cmd)
+    cmd += list(extra)
+    with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(os.cpu_count() or 1) as pool:
+        def compile_one(src):       # the files are independent of each other
+            obj = os.path.join(tmp, os.path.basename(src) + ".o")
+            subprocess.check_call(cmd + ["-c", "-o", obj, src])
+            return obj
+        objects = list(pool.map(compile_one, sources()))
+        subprocess.check_call(cmd + ["-shared", "-o", LIB] + objects)
     return LIB
 
 

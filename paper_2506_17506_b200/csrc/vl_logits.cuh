@@ -20,6 +20,17 @@ struct LogitRows {
     const uint8_t *widths;
     float scale;
 };
+// Where the scores go; what is null is not wanted.
+struct ScoreOut {
+    float *logprob, *entropy, *stats;
+    uint32_t top;
+    int32_t *ids;
+    float *lps;
+};
+cudaError_t vl_scores_f32(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st);
+cudaError_t vl_scores_f16(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st);
+cudaError_t vl_scores_bf16(const LogitRows &q, const ScoreOut &o, int device, cudaStream_t st);
+
 // Checks a descriptor: VL_OK and the kernels' form of it, or an error.
 int vl_logit_rows(const vl_logits *x, LogitRows *out);
 
