@@ -255,16 +255,17 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams 
                 if (__shfl_sync(0xffffffffu, near, n + d - 1) <= (int)t) n += d;
             uint64_t k = k0 + n;
             Weight w = weight_of(q, k);
+            Part p{0.0f, 0.0f, 0, 0};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
+                uint64_t to;
                 if (many) {
                     uint64_t a = k0, b = q.N + 1;
                     while (a < b) {
                         const uint64_t mid = (a + b) >> 1;
                         if (offset(mid) <= (int)(t + j)) a = mid + 1; else b = mid;
                     }
-                    k = a;
-                    w = weight_of(q, k);
+                    to = a;
                 } else {
                     for (;;) {
                         const int next = __shfl_sync(0xffffffffu, near, n);
@@ -272,15 +273,17 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams 
                         if (!__any_sync(0xffffffffu, on)) break;
                         n += on;
                     }
-                    if (k != k0 + n) {
-                        k = k0 + n;
-                        w = weight_of(q, k);
-                    }
+                    to = k0 + n;
                 }
-                Part p{0.0f, 0.0f, 0, 0};
+                if (to != k) {  // another candidate's
+                    loss += part_loss<REF>(q, p, w);
+                    p = Part{0.0f, 0.0f, 0, 0};
+                    k = to;
+                    w = weight_of(q, k);
+                }
                 g[j] = token<REF>(q, x[j], y[j], z[j], w, k > 0 && k <= q.N && t + j < len, p);
-                loss += part_loss<REF>(q, p, w);
             }
+            loss += part_loss<REF>(q, p, w);
             // first offset above the next step's first token
             if (many) k0 = first_above(q.off, q.N + 1, (int64_t)(begin + t0 + PL_STEP), lane);
             else k0 += __popc(__ballot_sync(0xffffffffu, near <= (int)(t0 + PL_STEP)));
