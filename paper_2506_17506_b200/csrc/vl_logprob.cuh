@@ -20,7 +20,6 @@ namespace {
 namespace cg = cooperative_groups;
 typedef unsigned long long key_t64;
 
-
 // ---- values with their places, as keys: larger values first, lower places first among equals (zeros of both signs are equal)
 __device__ __forceinline__ uint32_t ordered(float x)
 {
@@ -55,6 +54,7 @@ __device__ __forceinline__ key_t64 merge32(key_t64 a, key_t64 b, uint32_t lane)
     for (uint32_t d = 16; d; d /= 2) k = exchange(k, d, (lane & d) == 0);
     return k;
 }
+
 // ---- running sums
 // In powers of two: y_i = c x_i - B with c = scale log2 e and B = c m rounded, m the largest logit so far; s = sum 2^y, t = sum 2^y y.
 // One multiply-add makes y, and B being rounded makes no difference: it is the same B in every term, and what it lacks to c m is put
@@ -209,7 +209,8 @@ __device__ __forceinline__ uint4 fetch(const RowVectors<T> &x, const RowMask &ma
 // barrier.)  The warps' sums of a row meet in one of the cluster's blocks and are summed up there by one warp, another one for every
 // row; nobody waits for it: there are two sets of places, and a cluster barrier whose two halves are a row apart.
 // Small blocks, eight to a multiprocessor: what a warp does once per row weighs less with four warps at a row than with sixteen
-// (4,096 rows of 131,072: 185 us, 198 with blocks of 512 threads; 1,200 rows of 8,000: 12 and 22).
+// (bf16, 4,096 rows of 131,072 185 us and 198 with blocks of 512 threads when this was chosen, 180 now: 5.9 TB/s; 1,200 rows of 8,000 12
+// and 22).  592 rows of 1,000,000 take 187 us, 6.3 TB/s: what is left at 131,072 is what a row costs at its end.
 constexpr int LONG_THREADS = 128, LONG_U = 4, LONG_RING = 3, LONG_PARTS = 8;
 constexpr size_t LONG_SMEM = (size_t)LONG_THREADS * LONG_U * LONG_RING * 16;
 
@@ -246,12 +247,12 @@ struct PartOfRow {
 // (from L2), and what is no smaller than the bound is gathered in one block.  If that is more than fits (rows of many equal logits), the
 // k-th best of what was gathered is a higher bound, and the stripes are read once more.
 constexpr uint32_t CAND = 256, TOP_GROUPS = 32;
+static_assert(LONG_PARTS * (LONG_THREADS / 32) <= TOP_GROUPS && VL_MAX_ALTERNATIVES <= TOP_GROUPS, "a group lies in a warp; as many groups as alternatives");
 
-// The bound's key out of the groups' keys: keys[] holds `per` of them for each group.
-__device__ __forceinline__ key_t64 bound_of(const key_t64 *keys, uint32_t per, uint32_t top, uint32_t lane)
+// The k-th best of the groups' keys.
+__device__ __forceinline__ key_t64 bound_of(const key_t64 *keys, uint32_t top, uint32_t lane)
 {
-    key_t64 mine = 0;
-    for (uint32_t i = 0; i < per; ++i) mine = max(mine, keys[lane * per + i]);
+    const key_t64 mine = keys[lane];
     uint32_t rank = 0;
 #pragma unroll 8
     for (uint32_t j = 0; j < 32; ++j) {
@@ -281,7 +282,7 @@ __global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_lon
     const uint32_t log_parts = CLUSTER ? log_of_parts : 0;
     extern __shared__ uint4 s_ring[];  // [RING][U][NT]
     __shared__ float s_sums[2][MAX_PARTS * NW][3];
-    __shared__ key_t64 s_keys[TOP ? (MAX_PARTS * NW > TOP_GROUPS ? MAX_PARTS * NW : TOP_GROUPS) : 1], s_cand[TOP ? CAND : 1], s_bound;
+    __shared__ key_t64 s_keys[TOP ? TOP_GROUPS : 1], s_cand[TOP ? CAND : 1], s_bound;
     __shared__ uint32_t s_n[2];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
     const uint64_t step = gridDim.x >> log_parts;
@@ -427,8 +428,8 @@ __global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_lon
         }
         uint32_t n = 0;
         if (TOP) {
-            // a key that the thread's best entry reaches, whatever its place in its vector; the best of each of 32 / parts groups of
-            // the block, or of its warps if these are more, to every block
+            // a key that the thread's best entry reaches, whatever its place in its vector; the best of each of the block's 32 / parts
+            // groups, to every block
             const bool any = a.best < p.v1;
             const int in = any ? x.first(a.best) : 0;
             key_t64 k = any ? rank_key(a.m, (uint32_t)(in + EPV<T> - 1)) : 0ull;
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_lon
                 *away(&s_keys[TOP ? (part * NW + warp) * per_warp + lane / lanes : 0], b) = k;
             if (tid == 0) s_n[set & 1] = 0;
             meet();
-            key_t64 bound = bound_of(s_keys, parts * NW * per_warp / TOP_GROUPS, o.top, lane);
+            key_t64 bound = bound_of(s_keys, o.top, lane);
             uint32_t *const count = away(&s_n[set & 1], block);
             key_t64 *const cand = away(&s_cand[0], block);
             for (;;) {
