@@ -9,6 +9,7 @@ int vl_logit_rows(const vl_logits *x, LogitRows *q)
     if (x->n_rows > 1 && x->row_stride < x->n_vocab) return VL_ERR_INVALID_ARG;
     if (x->n_rows && (!x->logits || (uintptr_t)x->logits % size)) return VL_ERR_INVALID_ARG;
     if (x->n_rows > (1ull << 40) || x->row_stride > (1ull << 40)) return VL_ERR_INVALID_ARG;
+    if (x->n_rows > 1 && x->row_stride > (1ull << 56) / x->n_rows) return VL_ERR_INVALID_ARG;  // (no such memory)
     if (x->tokens && ((x->token_bytes != 2 && x->token_bytes != 4 && x->token_bytes != 8) || (uintptr_t)x->tokens % x->token_bytes))
         return VL_ERR_INVALID_ARG;
     if (((uintptr_t)x->occupied | (uintptr_t)x->mask_rows) & 3) return VL_ERR_INVALID_ARG;

@@ -251,7 +251,7 @@ extern "C" int vl_token_logprobs_backward(int device, const vl_logits *x, const 
     if (d_g_entropy && !d_entropy) return VL_ERR_INVALID_ARG;
     if (d_g_logprob && !q.tokens) return VL_ERR_INVALID_ARG;
     if (q.n_rows > 1 && out_stride < q.V) return VL_ERR_INVALID_ARG;
-    if (out_stride > (1ull << 40)) return VL_ERR_INVALID_ARG;
+    if (out_stride > (1ull << 40) || (q.n_rows > 1 && out_stride > (1ull << 56) / q.n_rows)) return VL_ERR_INVALID_ARG;
     if (q.n_rows && (!d_row_stats || !d_dlogits || (uintptr_t)d_dlogits % (x->dtype == VL_F32 ? 4 : 2))) return VL_ERR_INVALID_ARG;
     if (d_dlogits == x->logits && q.n_rows > 1 && out_stride != q.stride) return VL_ERR_INVALID_ARG;
     if (q.n_rows == 0) return VL_OK;

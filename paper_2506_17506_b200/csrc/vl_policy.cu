@@ -54,30 +54,53 @@ __device__ __forceinline__ double block_sum(double v, double *s)
 
 __device__ __forceinline__ int64_t inside(int64_t t, uint64_t T) { return min(max(t, (int64_t)0), (int64_t)T); }
 
-// A block or a cluster of eight per program.  A thread's first rewards stay in registers.
-constexpr uint32_t ADV_THREADS = 1024, ADV_KEEP = 8;
+// The advantages and weights of program j, by `step` threads of which this one is thread k0; total(v, at) sums over them, at = 0 the first
+// time, 1 the second.  A thread's first KEEP rewards stay in registers.
+template <uint32_t KEEP, typename F>
+__device__ __forceinline__ void advantages(const GroupParams &q, uint32_t j, uint64_t step, uint64_t k0, double2 *weights, float *advantage, F &&total)
+{
+    const uint64_t K = q.K[j];
+    const uint4 *out = q.out[j];
+    // taken from the first one's: equal rewards leave exactly nothing, which a division by their deviation would blow up
+    const double base = reward_of(__ldg(out), q.pair_cost, q.bank_cost);
+    double keep[KEEP];
+#pragma unroll
+    for (uint32_t i = 0; i < KEEP; ++i)
+        keep[i] = k0 + i * step < K ? reward_of(__ldg(out + k0 + i * step), q.pair_cost, q.bank_cost) - base : 0.0;
+    auto each = [&](auto &&f) {
+#pragma unroll
+        for (uint32_t i = 0; i < KEEP; ++i)
+            if (k0 + i * step < K) f(k0 + i * step, keep[i]);
+        for (uint64_t k = k0 + KEEP * step; k < K; k += step) f(k, reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base);
+    };
+    double sum = 0.0;
+    each([&](uint64_t, double c) { sum += c; });
+    const double mean = total(sum, 0u) / (double)K;
+    double by = 1.0;
+    if (q.normalise) {
+        double var = 0.0;
+        each([&](uint64_t, double c) { var += (c - mean) * (c - mean); });
+        by = 1.0 / (sqrt(total(var, 1u) / (double)K) + q.eps);
+    }
+    const double per_token = 1.0 / (double)max(inside(q.off[q.N], q.T) - inside(q.off[0], q.T), (int64_t)1);
+    each([&](uint64_t k, double c) {
+        const double a = (c - mean) * by;
+        const uint64_t at = q.first[j] + k;
+        const double w = q.per_token ? per_token : 1.0 / ((double)q.N * (double)max(q.off[at + 1] - q.off[at], (int64_t)1));
+        weights[at] = make_double2(w, w * a);
+        if (advantage) advantage[at] = (float)a;
+    });
+}
+
+// A block or a cluster of eight per program.
+constexpr uint32_t ADV_THREADS = 1024;
 __global__ void __launch_bounds__(ADV_THREADS) k_advantages(const __grid_constant__ GroupParams q)
 {
     __shared__ double s[ADV_THREADS / 32], s_all[2][8];
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t parts = cluster.num_blocks(), part = cluster.block_rank();
-    const uint32_t j = blockIdx.x / parts;
-    const uint64_t K = q.K[j], step = (uint64_t)parts * blockDim.x, k0 = (uint64_t)part * blockDim.x + threadIdx.x;
-    const uint4 *out = q.out[j];
     pdl_go();
     pdl_wait();
-    // taken from the first one's: equal rewards leave exactly nothing, which a division by their deviation would blow up
-    const double base = reward_of(__ldg(out), q.pair_cost, q.bank_cost);
-    double keep[ADV_KEEP];
-#pragma unroll
-    for (uint32_t i = 0; i < ADV_KEEP; ++i)
-        keep[i] = k0 + i * step < K ? reward_of(__ldg(out + k0 + i * step), q.pair_cost, q.bank_cost) - base : 0.0;
-    auto each = [&](auto &&f) {
-#pragma unroll
-        for (uint32_t i = 0; i < ADV_KEEP; ++i)
-            if (k0 + i * step < K) f(k0 + i * step, keep[i]);
-        for (uint64_t k = k0 + ADV_KEEP * step; k < K; k += step) f(k, reward_of(__ldg(out + k), q.pair_cost, q.bank_cost) - base);
-    };
     auto total = [&](double v, uint32_t at) {  // over the cluster, in the blocks' order
         v = block_sum(v, s);
         if (parts == 1) return v;
@@ -88,23 +111,7 @@ __global__ void __launch_bounds__(ADV_THREADS) k_advantages(const __grid_constan
         return v;
     };
     if (parts > 1) cluster.sync();  // (all of them run)
-    double sum = 0.0;
-    each([&](uint64_t, double c) { sum += c; });
-    const double mean = total(sum, 0) / (double)K;
-    double by = 1.0;
-    if (q.normalise) {
-        double var = 0.0;
-        each([&](uint64_t, double c) { var += (c - mean) * (c - mean); });
-        by = 1.0 / (sqrt(total(var, 1) / (double)K) + q.eps);
-    }
-    const double per_token = 1.0 / (double)max(inside(q.off[q.N], q.T) - inside(q.off[0], q.T), (int64_t)1);
-    each([&](uint64_t k, double c) {
-        const double a = (c - mean) * by;
-        const uint64_t at = q.first[j] + k;
-        const double w = q.per_token ? per_token : 1.0 / ((double)q.N * (double)max(q.off[at + 1] - q.off[at], (int64_t)1));
-        q.weights[at] = make_double2(w, w * a);
-        if (q.advantage) q.advantage[at] = (float)a;
-    });
+    advantages<8>(q, blockIdx.x / parts, (uint64_t)parts * blockDim.x, (uint64_t)part * blockDim.x + threadIdx.x, q.weights, q.advantage, total);
 }
 
 struct TokenParams {
@@ -198,13 +205,10 @@ __device__ __forceinline__ double part_loss(const TokenParams &q, const Part &p,
     return REF ? fma(q.kl * w.w, (double)p.kl, -w.wA * in) : -w.wA * in;
 }
 
+// A warp's run of tokens, `len` of them from `begin` on: their derivatives; the lanes' parts of the loss.
 template <bool REF>
-__global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams q)
+__device__ __forceinline__ double run_tokens(const TokenParams &q, uint64_t begin, uint32_t len, uint32_t lane)
 {
-    __shared__ double s[PL_WARPS];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint64_t begin = ((uint64_t)blockIdx.x * PL_WARPS + warp) * q.per_warp;
-    const uint32_t len = begin < q.T ? (uint32_t)min(q.per_warp, q.T - begin) : 0;  // tokens of the warp; from here on counted from its first
     const float *const lp = q.lp + begin, *const old = (q.old ? q.old : q.lp) + begin, *const ref = (REF ? q.ref : q.lp) + begin;
     constexpr int FAR = 0x7FFFFFFF;
     auto offset = [&](uint64_t k) -> int {
@@ -224,7 +228,6 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams 
             nz = make_float4(one(ref, 0), one(ref, 1), one(ref, 2), one(ref, 3));
         }
     };
-    pdl_go();
     double loss = 0.0;
     uint64_t k0 = 0;  // first offset above the step's first token
     if (len) {
@@ -302,15 +305,58 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams 
             }
         }
     }
-    // fixed order: lanes, warps, blocks
+    return loss;
+}
+
+// Sum over the block's warps, in their order; in the first thread.
+__device__ __forceinline__ double warps_sum(double v, double *s)
+{
 #pragma unroll
-    for (int d = 16; d; d >>= 1) loss += __shfl_xor_sync(0xffffffffu, loss, d);
-    if (lane == 0) s[warp] = loss;
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = v;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        loss = 0.0;
-        for (uint32_t w = 0; w < PL_WARPS; ++w) loss += s[w];
-        q.part[blockIdx.x] = loss;
+    v = 0.0;
+    if (threadIdx.x == 0)
+        for (uint32_t w = 0; w < PL_WARPS; ++w) v += s[w];
+    return v;
+}
+
+template <bool REF>
+__global__ void __launch_bounds__(PL_THREADS) k_policy_tokens(const TokenParams q)
+{
+    __shared__ double s[PL_WARPS];
+    const uint64_t begin = ((uint64_t)blockIdx.x * PL_WARPS + (threadIdx.x >> 5)) * q.per_warp;
+    pdl_go();
+    const double loss = warps_sum(run_tokens<REF>(q, begin, begin < q.T ? (uint32_t)min(q.per_warp, q.T - begin) : 0, threadIdx.x & 31), s);
+    if (threadIdx.x == 0) q.part[blockIdx.x] = loss;
+}
+
+// Small losses of one program: one launch of one cluster, each block with all the weights in its shared memory.  On the device it is no
+// shorter than the three kernels that overlap (100 samples of 113 tokens 7.8 us and 7.3, 1,000 of 30 12.2 and 9.9), but the
+// host makes one launch for three (15 us a call, 20).
+constexpr uint32_t SMALL_BLOCKS = 8, SMALL_N = 256, SMALL_T = 16384;
+
+template <bool REF>
+__global__ void __launch_bounds__(PL_THREADS) k_policy_small(const __grid_constant__ GroupParams g, const __grid_constant__ TokenParams all,
+                                                             float *out)
+{
+    __shared__ double2 s_weights[SMALL_N];
+    __shared__ double s[PL_WARPS], s_part[SMALL_BLOCKS];
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t part = cluster.block_rank();
+    TokenParams q = all;
+    q.weights = s_weights;
+    const uint64_t begin = ((uint64_t)part * PL_WARPS + (threadIdx.x >> 5)) * q.per_warp;
+    advantages<SMALL_N / PL_THREADS>(g, 0, PL_THREADS, threadIdx.x, s_weights, part == 0 ? g.advantage : nullptr,
+                                     [&](double v, uint32_t) { return block_sum(v, s); });
+    cluster.sync();  // (the weights are there; all blocks run)
+    const double loss = warps_sum(run_tokens<REF>(q, begin, begin < q.T ? (uint32_t)min(q.per_warp, q.T - begin) : 0, threadIdx.x & 31), s);
+    if (threadIdx.x == 0) *cluster.map_shared_rank(&s_part[part], 0) = loss;
+    cluster.sync();
+    if (part == 0 && threadIdx.x == 0) {
+        double v = 0.0;
+        for (uint32_t b = 0; b < SMALL_BLOCKS; ++b) v += s_part[b];
+        *out = (float)v;
     }
 }
 
@@ -324,19 +370,18 @@ __global__ void __launch_bounds__(PL_THREADS) k_policy_sum(const double *part, u
     if (threadIdx.x == 0) *loss = (float)v;
 }
 
-cudaError_t launch_advantages(const GroupParams &q, uint32_t groups, uint64_t most, cudaStream_t st)
+template <typename... P, typename... A>
+cudaError_t launch_cluster(void (*kernel)(P...), uint32_t blocks, uint32_t parts, uint32_t threads, cudaStream_t st, const A &...args)
 {
-    const uint32_t parts = most > 2 * ADV_THREADS ? 8 : 1;  // most: candidates of the largest program
-    const uint64_t threads = (most / parts + 31) / 32 * 32;
     cudaLaunchAttribute at{};
     at.id = cudaLaunchAttributeClusterDimension;
     at.val.clusterDim.x = parts;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(groups * parts); cfg.blockDim = (uint32_t)(threads < 64 ? 64 : threads < ADV_THREADS ? threads : ADV_THREADS); cfg.stream = st;
+    cfg.gridDim = dim3(blocks); cfg.blockDim = threads; cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = 1;
     g_vl_launches.fetch_add(1);
-    return cudaLaunchKernelEx(&cfg, k_advantages, q);
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
@@ -375,22 +420,6 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
     q.off = d_token_off; q.N = N; q.T = n_tokens;
     q.weights = static_cast<double2 *>(d_work); q.advantage = d_advantage; q.per_token = rules->per_token;
     double *const part = reinterpret_cast<double *>(q.weights + N);
-    uint64_t first = 0;
-    for (uint32_t j = 0; j < n;) {
-        uint32_t m = 0;
-        uint64_t most = 0;
-        for (; j < n && m < PL_GROUPS; ++j) {
-            if (!K[j]) continue;
-            q.out[m] = reinterpret_cast<const uint4 *>(d_out[j]);
-            q.K[m] = K[j];
-            q.first[m++] = first;
-            first += K[j];
-            most = K[j] > most ? K[j] : most;
-        }
-        if (!m) break;
-        // (no overlap with a launch in front that it does not know)
-        if (launch_advantages(q, m, most, st) != cudaSuccess) return VL_ERR_CUDA;
-    }
     TokenParams t;
     t.weights = q.weights; t.off = d_token_off; t.N = N; t.T = n_tokens;
     t.lp = d_logprob; t.old = d_old_logprob; t.ref = d_ref_logprob;
@@ -404,6 +433,30 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
     t.g = d_g_logprob; t.part = part;
     t.vectors = !(((uintptr_t)d_logprob | (uintptr_t)d_old_logprob | (uintptr_t)(rules->kl != 0.0 ? d_ref_logprob : nullptr) | (uintptr_t)d_g_logprob) & 15);
     const uint64_t steps = (n_tokens + PL_STEP - 1) / PL_STEP;
+    uint64_t first = 0;
+    for (uint32_t j = 0; j < n;) {
+        uint32_t m = 0;
+        uint64_t most = 0;
+        for (; j < n && m < PL_GROUPS; ++j) {
+            if (!K[j]) continue;
+            q.out[m] = reinterpret_cast<const uint4 *>(d_out[j]);
+            q.K[m] = K[j];
+            q.first[m++] = first;
+            first += K[j];
+            most = K[j] > most ? K[j] : most;
+        }
+        if (!m) break;
+        if (m == 1 && q.K[0] == N && N <= SMALL_N && n_tokens <= SMALL_T) {
+            t.per_warp = (steps + SMALL_BLOCKS * PL_WARPS - 1) / (SMALL_BLOCKS * PL_WARPS) * PL_STEP;
+            const auto kernel = t.kl != 0.0 ? k_policy_small<true> : k_policy_small<false>;
+            return launch_cluster(kernel, SMALL_BLOCKS, SMALL_BLOCKS, PL_THREADS, st, q, t, d_loss) == cudaSuccess ? VL_OK : VL_ERR_CUDA;
+        }
+        // a block, or a cluster for programs of many candidates
+        const uint32_t parts = most > 2 * ADV_THREADS ? 8 : 1;
+        const uint64_t threads = (most / parts + 31) / 32 * 32;
+        if (launch_cluster(k_advantages, m * parts, parts, (uint32_t)(threads < 64 ? 64 : threads < ADV_THREADS ? threads : ADV_THREADS), st, q) != cudaSuccess)
+            return VL_ERR_CUDA;
+    }
     uint64_t blocks = (steps + PL_WARPS - 1) / PL_WARPS;
     const uint64_t resident = 8 * (uint64_t)vl_device_sm_count(device);
     const uint64_t at_most = resident < PL_MAX_BLOCKS ? resident : PL_MAX_BLOCKS;

@@ -75,7 +75,7 @@ def _check(got, verdicts, off, lp, old=None, rf=None, **kw):
 
 
 @pytest.mark.parametrize("sizes,mean", [([1], 5), ([2], 1), ([100], 113), ([7, 1, 300], 40), ([33] * 230, 3), ([5000], 2), ([1200, 900], 9),
-                                        ([3], 9000), ([1, 1, 1], 700), ([100] * 20, 60), ([40], 0.3)])
+                                        ([3], 9000), ([1, 1, 1], 700), ([100] * 20, 60), ([40], 0.3), ([500, 0, 1, 523], 31), ([1023, 1], 20)])
 @pytest.mark.parametrize("kw", [dict(), dict(normalise=False, pair_cost=0.01, bank_cost=0.001, per_token=True),
                                 dict(pair_cost=0.002, kl=0.1, clip_lo=0.1, clip_hi=0.4), dict(per_token=True, kl=-0.05, clip_lo=1.5, clip_hi=float("inf"))],
                          ids=["plain", "costs", "reference", "unclipped"])
@@ -195,10 +195,11 @@ def test_derivative_against_differences(B):
         assert abs(g[t] - want) <= 1e-8 + 32 * U * abs(want), (t, g[t], want)
 
 
-def test_streams_graphs_and_two_calls_at_once(B):
+@pytest.mark.parametrize("mean", [20, 300])
+def test_streams_graphs_and_two_calls_at_once(B, mean):
     import torch
     rng = np.random.default_rng(8)
-    v, off, lp, old, rf = _case(rng, [100, 50], 300)
+    v, off, lp, old, rf = _case(rng, [100, 50], mean)
     outs, o, l, ol, r = _dev(v, off, lp, old, rf)
     l2 = ol.clone()
     want = [B.vl_policy_loss(outs, o, x, ol, ref_logprob=r, kl=0.1) for x in (l, l2)]

@@ -18,7 +18,7 @@ def _good(B):
 
 
 BAD = [dict(logits=None), dict(logits=4098), dict(dtype=3), dict(dtype=-1), dict(n_vocab=0), dict(n_vocab=(1 << 30) + 1, row_stride=1 << 31),
-       dict(row_stride=39), dict(n_rows=(1 << 40) + 1), dict(token_bytes=1), dict(tokens=4100), dict(occupied=4097), dict(mask_rows=4098),
+       dict(row_stride=39), dict(n_rows=(1 << 40) + 1), dict(n_rows=1 << 30, n_masks=1 << 30, row_stride=1 << 30), dict(token_bytes=1), dict(tokens=4100), dict(occupied=4097), dict(mask_rows=4098),
        dict(occupied=None, mask_rows=4096), dict(n_masks=1), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
        dict(scale=float("inf"))]
 
