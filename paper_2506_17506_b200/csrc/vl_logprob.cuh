@@ -569,81 +569,80 @@ cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaS
 // Short rows: a group of lanes per row, every logit read once into registers.
 constexpr uint32_t SHORT_WARPS = 8, SHORT_CAND = 128;
 
-// The warp's first `top` keys in order, one to a lane, out of one key per lane: round by round for few (8 instructions a round), sorted
-// for many.
-__device__ __forceinline__ key_t64 first_keys(key_t64 k, uint32_t top, uint32_t lane)
+// The k-th largest of the lanes' values (0 if fewer lanes have one): value by value for few, sorted for many.
+__device__ __forceinline__ uint32_t kth_value(uint32_t v, uint32_t k, uint32_t lane)
 {
-    if (top > 16) return sort32(k, lane);
-    key_t64 mine = 0;
-    for (uint32_t i = 0; i < top; ++i) {
-        const uint32_t hi = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32));
-        const uint32_t lo = __reduce_max_sync(0xffffffffu, (uint32_t)(k >> 32) == hi ? (uint32_t)k : 0u);
-        const key_t64 best = ((key_t64)hi << 32) | lo;
-        if (lane == i) mine = best;
-        if (k == best) k = 0;
+    if (k <= 8) {
+        for (uint32_t found = 0;;) {
+            const uint32_t most = __reduce_max_sync(0xffffffffu, v);
+            found += __popc(__ballot_sync(0xffffffffu, v == most));
+            if (found >= k || most == 0) return most;
+            if (v == most) v = 0;
+        }
     }
-    return mine;
+#pragma unroll
+    for (uint32_t n = 2; n <= 32; n *= 2)
+#pragma unroll
+        for (uint32_t d = n / 2; d; d /= 2) {
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, v, d);
+            v = ((lane & d) == 0) == ((lane & n) == 0) ? max(v, other) : min(v, other);
+        }
+    return __shfl_sync(0xffffffffu, v, k - 1);
 }
 
-// The best entries of a row that the whole warp holds (G = 32), as in the long rows: the k-th of the lanes' best bounds the k-th of all.
+// The best entries of a row that the whole warp holds (G = 32), one to a lane in order, as in the long rows: the k-th of the lanes' best bounds
+// the k-th of all, what is no smaller is gathered, and if that is more than fits, the k-th of what was gathered is a higher bound.
 // own: the lane's largest logit.
 template <typename T, int NV>
 __device__ __forceinline__ key_t64 warp_alternatives(const uint4 (&raw)[NV], float own, const RowVectors<T> &x, uint32_t lane, uint32_t top,
                                                      key_t64 *cand, uint32_t *n_cand)
 {
-    key_t64 mine = 0;
-    if (own > __int_as_float(0xFF800000)) {
-        uint32_t at = 0;
+    const float inf = __int_as_float(0x7f800000);
+    key_t64 least = (key_t64)kth_value(own > -inf ? ordered(own) : 0u, top, lane) << 32;
+    key_t64 best = 0;
+    for (;;) {
+        const float floor = fmaxf(least ? key_value(least) : -inf, LOWEST);  // (an impossible entry is none)
+        if (lane == 0) *n_cand = 0;
+        __syncwarp();
+        if (own >= floor) {
+            constexpr int AT_ONCE = 32 / EPV<T>;  // vectors whose entries are bits of a word
 #pragma unroll
-        for (int j = NV - 1; j >= 0; --j) {
-            float e[EPV<T>];
-            unpack(raw[j], e, T{});
+            for (int j0 = 0; j0 < NV; j0 += AT_ONCE) {
+                uint32_t there = 0;
 #pragma unroll
-            for (int i = EPV<T> - 1; i >= 0; --i)
-                if (e[i] == own) at = x.first(lane + 32 * j) + i;
-        }
-        mine = rank_key(own, at);
-    }
-    const key_t64 least = __shfl_sync(0xffffffffu, first_keys(mine, top, lane), top - 1);
-    const float floor = least ? key_value(least) : __int_as_float(0xFF800000);
-    if (lane == 0) *n_cand = 0;
-    __syncwarp();
-    if (own >= floor) {
+                for (int j = j0; j < NV && j < j0 + AT_ONCE; ++j) {
+                    float e[EPV<T>];
+                    unpack(raw[j], e, T{});
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
-            if (vector_max(raw[j], T{}) >= floor)
-                each_key<T>(raw[j], x.first(lane + 32 * j), least, [&](key_t64 k) {
+                    for (int i = 0; i < EPV<T>; ++i) there |= (uint32_t)(e[i] >= floor) << ((j - j0) * EPV<T> + i);
+                }
+                while (there) {  // one or two
+                    const uint32_t b = __ffs(there) - 1, i = x.first(lane + 32 * (j0 + b / EPV<T>)) + b % EPV<T>;
+                    there &= there - 1;
+                    const key_t64 k = rank_key(to_f32(x.row[i]), i);  // (from L1)
+                    if (k < least) continue;
                     const uint32_t at = atomicAdd(n_cand, 1u);
                     if (at < SHORT_CAND) cand[at] = k;
-                });
-    }
-    __syncwarp();
-    const uint32_t n = *n_cand;
-    key_t64 best = 0;
-    if (n <= 32) {
-        best = first_keys(lane < n ? cand[lane] : 0ull, top, lane);
-    } else if (n <= SHORT_CAND) {
-        best = sort32(cand[lane], lane);
-        for (uint32_t b = 32; b < n; b += 32) best = merge32(best, sort32(b + lane < n ? cand[b + lane] : 0ull, lane), lane);
-    } else {  // one by one
-        key_t64 last = ~0ull;
-        for (uint32_t i = 0; i < top; ++i) {
-            key_t64 b = 0;
-#pragma unroll 1
-            for (int j = 0; j < NV; ++j) {
-                uint4 r = raw[0];
-#pragma unroll
-                for (int l = 1; l < NV; ++l)
-                    if (j == l) r = raw[l];
-                each_key<T>(r, x.first(lane + 32 * j), b, [&](key_t64 k) { if (k < last && k > b) b = k; });
+                }
             }
-            for (int d = 16; d; d >>= 1) b = max(b, __shfl_xor_sync(0xffffffffu, b, d));
-            if (lane == i) best = b;
-            last = b;
         }
+        __syncwarp();
+        const uint32_t n = *n_cand, kept = min(n, SHORT_CAND);
+        if (n <= 32) {  // each to the lane of its rank
+            const key_t64 mine = lane < n ? cand[lane] : 0ull;
+            uint32_t rank = 0;
+            for (uint32_t j = 0; j < n; ++j) rank += cand[j] > mine;
+            if (lane < n) cand[32 + rank] = mine;
+            __syncwarp();
+            best = lane < n ? cand[32 + lane] : 0ull;
+        } else {
+            best = sort32(cand[lane], lane);
+            for (uint32_t b = 32; b < kept; b += 32) best = merge32(best, sort32(b + lane < kept ? cand[b + lane] : 0ull, lane), lane);
+        }
+        __syncwarp();
+        if (n <= SHORT_CAND) return best;
+        least = __shfl_sync(0xffffffffu, best, top - 1);
     }
-    __syncwarp();
-    return best;
 }
 
 template <typename T, bool MASKED, bool TOP, bool ALIGNED, int G, int NV>
