@@ -212,7 +212,7 @@ __device__ __forceinline__ uint4 fetch(const RowVectors<T> &x, const RowMask &ma
 // (bf16, 4,096 rows of 131,072 185 us and 198 with blocks of 512 threads when this was chosen, 180 now: 5.9 TB/s; 1,200 rows of 8,000 12
 // and 22).  592 rows of 1,000,000 take 187 us, 6.3 TB/s: what is left at 131,072 is what a row costs at its end.
 constexpr int LONG_THREADS = 128, LONG_U = 4, LONG_RING = 3, LONG_PARTS = 8;
-constexpr size_t LONG_SMEM = (size_t)LONG_THREADS * LONG_U * LONG_RING * 16;
+constexpr int long_smem(int threads) { return threads * LONG_U * LONG_RING * 16; }
 
 __device__ __forceinline__ void copy_vector(uint32_t to, const uint4 *from)
 {
@@ -275,10 +275,10 @@ __device__ __forceinline__ key_t64 kth_key(const key_t64 *keys, uint32_t n, uint
     return found;
 }
 
-template <typename T, bool MASKED, bool TOP, bool CLUSTER>
-__global__ void __launch_bounds__(LONG_THREADS, 1024 / LONG_THREADS) k_score_long(const LogitRows q, const ScoreOut o, uint32_t log_of_parts)
+template <typename T, bool MASKED, bool TOP, bool CLUSTER, int NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q, const ScoreOut o, uint32_t log_of_parts)
 {
-    constexpr int U = LONG_U, RING = LONG_RING, NT = LONG_THREADS, NW = NT / 32, MAX_PARTS = CLUSTER ? LONG_PARTS : 1;
+    constexpr int U = LONG_U, RING = LONG_RING, NW = NT / 32, MAX_PARTS = CLUSTER ? LONG_PARTS : 1;
     const uint32_t log_parts = CLUSTER ? log_of_parts : 0;
     extern __shared__ uint4 s_ring[];  // [RING][U][NT]
     __shared__ float s_sums[2][MAX_PARTS * NW][3];
@@ -528,11 +528,11 @@ int long_clusters(int device, uint32_t at, const cudaLaunchConfig_t &cfg)
     return n;
 }
 
-template <typename T, bool MASKED, bool TOP, bool CLUSTER>
+template <typename T, bool MASKED, bool TOP, bool CLUSTER, int NT>
 cudaError_t run_long(const LogitRows &q, const ScoreOut &o, uint32_t log_parts, int device, cudaStream_t st)
 {
-    constexpr auto kernel = k_score_long<T, MASKED, TOP, CLUSTER>;
-    const cudaError_t e = allow_smem<kernel, (int)LONG_SMEM>(device);
+    constexpr auto kernel = k_score_long<T, MASKED, TOP, CLUSTER, NT>;
+    const cudaError_t e = allow_smem<kernel, long_smem(NT)>(device);
     if (e != cudaSuccess) return e;
     const uint32_t parts = 1u << log_parts;
     cudaLaunchAttribute at{};
@@ -540,10 +540,10 @@ cudaError_t run_long(const LogitRows &q, const ScoreOut &o, uint32_t log_parts, 
     at.val.clusterDim.x = parts;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(parts); cfg.blockDim = LONG_THREADS; cfg.dynamicSmemBytes = LONG_SMEM; cfg.stream = st;
+    cfg.gridDim = dim3(parts); cfg.blockDim = NT; cfg.dynamicSmemBytes = long_smem(NT); cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = CLUSTER ? 1 : 0;
     const uint64_t most = CLUSTER ? (uint64_t)long_clusters<kernel>(device, log_parts, cfg)
-                                  : (1024 / LONG_THREADS) * (uint64_t)vl_device_sm_count(device);
+                                  : (1024 / NT) * (uint64_t)vl_device_sm_count(device);
     cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
     g_vl_launches.fetch_add(1);
     return cudaLaunchKernelEx(&cfg, kernel, q, o, log_parts);
@@ -563,7 +563,11 @@ cudaError_t launch_long(const LogitRows &q, const ScoreOut &o, int device, cudaS
         while ((1u << log_parts) < LONG_PARTS && q.n_rows << (log_parts + 1) <= (n >> (log_parts + 1) > 2048 ? resident : resident * 2 / 5))
             ++log_parts;
     if (log_parts == 1 && n < 8192) log_parts = 0;
-    return log_parts ? run_long<T, MASKED, TOP, true>(q, o, log_parts, device, st) : run_long<T, MASKED, TOP, false>(q, o, 0, device, st);
+    if (log_parts) return run_long<T, MASKED, TOP, true, LONG_THREADS>(q, o, log_parts, device, st);
+    // half as many warps at a row where it is short and there are rows for all the places: us in blocks of 128 and of 64 threads, bf16: 16,000
+    // rows of 5,000 65.7, 48.7; of 16,000 125, 104; of 32,000 196, 213; 1,200 rows of 9,000 11.1, 10.7; 600 rows 7.1, 7.4
+    if (n <= 2048 && q.n_rows >= resident) return run_long<T, MASKED, TOP, false, LONG_THREADS / 2>(q, o, 0, device, st);
+    return run_long<T, MASKED, TOP, false, LONG_THREADS>(q, o, 0, device, st);
 }
 
 // Short rows: a group of lanes per row, every logit read once into registers.
