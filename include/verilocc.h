@@ -429,7 +429,8 @@ uint64_t vl_policy_work(uint64_t n_candidates, uint64_t n_tokens);
  * ([candidates + 1], ascending, 8-byte aligned; a candidate may have none) of the n_tokens entries of d_logprob, d_old_logprob (NULL: d_logprob
  * itself) and d_ref_logprob (read if kl is not 0).  *d_loss receives the sum of the weighted token losses, d_advantage (or NULL) the candidates'
  * advantages, d_g_logprob [n_tokens] (or NULL) the derivative of the loss to every ln p, 0 for tokens that no candidate owns.
- * A token with a ln p of minus infinity on any side adds nothing to the loss and has derivative 0, though it counts as a token.  d_work: at
+ * A token with a ln p of minus infinity on any side adds nothing to the loss and has derivative 0, though it counts as a token.  Exponentials
+ * above 2^122 count as 2^122.  d_work: at
  * least vl_policy_work bytes of device memory, 16-byte aligned, the call's own until its work is done.  Equal inputs give equal results, bit for bit.
  * Stream-ordered on `cuda_stream` of `device`, no synchronisation, no allocation.  Errors: INVALID_ARG, CUDA.
  */

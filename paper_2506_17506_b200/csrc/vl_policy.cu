@@ -4,11 +4,11 @@
 //   reward = [pass] - pair_cost conflict_pairs - bank_cost bank_conflicts,   A = reward - mean  (/ (std + eps))
 //   d = logprob - old, rho = exp d,  token loss = -min(rho A, clip(rho) A) + kl (exp q - q - 1),  q = ref - logprob
 // The loss rests on small differences (A sums to nothing within a program, rho is near 1): rewards, advantages and sums are held in 64
-// bits, rho - 1 comes from expm1, and on which side of a border of the clip a token lies is decided as in exact arithmetic.
+// bits, rho - 1 comes from a series where it is small, and on which side of a border of the clip a token lies is decided as in exact arithmetic.
 //
 // Three kernels: k_advantages, a cluster or a block per program, leaves each candidate's weight and weighted advantage; k_policy_tokens
 // streams the tokens, which is what bounds it (12 to 16 bytes a token), each warp a run of them, finding candidates by their
-// offsets; k_policy_sum adds the blocks' sums in order.
+// offsets; k_policy_sum adds the blocks' sums in order.  Small losses take one kernel, k_policy_small.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -142,6 +142,9 @@ __device__ __forceinline__ uint64_t first_above(const int64_t *off, uint64_t n, 
     return a;
 }
 
+// No exponential is above 2^122 = 5e36, so that nothing times it, and four of them together, are numbers.
+constexpr float EXP_MOST = 122.0f;
+
 // exp d - 1 and exp d - 1 - d.  Near 0 from the exponential series (|d| < 0.35: its terms from the ninth on are below 2^-26 of the
 // first), elsewhere from the exponential itself, where nothing cancels: within 4 u exp d.
 __device__ __forceinline__ void exp_less(float d, float *m1, float *m2)
@@ -153,7 +156,7 @@ __device__ __forceinline__ void exp_less(float d, float *m1, float *m2)
     p = fmaf(p, d, 1.0f / 24.0f);
     p = fmaf(p, d, 1.0f / 6.0f);
     p = fmaf(p, d, 0.5f);
-    const float near2 = d * d * p, far1 = ex2(d * LOG2E) - 1.0f;
+    const float near2 = d * d * p, far1 = ex2(min_nan(d * LOG2E, EXP_MOST)) - 1.0f;
     const bool near = fabsf(d) < 0.35f;
     *m1 = near ? d + near2 : far1;
     *m2 = near ? near2 : far1 - d;

@@ -119,6 +119,19 @@ def test_equal_rewards_give_no_signal(B, K):
     assert loss.item() == 0.0 and bool((adv == 0).all()) and bool((g == 0).all())
 
 
+def test_ratios_beyond_the_range_of_numbers(B):
+    """They are cut for a positive advantage, large for a negative one, and nothing for none."""
+    import torch
+    v = np.array([[1, -1, 0, 0], [2, 0, 0, 0]])
+    off, lp, old = np.array([0, 2, 4]), np.full(4, -1.0, dtype=np.float32), np.array([-300, -1, -300, -1], dtype=np.float32)
+    outs, o, l, ol = _dev([v], off, lp, old)
+    loss, adv, g = B.vl_policy_loss(outs, o, l, ol)
+    assert adv[0] > 0 and g[0] == 0 and g[2] > 1e34 and bool(torch.isfinite(g).all()) and bool(torch.isfinite(loss))
+    outs, o, l, ol = _dev([v[:1], v[:1]], off, lp, old)       # programs of one sample each
+    loss, adv, g = B.vl_policy_loss(outs, o, l, ol, ref_logprob=l, kl=0.1)
+    assert bool((adv == 0).all()) and bool((g == 0).all()) and loss.item() == 0.0
+
+
 def test_counts_of_32_bits(B):
     rng = np.random.default_rng(4)
     v = _verdicts(rng, 40)
