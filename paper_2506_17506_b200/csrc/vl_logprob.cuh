@@ -88,12 +88,14 @@ __device__ __forceinline__ void warp_join(Sums &a, float m, float c)
     a.s = warp_sum(a.s);
     a.t = warp_sum(a.t);
 }
-// L = ln sum exp(scale (x - m)), and the entropy.
+// L = ln sum exp(scale (x - m)), and the entropy: neither is below 0, whatever rounding makes of it (a ln p is not above 0); minus infinity
+// for no entries.
 __device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *H)
 {
     const float ln_s = logf(a.s);
-    *L = far_out(a.m) ? ln_s : fmaf(LN2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
-    *H = ln_s - LN2 * __fdividef(a.t, a.s);  // (s is between 1/2 and 2^31)
+    const float l = far_out(a.m) ? ln_s : fmaf(LN2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
+    *L = a.s == 0.0f ? ln_s : max_nan(l, 0.0f);
+    *H = max_nan(ln_s - LN2 * __fdividef(a.t, a.s), 0.0f);  // (s is between 1/2 and 2^31)
 }
 
 // The entries of vectors into the sums relative to m.

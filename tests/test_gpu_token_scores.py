@@ -87,10 +87,10 @@ def _check_scores(got, x64, scale, closed, tokens, top):
             assert abs(stats[r, 1] - L) <= S + 2 * U * abs(L), (r, stats[r, 1], L)
         else:
             assert stats[r, 1] == L
-        assert abs(ent[r] - H) <= 3 * S * (1 + H), (r, ent[r], H)
+        assert abs(ent[r] - H) <= 3 * S * (1 + H) and ent[r] >= 0, (r, ent[r], H)
         if tokens is not None:
             if np.isfinite(wlp):
-                assert abs(lp[r] - wlp) <= S + 3 * U * (abs(wlp) + 2 * abs(L)), (r, lp[r], wlp)
+                assert abs(lp[r] - wlp) <= S + 3 * U * (abs(wlp) + 2 * abs(L)) and lp[r] <= 0, (r, lp[r], wlp)
             else:
                 assert lp[r] == wlp
         if top:
