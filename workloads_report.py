@@ -14,6 +14,9 @@ solved, attempts summed and largest, Pass@1/10/100 counts), and the time of the 
 vl_verify_until_pass in batches of 100 rows (it stops after the first batch with a passing row),
 and the times of vl_diagnose and vl_occupied_masks on one row, and vl_verify_dict over the rows of the
 first program in dictionary form (its algorithmic bytes are 2 bytes per dictionary column + the verdict).
+Last, the step from verdicts to a gradient over 20 samples of the first program: vl_token_logprobs over a row of
+random bf16 logits per definition (one entry per register, occupied registers and tuple widths masked),
+vl_policy_loss and vl_token_logprobs_backward, medians of events around each call (host work included where it is longer).
 """
 from __future__ import annotations
 
@@ -167,6 +170,36 @@ def main() -> int:
         edd[1].record(stream)
         torch.cuda.synchronize()
         dict_ms = edd[0].elapsed_time(edd[1]) / args.steps
+        # from the verdicts of 20 samples of the first program to a gradient: a head over its registers, one row of bf16 logits per
+        # definition, under the masks of the first row
+        prog, S = progs[0], min(20, wl.K)
+        instr = np.repeat(np.arange(prog.n_instrs), prog.instr_n_defs)
+        col = np.concatenate([np.arange(o, o + d) for o, d in zip(prog.instr_op_off[:-1], prog.instr_n_defs)]).astype(np.int64)
+        D = len(col)
+        tokens = cands[0][:S].view(torch.int16)[:, torch.from_numpy(col).cuda()].contiguous().view(-1)
+        widths = torch.from_numpy(prog.vreg_width[prog.op_vreg[col]]).cuda().repeat(S)
+        which = torch.from_numpy(instr.astype(np.int32)).cuda().repeat(S)
+        logits = torch.randn(S * D, prog.P, device="cuda", dtype=torch.bfloat16)
+        dlogits = torch.empty_like(logits)
+        tok_off = torch.arange(0, S * D + 1, D, device="cuda")
+        args_ = dict(occupied=masks, mask_rows=which, widths=widths)
+
+        def train():
+            sc = vl.vl_token_logprobs(logits, tokens, **args_)
+            et[1].record(stream)
+            _, _, g = vl.vl_policy_loss([outs[0][:S]], tok_off, sc.logprob, bank_cost=1e-5)
+            et[2].record(stream)
+            vl.vl_token_logprobs_backward(logits, tokens, sc.row_stats, g, out=dlogits, **args_)
+
+        et = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+        parts = []
+        for _ in range(3 + args.steps):
+            et[0].record(stream)
+            train()
+            et[3].record(stream)
+            torch.cuda.synchronize()
+            parts.append([et[j].elapsed_time(et[j + 1]) * 1e3 for j in range(3)])
+        score_us, loss_us, grad_us = (float(np.median([p[j] for p in parts[3:]])) for j in range(3))
         dict_bytes = (2 * d_host.shape[1] + 16) * wl.K
         occupied_us = eo[0].elapsed_time(eo[1]) / args.steps * 1e3
         diagnose_us = ed[0].elapsed_time(ed[1]) / args.steps * 1e3
@@ -192,6 +225,8 @@ def main() -> int:
             "until_pass_first_passing_row": first_pass,
             "diagnose_one_row_us": diagnose_us,
             "occupied_masks_one_row_us": occupied_us,
+            "training_step_20_samples": {"rows": S * D, "registers": int(prog.P), "token_logprobs_us": score_us, "policy_loss_us": loss_us,
+                                         "backward_us": grad_us},
             "dict_form_first_program": {"columns": int(len(layout[1])), "verify_dict_ms": dict_ms,
                                         "verifications_per_sec": wl.K / (dict_ms * 1e-3),
                                         "gb_per_sec": dict_bytes / (dict_ms * 1e-3) / 1e9,
