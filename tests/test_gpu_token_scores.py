@@ -5,7 +5,8 @@ more across threads (the smallest kernel gives a row to one warp), each term bei
 in d = scale (x - M), at most two steps in the exponential): relative error of a sum at most S = (V / 32 + 40 + 2 D) u, where D bounds
 |d| of the terms that matter (a term below exp(-D) V counts as nothing: D = 20 + ln V).  Then |L - exact| <= S + 2 u L, the
 entropy L - T / s is within 3 S (1 + H), and ln p within S + 3 u (|d| + L).  A gradient's p = exp(l) is within (6 + 2 (|d| + L)) u of
-its value relatively, the sum of its two terms within a few u of their size, and the result is rounded once to its type.
+its value relatively, the sum of its two terms within a few u of their size, and the result is rounded once to its type.  A p below
+2^-126, the smallest normal number, counts as 0: what it would be multiplied with, times 2^-126, comes on top.
 """
 import numpy as np
 import pytest
@@ -226,6 +227,31 @@ def test_logits_far_from_zero(B):
     _check_scores(got, x.double().cpu().numpy(), 0.25, np.zeros((4, 5000), bool), t, 4)
 
 
+@pytest.mark.parametrize("scale", [1e-6, 1e-3, 50.0, 1e6])
+def test_scales_at_the_ends_of_their_range(B, scale):
+    import torch
+    rng = np.random.default_rng(9)
+    scale = float(np.float32(scale))
+    for R, V in [(3, 40), (4, 1500), (2, 30011)]:
+        vals = _make(rng, R, V)
+        vals[0, 3] = -np.inf
+        vals[1] = rng.choice([1e30, -1e30, 3e38, -3e38, 2e29], V)      # products with the scale leave the range of numbers
+        x = _rows(vals, "f32")
+        x64, closed, t = x.double().cpu().numpy(), np.zeros((R, V), bool), rng.integers(0, V, R)
+        got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), scale=scale, top=3)
+        real = [r for r in range(R) if r != 1]
+        pick = lambda v: None if v is None else v[real]
+        _check_scores(B.TokenLogprobs(*[pick(v) for v in got]), x64[real], scale, closed[real], t[real], 3)
+        lp, H, M, L, ids, _ = ref.score_row(x64[1], scale, closed[1], int(t[1]), 3)
+        assert got.row_stats[1, 0].item() == np.float32(M) and got.top_ids[1].tolist() == [int(i) for i in ids]
+        assert abs(got.row_stats[1, 1].item() - L) <= _sum_error(V) + 2 * U * L and abs(got.entropy[1].item() - H) <= 3 * _sum_error(V) * (1 + H)
+        stats, H = _oracle_stats(x64, scale, closed, t)
+        g, h = rng.normal(0, 8, R).astype(np.float32), rng.normal(0, 2, R).astype(np.float32)
+        dx = B.vl_token_logprobs_backward(x, torch.from_numpy(t).cuda(), stats, torch.from_numpy(g).cuda(), entropy=H,
+                                          g_entropy=torch.from_numpy(h).cuda(), scale=scale)
+        _check_grad(dx, x64, scale, closed, t, g.astype(float), h.astype(float), "f32")
+
+
 def test_tokens_that_leave_their_row_out(B):
     import torch
     rng = np.random.default_rng(3)
@@ -251,7 +277,8 @@ def _grad_tolerance(x64, scale, closed, token, g, h, dtype):
         tol[token] += 4 * U * abs(g)
     half = {"f32": U, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}[dtype]
     floor = {"f32": 2.0 ** -126, "f16": 2.0 ** -25, "bf16": 2.0 ** -126}[dtype]
-    return want, scale * tol * 1.01 + np.abs(want) * half * 1.01 + floor
+    tiny = 2.0 ** -126 * scale * (abs(g) + abs(h) * (np.abs(l) + H))
+    return want, scale * tol * 1.01 + np.abs(want) * half * 1.01 + floor + tiny
 
 
 def _check_grad(dx, x64, scale, closed, tokens, g, h, dtype):
