@@ -636,11 +636,10 @@ def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None,
         _refuse(where, "logprob: a CUDA vector")
     dev, T, n = logprob.get_device(), logprob.shape[0], len(outs)
     i32 = torch.int32
-    shapes = [o.shape for o in outs]
-    for o, s in zip(outs, shapes):
-        if not (o.get_device() == dev and o.dtype is i32 and len(s) == 2 and s[1] == 4 and o.is_contiguous()):
+    for o in outs:
+        if not (o.get_device() == dev and o.dtype is i32 and o.dim() == 2 and o.size(1) == 4 and o.is_contiguous()):
             _refuse(where, f"outs: contiguous int32 verdicts [samples, 4] on cuda:{dev}")
-    sizes = [s[0] for s in shapes]
+    sizes = [o.size(0) for o in outs]
     N = sum(sizes)
     lp = _vector(logprob, "logprob", where, dev, T, _Torch.f32)
     old = _vector(old_logprob, "old_logprob", where, dev, T, _Torch.f32)
