@@ -468,7 +468,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q,
                 meet();
                 bound = s_bound;
             }
-            waiting = false;
+            // the count has been read: the other half is before the next row, or at the end, where no block may leave while another
+            // one reads its shared memory
+            if (CLUSTER) cluster_arrive();
         } else {
             if (CLUSTER) {
                 cluster_arrive();
