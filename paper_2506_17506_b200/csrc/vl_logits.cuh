@@ -396,8 +396,10 @@ __device__ __forceinline__ RowMask row_mask(const LogitRows &q, uint64_t r)
 template <typename T, int G, int NV, bool ALIGNED>
 __device__ __forceinline__ bool close_row(uint4 (&raw)[NV], const RowVectors<T> &x, const RowMask &mask, uint32_t g, int64_t tok)
 {
-    constexpr int WL = NV * EPV<T> <= 32 ? 1 : NV * EPV<T> / 32;  // words of a lane
+    // words of a lane (rows that are not aligned have no more than one a lane to hand out, short_shape)
+    constexpr int WL = NV * EPV<T> <= 32 ? 1 : (NV * EPV<T> + (ALIGNED ? 31 : 0)) / 32;
     constexpr bool WORDS = ALIGNED || WL == 1;
+    static_assert(!ALIGNED || (NV - 1) * EPV<T> / 32 < WL, "every vector's word is one of the lane's");
     uint32_t word[WL];
     if (WORDS) {
 #pragma unroll

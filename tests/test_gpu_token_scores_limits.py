@@ -2,7 +2,8 @@
 import numpy as np
 import pytest
 
-from tests.test_gpu_token_scores import B, _check_scores, _make, _rows  # noqa: F401 (B is a fixture)
+from tests import score_oracle as ref
+from tests.test_gpu_token_scores import B, _check_scores, _make, _masks, _rows  # noqa: F401 (B is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +29,19 @@ def test_rows_split_over_blocks_again_and_again(B, R, V, kind):
         torch.cuda.synchronize()
         for g in got:
             assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.parametrize("V", [264, 512, 520, 1000, 1024])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_alternatives_of_aligned_rows_under_masks(B, dtype, V):
+    """Rows that start and end on vectors, the whole warp at a row: the last vectors of a lane lie behind the row, and behind its mask."""
+    import torch
+    rng = np.random.default_rng(V)
+    R = 9
+    m, w = _masks(rng, R, V, 0.3), rng.choice([1, 2, 4, 40], R).astype(np.uint8)
+    closed = np.array([ref.closed_entries(V, m[r], w[r]) for r in range(R)])
+    x = _rows(np.where(closed, np.nan, _make(rng, R, V)), dtype)
+    t = rng.integers(0, V, R)
+    got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), occupied=torch.from_numpy(m.view(np.int32)).cuda(),
+                              widths=torch.from_numpy(w).cuda(), top=5)
+    _check_scores(got, x.double().cpu().numpy(), 1.0, closed, t, 5)
