@@ -175,9 +175,10 @@ __device__ __forceinline__ uint4 above(const uint4 &r)
 
 constexpr float LOWEST = -3.402823466e38f;
 constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
-// From here on products of logits with scale log2 e (scale <= 1e6) could leave the range of numbers.
-constexpr float FAR_OUT = 1e29f;
-__device__ __forceinline__ bool far_out(float m) { return !(fabsf(m) < FAR_OUT); }
+// Up to here the rounded product of a logit with scale log2 e is off by at most 1/8 of a power of two.  Beyond it, it may be off by many
+// powers of two (by 440 at 1e10): there differences of logits are multiplied, which costs two instructions an entry for one.
+constexpr float FAR_OUT = 4194304.0f;  // 2^22
+__device__ __forceinline__ bool far_out(float m, float c) { return !(fabsf(__fmul_rn(m, c)) < FAR_OUT); }
 
 // A row as 16-byte vectors: vector v holds the entries first(v) .. first(v) + EPV - 1; the first and the last vector may hold
 // entries of no row, which are read one by one around them.

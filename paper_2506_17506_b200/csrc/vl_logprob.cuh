@@ -57,8 +57,8 @@ __device__ __forceinline__ key_t64 merge32(key_t64 a, key_t64 b, uint32_t lane)
 
 // ---- running sums
 // In powers of two: y_i = c x_i - B with c = scale log2 e and B = c m rounded, m the largest logit so far; s = sum 2^y, t = sum 2^y y.
-// One multiply-add makes y, and B being rounded makes no difference: it is the same B in every term, and what it lacks to c m is put
-// right once, at the end.  Where c x would leave the range of numbers (FAR_OUT), y is (x - m) c.
+// One multiply-add makes y, and B being rounded makes no difference: it is the same B in every term, and what it lacks to c m (little,
+// up to FAR_OUT) is put right once, at the end.  Where c m is larger, y is (x - m) c.
 constexpr float FAR_BELOW = -1e30f;  // stands for minus infinity, whose 2^y y would be none: its power of two is 0 (scale >= 1e-6)
 struct Sums {
     float m, s, t;
@@ -66,7 +66,12 @@ struct Sums {
 // What sums relative to m lack to sums relative to the larger m1, as a power of two.
 __device__ __forceinline__ float step_down(float m, float m1, float c)
 {
-    return fmaxf(far_out(m) ? (m - m1) * c : __fsub_rn(__fmul_rn(m, c), __fmul_rn(m1, c)), FAR_BELOW);
+    const float B = __fmul_rn(m, c), B1 = __fmul_rn(m1, c);
+    const bool far = far_out(m, c), far1 = far_out(m1, c);
+    if (!far && !far1) return __fsub_rn(B, B1);
+    // one of them is relative to c m itself: the other one's B lacks something to it
+    const float lacks = (far ? 0.0f : __fmaf_rn(m, c, -B)) - (far1 ? 0.0f : __fmaf_rn(m1, c, -B1));
+    return fmaxf((m - m1) * c - lacks, FAR_BELOW);
 }
 __device__ __forceinline__ void raise(Sums &a, float m, float c)
 {
@@ -93,7 +98,7 @@ __device__ __forceinline__ void warp_join(Sums &a, float m, float c)
 __device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *H)
 {
     const float ln_s = logf(a.s);
-    const float l = far_out(a.m) ? ln_s : fmaf(LN2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
+    const float l = far_out(a.m, c) ? ln_s : fmaf(LN2, __fmaf_rn(-a.m, c, __fmul_rn(a.m, c)), ln_s);
     *L = a.s == 0.0f ? ln_s : max_nan(l, 0.0f);
     *H = max_nan(ln_s - LN2 * __fdividef(a.t, a.s), 0.0f);  // (s is between 1/2 and 2^31)
 }
@@ -103,7 +108,7 @@ template <typename T, int N>
 __device__ __forceinline__ void add_vectors(const uint4 (&raw)[N], float m, float c, f32x2 &s, f32x2 &t)
 {
     m = m == __int_as_float(0xFF800000) ? 0.0f : m;  // (nothing but impossible entries, whose powers of two are 0 relative to anything)
-    if (!far_out(m)) {
+    if (!far_out(m, c)) {
         const float b = -__fmul_rn(m, c);
         const f32x2 c2 = both(c, c), low = both(b, b);
 #pragma unroll

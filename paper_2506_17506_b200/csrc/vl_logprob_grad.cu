@@ -35,7 +35,7 @@ __device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p,
     if (shut) g = 0.0f;
     w.c = q.scale * LOG2E;
     w.M = st.x;
-    w.far = far_out(st.x);
+    w.far = !(fabsf(st.x) < 1e29f);
     w.L2 = st.y * LOG2E;
     const float B = __fmul_rn(st.x, w.c), K = __fadd_rn(B, w.L2), k = __fsub_rn(K, B);
     // what K lacks: the rounded bits of the sum and of both products

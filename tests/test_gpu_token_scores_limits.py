@@ -45,3 +45,43 @@ def test_alternatives_of_aligned_rows_under_masks(B, dtype, V):
     got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), occupied=torch.from_numpy(m.view(np.int32)).cuda(),
                               widths=torch.from_numpy(w).cuda(), top=5)
     _check_scores(got, x.double().cpu().numpy(), 1.0, closed, t, 5)
+
+
+# (type, logits' middle, their step, scale): products of logits and scale from 2^20 to beyond 2^100, where a product's own rounding
+# is up to many powers of two.  Steps are the type's own at that value, or larger.
+LARGE = [("f32", -1e10, 1024.0, 1.0), ("f32", 1e10, 1024.0, 1.0), ("f32", 1e10, 1024.0, 1e-3), ("f32", -1e10, 1024.0, 1e-3),
+         ("f32", 1e12, 65536.0, 1e-5), ("f32", -1e12, 65536.0, 1e-5), ("f32", 1e20, 2.0 ** 43, 1.0), ("f32", -1e20, 2.0 ** 43, 1e-6),
+         ("f32", 5000.0, 2.0 ** -11, 1e6), ("f32", -5000.0, 2.0 ** -11, 1e3), ("f32", 2907270.4, 0.25, 1.0), ("f32", -2907270.4, 0.25, 1.0),
+         ("f32", -1e9, 64.0, 1.0), ("f32", 9e28, 2.0 ** 73, 1e-6),
+         ("f16", 65504.0, 32.0, 1e5), ("f16", -65504.0, 32.0, 1e5), ("f16", -65504.0, 32.0, 3e5), ("f16", 65504.0, 32.0, 1e6),
+         ("f16", 60000.0, 32.0, 50.0), ("f16", -3000.0, 2.0, 1000.0),
+         ("bf16", 1e10, 2.0 ** 26, 1e-6), ("bf16", -1e10, 2.0 ** 26, 1.0), ("bf16", 1e20, 2.0 ** 59, 1.0), ("bf16", -9e28, 2.0 ** 89, 1e-3)]
+
+
+def _large(rng, R, V, dtype, middle, step):
+    """Values around `middle`, a few dozen steps wide, below the type's largest; one row rises, one holds impossible entries."""
+    k = rng.integers(-24, 25, (R, V)).astype(float)
+    k[0] = np.round(np.linspace(-24, 24, V))
+    x = middle + step * k
+    most = {"f32": 3.4e38, "f16": 65504.0, "bf16": 3.3e38}[dtype]
+    x = np.clip(x, -most, most)
+    if V > 4:
+        x[-1, ::3] = -np.inf
+    return x
+
+
+@pytest.mark.parametrize("dtype,middle,step,scale", LARGE)
+@pytest.mark.parametrize("R,V", [(5, 40), (3, 300), (3, 2041), (3, 9001), (2, 131072), (700, 4200)])
+def test_products_of_logits_and_scale_that_are_large(B, dtype, middle, step, scale, R, V):
+    import torch
+    rng = np.random.default_rng(V)
+    x = _rows(_large(rng, R, V, dtype, middle, step), dtype, pad=V % 3)
+    scale = float(np.float32(scale))
+    t = rng.integers(0, V, R)
+    n = min(R, 4)
+    pick = np.r_[0:n - 1, R - 1]
+    x64 = x[torch.from_numpy(pick).cuda()].double().cpu().numpy()
+    for top in (0, 3):
+        got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), scale=scale, top=top)
+        head = B.TokenLogprobs(*[None if v is None else v[torch.from_numpy(pick).cuda()] for v in got])
+        _check_scores(head, x64, scale, np.zeros((n, V), bool), t[pick], top)
