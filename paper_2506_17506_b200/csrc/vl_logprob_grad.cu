@@ -20,7 +20,7 @@ struct GradIn {
 // What a row's entries have in common.
 struct GradRow {
     float c, K, a, b, at_token;
-    float M, L2;  // for rows far out
+    float M, L2;  // for rows far out, where K would lack whole powers of two
     bool far, dead;
     int tok;
 };
@@ -35,7 +35,7 @@ __device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p,
     if (shut) g = 0.0f;
     w.c = q.scale * LOG2E;
     w.M = st.x;
-    w.far = !(fabsf(st.x) < 1e29f);
+    w.far = far_out(st.x, w.c);
     w.L2 = st.y * LOG2E;
     const float B = __fmul_rn(st.x, w.c), K = __fadd_rn(B, w.L2), k = __fsub_rn(K, B);
     // what K lacks: the rounded bits of the sum and of both products

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from tests import score_oracle as ref
-from tests.test_gpu_token_scores import B, _check_scores, _make, _masks, _rows  # noqa: F401 (B is a fixture)
+from tests.test_gpu_token_scores import B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows  # noqa: F401 (B is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,19 @@ def test_products_of_logits_and_scale_that_are_large(B, dtype, middle, step, sca
         got = B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), scale=scale, top=top)
         head = B.TokenLogprobs(*[None if v is None else v[torch.from_numpy(pick).cuda()] for v in got])
         _check_scores(head, x64, scale, np.zeros((n, V), bool), t[pick], top)
+
+
+@pytest.mark.parametrize("dtype,middle,step,scale", LARGE)
+@pytest.mark.parametrize("R,V", [(5, 40), (3, 300), (3, 9001), (2, 50000)])
+def test_gradients_at_products_that_are_large(B, dtype, middle, step, scale, R, V):
+    import torch
+    rng = np.random.default_rng(V + 1)
+    x = _rows(_large(rng, R, V, dtype, middle, step), dtype, pad=V % 3)
+    x64, closed, t, scale = x.double().cpu().numpy(), np.zeros((R, V), bool), rng.integers(0, V, R), float(np.float32(scale))
+    stats, H = _oracle_stats(x64, scale, closed, t)
+    by = 1e-3 / scale if dtype == "f16" else 1.0          # within the range of halves
+    g, h = (rng.normal(0, 8, R) * by).astype(np.float32), (rng.normal(0, 2, R) * by).astype(np.float32)
+    for ent in (False, True):
+        dx = B.vl_token_logprobs_backward(x, torch.from_numpy(t).cuda(), stats, torch.from_numpy(g).cuda(), entropy=H if ent else None,
+                                          g_entropy=torch.from_numpy(h).cuda() if ent else None, scale=scale)
+        _check_grad(dx, x64, scale, closed, t, g.astype(float), h.astype(float) * ent, dtype)
