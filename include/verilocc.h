@@ -395,8 +395,8 @@ int vl_token_logprobs(int device, const vl_logits *x, float *d_logprob, float *d
 
 /*
  * The gradient of vl_token_logprobs: from d_g_logprob[r] and d_g_entropy[r] (a loss's derivatives to ln p and entropy of row r; NULL: 0)
- * to d_dlogits (the type of the logits, rows out_stride elements apart), which is written whole: 0 where an entry is not open and in
- * rows that are left out or have nothing open.  ln p of a token that is not open is constant and hands nothing on.  d_row_stats, and
+ * to d_dlogits (the type of the logits, rows out_stride elements apart), which is written whole: 0 where an entry is not open (infinite
+ * derivatives, and statistics that are no numbers, make no difference to that) and in rows that are left out or have nothing open.  ln p of a token that is not open is constant and hands nothing on.  d_row_stats, and
  * d_entropy where d_g_entropy is given, are the forward call's outputs for the same descriptor.  d_dlogits may be the logits themselves
  * (with the same stride), and overlaps them in no other way.  Each value is rounded once; a p below 2^-126 counts as 0.  Stream order, errors: as vl_token_logprobs.
  */

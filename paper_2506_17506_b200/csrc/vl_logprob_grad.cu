@@ -20,8 +20,8 @@ struct GradIn {
 // What a row's entries have in common.
 struct GradRow {
     float c, K, a, b, at_token;
-    float M, L2;  // for rows far out, where K would lack whole powers of two
-    bool far, dead;
+    float M;         // for rows far out, where K would lack whole powers of two: it is L log2 e alone there
+    bool far, dead;  // far: or the derivatives are; a, b and at_token are then without the scale, which is multiplied last
     int tok;
 };
 __device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p, uint64_t r, int64_t tok, bool shut)  // shut: the token is closed
@@ -35,47 +35,58 @@ __device__ __forceinline__ GradRow grad_row(const LogitRows &q, const GradIn &p,
     if (shut) g = 0.0f;
     w.c = q.scale * LOG2E;
     w.M = st.x;
-    w.far = far_out(st.x, w.c);
-    w.L2 = st.y * LOG2E;
-    const float B = __fmul_rn(st.x, w.c), K = __fadd_rn(B, w.L2), k = __fsub_rn(K, B);
+    const float L2 = __fmul_rn(st.y, LOG2E), B = __fmul_rn(st.x, w.c), K = __fadd_rn(B, L2), k = __fsub_rn(K, B);
     // what K lacks: the rounded bits of the sum and of both products
-    const float lacks = __fadd_rn(__fsub_rn(B, __fsub_rn(K, k)), __fsub_rn(w.L2, k)) + __fmaf_rn(st.x, w.c, -B) + __fmaf_rn(st.y, LOG2E, -w.L2);
+    const float lacks = __fadd_rn(__fsub_rn(B, __fsub_rn(K, k)), __fsub_rn(L2, k)) + __fmaf_rn(st.x, w.c, -B) + __fmaf_rn(st.y, LOG2E, -L2);
     const float a = -q.scale * fmaf(h, H, g), b = -q.scale * h * LN2;
-    w.K = K;
-    const float f = w.far ? 1.0f : ex2(-lacks);
-    w.a = w.far ? a : f * fmaf(-b, lacks, a);
-    w.b = f * b;
     w.at_token = q.scale * g;
+    // (b times 300, the most that y is, is a number below the limit; what is no number is not below it)
+    w.far = far_out(st.x, w.c) || !(fabsf(K) + fabsf(a) + fabsf(b) + fabsf(w.at_token) < 1e35f);
+    w.K = K;
+    const float f = ex2(-lacks);
+    w.a = f * fmaf(-b, lacks, a);
+    w.b = f * b;
+    if (w.far) {
+        w.K = L2;
+        w.a = -fmaf(h, H, g);
+        w.b = -h * LN2;
+        w.at_token = g;
+    }
     return w;
 }
 
 constexpr float FLOOR = -300.0f;  // 2^-300 is 0, and 0 (a + b y) too
 
-// The gradient of a vector that begins at entry `first`.
+// The gradient of a vector that begins at entry `first`.  An entry of minus infinity (closed, or impossible) has p = 0 whatever the
+// row's numbers are.
 template <typename T>
-__device__ __forceinline__ uint4 grad_vector(const uint4 &raw, int first, const GradRow &w)
+__device__ __forceinline__ uint4 grad_vector(const uint4 &raw, int first, const GradRow &w, float scale)
 {
     float x[EPV<T>], d[EPV<T>];
     unpack(raw, x, T{});
-    const f32x2 c2 = both(w.c, w.c), K2 = both(-w.K, -w.K), a2 = both(w.a, w.a), b2 = both(w.b, w.b);
-#pragma unroll
-    for (int j = 0; j < EPV<T>; j += 2) {
-        float y0, y1;
-        if (!w.far) {
-            apart(fma2(both(x[j], x[j + 1]), c2, K2), y0, y1);
-        } else {
-            y0 = (x[j] - w.M) * w.c - w.L2;
-            y1 = (x[j + 1] - w.M) * w.c - w.L2;
-        }
-        y0 = max_nan(y0, FLOOR);
-        y1 = max_nan(y1, FLOOR);
-        apart(mul2(both(ex2(y0), ex2(y1)), fma2(b2, both(y0, y1), a2)), d[j], d[j + 1]);
-    }
     const uint32_t at = (uint32_t)(w.tok - first);
-    if (at < (uint32_t)EPV<T>) {
+    if (!w.far) {
+        const f32x2 c2 = both(w.c, w.c), K2 = both(-w.K, -w.K), a2 = both(w.a, w.a), b2 = both(w.b, w.b);
 #pragma unroll
-        for (int j = 0; j < EPV<T>; ++j)
-            if ((uint32_t)j == at) d[j] += w.at_token;
+        for (int j = 0; j < EPV<T>; j += 2) {
+            float y0, y1;
+            apart(fma2(both(x[j], x[j + 1]), c2, K2), y0, y1);
+            y0 = max_nan(y0, FLOOR);
+            y1 = max_nan(y1, FLOOR);
+            apart(mul2(both(ex2(y0), ex2(y1)), fma2(b2, both(y0, y1), a2)), d[j], d[j + 1]);
+        }
+        if (at < (uint32_t)EPV<T>) {
+#pragma unroll
+            for (int j = 0; j < EPV<T>; ++j)
+                if ((uint32_t)j == at) d[j] += w.at_token;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < EPV<T>; ++j) {
+            const float y = max_nan((x[j] - w.M) * w.c - w.K, FLOOR);
+            const float v = x[j] == __int_as_float(0xFF800000) ? 0.0f : ex2(y) * fmaf(w.b, y, w.a);
+            d[j] = ((uint32_t)j == at ? v + w.at_token : v) * scale;
+        }
     }
     return pack(d, T{});
 }
@@ -162,7 +173,7 @@ __global__ void __launch_bounds__(NT) k_grad_long(const LogitRows q, const GradI
             const int first = x.first(v);
             if (v < x.n && !whole) raw[u] = x.part(v);
             if (MASKED && v < x.n) close_entries<T>(raw[u], mask.closed_from(first, EPV<T>));
-            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[u], first, w);
+            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[u], first, w, q.scale);
             if (!ALIKE && !alike) store_shifted<T>(dx, x, v, d, lane);
             else if (whole) __stcs(to + v, d);
             else if (v < x.n) store_entries<T>(dx, first, q.V, d);
@@ -198,7 +209,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_grad_sho
         for (int j = 0; j < NV; ++j) {
             const uint32_t v = g + G * j;
             if (v >= x.n) break;
-            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[j], x.first(v), w);
+            const uint4 d = w.dead ? make_uint4(0u, 0u, 0u, 0u) : grad_vector<T>(raw[j], x.first(v), w, q.scale);
             if (alike && (ALIGNED || x.whole(v))) to[G * j] = d;
             else store_entries<T>(dx, x.first(v), q.V, d);
         }

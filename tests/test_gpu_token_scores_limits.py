@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from tests import score_oracle as ref
-from tests.test_gpu_token_scores import B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows  # noqa: F401 (B is a fixture)
+from tests.test_gpu_token_scores import U, B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows  # noqa: F401 (B is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,54 @@ def test_gradients_at_products_that_are_large(B, dtype, middle, step, scale, R, 
         dx = B.vl_token_logprobs_backward(x, torch.from_numpy(t).cuda(), stats, torch.from_numpy(g).cuda(), entropy=H if ent else None,
                                           g_entropy=torch.from_numpy(h).cuda() if ent else None, scale=scale)
         _check_grad(dx, x64, scale, closed, t, g.astype(float), h.astype(float) * ent, dtype)
+
+
+@pytest.mark.parametrize("V", [16, 61, 300, 1500, 9001])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_closed_entries_have_no_gradient_whatever_the_others_hold(B, dtype, V):
+    """Derivatives that overflowed or are no numbers, rows whose open logits hold an infinity or no number, statistics that are no numbers:
+    the gradient of a closed entry is 0."""
+    import torch
+    rng = np.random.default_rng(V)
+    R = 12
+    m = _masks(rng, R, V, 0.4)
+    m[:, 0] = (m[:, 0] | 1) & ~np.uint32(2)
+    closed = np.array([ref.closed_entries(V, m[r]) for r in range(R)])
+    vals = np.where(closed, rng.choice([np.nan, np.inf, -np.inf, 7.0], (R, V)), _make(rng, R, V))
+    vals[0, 1], vals[1, 1] = np.nan, np.inf
+    x = _rows(vals, dtype, pad=V % 2)
+    t = torch.full((R,), 1, device="cuda")
+    occ = torch.from_numpy(m.view(np.int32)).cuda()
+    fwd = B.vl_token_logprobs(x, t, occupied=occ)
+    stats, ent = fwd.row_stats.clone(), fwd.entropy.clone()
+    stats[2, 1], stats[3, 0], stats[4] = float("nan"), float("nan"), float("inf")
+    g, h = torch.ones(R, device="cuda"), torch.ones(R, device="cuda")
+    g[5], g[6], h[7], h[8], g[9] = float("inf"), float("nan"), float("inf"), float("nan"), -float("inf")
+    ent[10] = float("nan")
+    for out in (None, x.clone()):
+        for more in (dict(), dict(entropy=ent, g_entropy=h)):
+            if out is not None:
+                out.copy_(x)
+            dx = B.vl_token_logprobs_backward(x if out is None else out, t, stats, g, occupied=occ, out=out, **more).float().cpu().numpy()
+            assert np.all(dx[closed] == 0)
+            assert not any(np.all(np.isfinite(dx[r])) for r in (0, 1, 5, 6, 9)) and np.all(np.isfinite(dx[11]))
+
+
+@pytest.mark.parametrize("V", [40, 1500, 9001])
+def test_derivatives_that_overflow_with_the_scale(B, V):
+    """scale g is beyond the range of numbers: what p = 0 leaves of it is 0, and small p leave numbers."""
+    import torch
+    rng = np.random.default_rng(V)
+    vals = np.full((2, V), -8e-5)
+    vals[:, ::4] = -1.0           # exp(-1e6) = 0
+    vals[0, 1] = 0.0
+    x = _rows(vals, "f32")
+    x64, closed, t, scale = x.double().cpu().numpy(), np.zeros((2, V), bool), np.array([1, 2]), 1e6
+    stats, H = _oracle_stats(x64, scale, closed, t)
+    g = np.array([1e33, -1e33], dtype=np.float32)
+    dx = B.vl_token_logprobs_backward(x, torch.from_numpy(t).cuda(), stats, torch.from_numpy(g).cuda(), scale=scale).double().cpu().numpy()
+    assert np.all(dx[:, ::4] == 0) and not np.any(np.isnan(dx))
+    want = ref.grad_row(x64[0], scale, closed[0], 1, float(g[0]), 0.0)
+    ok = (np.abs(want) < 1e38) & (want != 0)
+    # p = exp(-80): (12 + 4 (80 + 1)) u and a few roundings
+    assert np.count_nonzero(ok) and np.all(np.abs(dx[0][ok] - want[ok]) <= 500 * U * np.abs(want[ok]))
