@@ -410,7 +410,9 @@ int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_ro
  * advantage A is the reward less the mean over the samples of its program, with `normalise` divided by their standard deviation (of the
  * population) + eps.  Per token of a candidate, with r = exp(logprob - old): the loss -min(r A, clip(r, 1 - clip_lo, 1 + clip_hi) A), plus
  * kl (exp q - q - 1) with q = ref - logprob.  The token weighs 1 / (candidates * tokens of its candidate), or with `per_token`
- * 1 / tokens of all.  The advantage is a constant of the derivative.
+ * 1 / tokens of all.  The advantage is a constant of the derivative.  Rewards, advantages, weights and sums are held in 64 bits; a token's
+ * ratio in 32: with d = logprob - old its part of the derivative is within (6 + 3 |d|) 2^-24 of its value, that of kl likewise within
+ * (6 + 3 |q|) 2^-24 kl w (1 + exp q).
  */
 typedef struct {
     double pair_cost, bank_cost;

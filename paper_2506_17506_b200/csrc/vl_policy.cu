@@ -3,8 +3,10 @@
 //
 //   reward = [pass] - pair_cost conflict_pairs - bank_cost bank_conflicts,   A = reward - mean  (/ (std + eps))
 //   d = logprob - old, rho = exp d,  token loss = -min(rho A, clip(rho) A) + kl (exp q - q - 1),  q = ref - logprob
-// The loss rests on small differences (A sums to nothing within a program, rho is near 1): rewards, advantages and sums are held in 64
-// bits, rho - 1 comes from a series where it is small, and on which side of a border of the clip a token lies is decided as in exact arithmetic.
+// The loss rests on small differences (A sums to nothing within a program, rho is near 1): rewards, advantages and weights are worked out
+// in 64 bits, rho - 1 comes from a series where it is small, and on which side of a border of the clip a token lies is decided as in exact
+// arithmetic.  A token's difference, exponential and derivative are in 32 bits, the type they are given and wanted in; so are sums of up to four
+// tokens' terms, less 1 where these are near 1, and all sums beyond that are in 64.
 //
 // Three kernels: k_advantages, a cluster or a block per program, leaves each candidate's weight and weighted advantage; k_policy_tokens
 // streams the tokens, which is what bounds it (12 to 16 bytes a token), each warp a run of them, finding candidates by their
@@ -145,9 +147,15 @@ __device__ __forceinline__ uint64_t first_above(const int64_t *off, uint64_t n, 
 // No exponential is above 2^122 = 5e36, so that nothing times it, and four of them together, are numbers.
 constexpr float EXP_MOST = 122.0f;
 
-// exp d - 1 and exp d - 1 - d.  Near 0 from the exponential series (|d| < 0.35: its terms from the ninth on are below 2^-26 of the
-// first), elsewhere from the exponential itself, where nothing cancels: within 4 u exp d.
-__device__ __forceinline__ void exp_less(float d, float *m1, float *m2)
+// exp d, as such where |d| >= 0.35, or less 1 near 0, where the rest would have lost the digits of the difference; and exp d - 1 - d.
+// Near 0 from the exponential series (its terms from the ninth on are below 2^-26 of the first), elsewhere from the exponential
+// itself: within (5 + 2 |d|) u of its value, u = 2^-24 (its argument is rounded twice), and of 1 more in the difference.
+struct Exp {
+    float value, less;
+    bool near;  // value is exp d - 1
+    __device__ __forceinline__ float minus_1() const { return near ? value : value - 1.0f; }
+};
+__device__ __forceinline__ Exp exp_of(float d)
 {
     float p = 1.0f / 40320.0f;
     p = fmaf(p, d, 1.0f / 5040.0f);
@@ -156,15 +164,14 @@ __device__ __forceinline__ void exp_less(float d, float *m1, float *m2)
     p = fmaf(p, d, 1.0f / 24.0f);
     p = fmaf(p, d, 1.0f / 6.0f);
     p = fmaf(p, d, 0.5f);
-    const float near2 = d * d * p, far1 = ex2(min_nan(d * LOG2E, EXP_MOST)) - 1.0f;
+    const float less = d * d * p, far = ex2(min_nan(d * LOG2E, EXP_MOST));
     const bool near = fabsf(d) < 0.35f;
-    *m1 = near ? d + near2 : far1;
-    *m2 = near ? near2 : far1 - d;
+    return {near ? d + less : far, near ? less : (far - 1.0f) - d, near};
 }
 
 // What tokens add to the loss of their candidate, of weight w and w times advantage wA: -wA (in + n_in + n_cut border) + kl w sum.
 struct Part {
-    float in, kl;  // sums of rho - 1 of the tokens that are not clipped, and of exp q - q - 1
+    float in, kl;  // sums over the tokens that are not clipped, of rho - 1 where it is near 1 (n_in of them) and of rho; and of exp q - q - 1
     int n_in, n_cut;
 };
 struct Weight {
@@ -187,17 +194,16 @@ __device__ __forceinline__ float token(const TokenParams &q, float lp, float old
         const float back = __fsub_rn(d, lp), lost = __fsub_rn(__fsub_rn(lp, __fsub_rn(d, back)), __fadd_rn(old, back));
         cut = w.up ? lost > q.hi_rest : lost < q.lo_rest;
     }
-    float m, m2;
-    exp_less(d, &m, &m2);
+    const Exp r = exp_of(d);
     const bool in = counts && !cut;
-    p.in += in ? m : 0.0f;
-    p.n_in += in;
+    p.in += in ? r.value : 0.0f;
+    p.n_in += in && r.near;
     p.n_cut += counts && cut;
-    float g = in ? -fmaf(w.wA32, m, w.wA32) : 0.0f;
+    float g = in ? -fmaf(w.wA32, r.value, r.near ? w.wA32 : 0.0f) : 0.0f;  // (a small rho keeps its digits)
     if (REF) {
-        exp_less(__fsub_rn(ref, lp), &m, &m2);
-        p.kl += counts ? m2 : 0.0f;
-        g = counts ? fmaf(-w.wk32, m, g) : 0.0f;
+        const Exp k = exp_of(__fsub_rn(ref, lp));
+        p.kl += counts ? k.less : 0.0f;
+        g = counts ? fmaf(-w.wk32, k.minus_1(), g) : 0.0f;
     }
     return g;
 }
