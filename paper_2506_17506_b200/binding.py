@@ -367,9 +367,10 @@ class Program:
         """uint8 numpy array [n_instrs, P]: registers the definitions of every instruction must keep off,
         for one candidate (CUDA uint16 tensor; entries >= P mean "no register yet").  With ``words`` the masks as they
         are on the device, a CUDA int32 tensor [n_instrs, ceil(P / 32)] (what vl_token_logprobs takes), without waiting."""
-        import torch
+        torch = _Torch.torch or _Torch.load()
         W = (P + 31) // 32
-        masks = torch.empty((max(self.n_instrs, 1), W), dtype=torch.int32, device=row.device)
+        with contextlib.nullcontext() if stream is None else _on(stream, row.get_device())[1]:     # the memory is the stream's
+            masks = torch.empty((max(self.n_instrs, 1), W), dtype=torch.int32, device=row.device)
         self._check(_lib.vl_occupied_masks(self._h, row.data_ptr(), masks.data_ptr(), _stream_ptr(stream)),
                     "vl_occupied_masks")
         if words:

@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from paper_2506_17506_b200 import synth
 from tests import score_oracle as ref
 from tests.test_gpu_token_scores import U, B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows  # noqa: F401 (B is a fixture)
 
@@ -152,3 +153,34 @@ def test_derivatives_that_overflow_with_the_scale(B, V):
     ok = (np.abs(want) < 1e38) & (want != 0)
     # p = exp(-80): (12 + 4 (80 + 1)) u and a few roundings
     assert np.count_nonzero(ok) and np.all(np.abs(dx[0][ok] - want[ok]) <= 500 * U * np.abs(want[ok]))
+
+
+def test_masks_on_a_side_stream_belong_to_it(B):
+    """Masks that stay on the device: memory that the current stream frees, or takes while a side stream still works with them, is another's."""
+    import torch
+    prog = synth.build_program(synth.shape_tiny(), 0)
+    rows, _ = synth.candidate_rows(prog, 2, 0.4, 3)
+    gp = B.Program(prog)
+    gp.vl_liveness()
+    row = torch.from_numpy(rows.view(np.int16)).cuda().view(torch.uint16)[0]
+    want = gp.vl_occupied_masks(row, prog.P, words=True)
+    x = torch.randn(want.shape[0], prog.P, device="cuda")
+    scores = B.vl_token_logprobs(x, occupied=want, top=4)
+    nbytes = want.numel() * 4
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for number in (False, True):
+        st = side.cuda_stream if number else side
+        for cycles in (0, 400_000_000, 400_000_000):      # first without a delay: memory and kernels are there from then on
+            masks = gp.vl_occupied_masks(row, prog.P, stream=st, words=True)
+            if cycles:
+                with torch.cuda.stream(side):
+                    torch.cuda._sleep(cycles)
+            got = B.vl_token_logprobs(x, occupied=masks, top=4, stream=st)
+            del masks
+            others = [torch.full((nbytes // 4,), -1, dtype=torch.int32, device="cuda") for _ in range(3000)]
+            assert not cycles or not side.query()          # they were written before the side stream began
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, scores) if a is not None)
+            del others, got
+    gp.close()
