@@ -577,12 +577,23 @@ def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths
                          out[3].view(torch.int32).view(R, top) if top else None, out[4].view(R, top) if top else None)
 
 
+def _row_by_row(out, logits, R: int, V: int, apart: int) -> bool:
+    """Whether a matrix is the logits themselves, or shares no entry with them (rows of both may lie in turn)."""
+    size, a, b = logits.element_size(), logits.data_ptr(), out.data_ptr()
+    if R == 1:
+        return a == b or abs(a - b) >= V * size
+    pitch, other = logits.stride(0) * size, apart * size
+    if b >= a + (R - 1) * pitch + V * size or a >= b + (R - 1) * other + V * size:
+        return True
+    return pitch == other and (a == b or V * size <= (b - a) % pitch <= pitch - V * size)
+
+
 def vl_token_logprobs_backward(logits, tokens, row_stats, g_logprob=None, entropy=None, g_entropy=None, occupied=None, mask_rows=None,
                                widths=None, scale: float = 1.0, out=None, stream=None):
     """Gradient to the logits of a loss whose derivatives to the log probabilities and entropies of ``vl_token_logprobs`` are
     ``g_logprob`` and ``g_entropy`` (contiguous float32 [rows]).  ``row_stats`` and ``entropy`` come from that call, the other
-    arguments are the ones it had.  ``out``: where to (the logits themselves, or a matrix of their shape and type that does not
-    overlap them); a new matrix without it."""
+    arguments are the ones it had.  ``out``: where to (the logits themselves, or a matrix of their shape and type that has no entry
+    in common with them); a new matrix without it."""
     where = "vl_token_logprobs_backward"
     x, R, V, dev = _logit_rows(where, logits, tokens, occupied, mask_rows, widths, scale)
     torch = _Torch.torch
@@ -610,14 +621,8 @@ def vl_token_logprobs_backward(logits, tokens, row_stats, g_logprob=None, entrop
         if not (out.get_device() == dev and out.dtype == logits.dtype and out.shape == logits.shape and (V == 1 or out.stride(1) == 1) and
                 apart >= V):
             _refuse(where, "out: a matrix of the logits' shape and type, entries of a row side by side")
-        if out.data_ptr() == logits.data_ptr():
-            if R > 1 and apart != logits.stride(0):
-                _refuse(where, "out: the logits themselves have the logits' stride")
-        elif R:
-            size = logits.element_size()
-            ends = [t.data_ptr() + ((R - 1) * (t.stride(0) if R > 1 else 0) + V) * size for t in (logits, out)]
-            if out.data_ptr() < ends[0] and logits.data_ptr() < ends[1]:
-                _refuse(where, "out: overlaps the logits")
+        if R and not _row_by_row(out, logits, R, V, apart):
+            _refuse(where, "out: the logits themselves (with their stride), or entries of its own")
     rc = _lib.vl_token_logprobs_backward(dev, x, row_stats.data_ptr(), ent, g, h, out.data_ptr(), apart, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)

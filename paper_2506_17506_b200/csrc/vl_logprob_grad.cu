@@ -15,6 +15,7 @@ struct GradIn {
     const float *stats, *entropy, *g, *h;
     void *dx;
     uint64_t stride;
+    int mixed;  // memory between the logits' rows is the gradient's: in place, or rows of both in turn
 };
 
 // What a row's entries have in common.
@@ -187,7 +188,6 @@ constexpr uint32_t SHORT_WARPS = 8;
 template <typename T, bool MASKED, bool ALIGNED, int G, int NV>
 __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_grad_short(const LogitRows q, const GradIn p)
 {
-    const bool in_place = p.dx == q.x;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
     const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
     for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
@@ -195,7 +195,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_grad_sho
         const uint64_t r = there ? r0 + lane / G : q.n_rows - 1;
         const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
         uint4 raw[NV];
-        if (there) fetch_row<T, G, NV, ALIGNED>(raw, x, g, !in_place && r != 0 && r != q.n_rows - 1);
+        if (there) fetch_row<T, G, NV, ALIGNED>(raw, x, g, !p.mixed && r != 0 && r != q.n_rows - 1);
         const RowMask mask = row_mask(q, r);
         const int64_t tok = row_token(q, r);
         bool shut = false;
@@ -264,11 +264,20 @@ extern "C" int vl_token_logprobs_backward(int device, const vl_logits *x, const 
     if (q.n_rows > 1 && out_stride < q.V) return VL_ERR_INVALID_ARG;
     if (out_stride > (1ull << 40) || (q.n_rows > 1 && out_stride > (1ull << 56) / q.n_rows)) return VL_ERR_INVALID_ARG;
     if (q.n_rows && (!d_row_stats || !d_dlogits || (uintptr_t)d_dlogits % (x->dtype == VL_F32 ? 4 : 2))) return VL_ERR_INVALID_ARG;
-    if (d_dlogits == x->logits && q.n_rows > 1 && out_stride != q.stride) return VL_ERR_INVALID_ARG;
     if (q.n_rows == 0) return VL_OK;
+    // Where the matrices' memory meets, they are the same rows, or rows of both in turn that have nothing in common.
+    const uint64_t size = x->dtype == VL_F32 ? 4 : 2, row = q.V * size, pitch = q.stride * size;
+    const uintptr_t from = (uintptr_t)x->logits, to = (uintptr_t)d_dlogits;
+    const bool meet = to < from + (q.n_rows - 1) * pitch + row && from < to + (q.n_rows - 1) * out_stride * size + row;
+    if (meet && q.n_rows > 1) {
+        const uint64_t behind = to >= from ? (to - from) % pitch : (pitch - (from - to) % pitch) % pitch;
+        if (out_stride != q.stride || (to != from && (behind < row || behind > pitch - row))) return VL_ERR_INVALID_ARG;
+    } else if (meet && to != from) {
+        return VL_ERR_INVALID_ARG;
+    }
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
-    const GradIn p{d_row_stats, d_entropy, d_g_logprob, d_g_entropy, d_dlogits, out_stride};
+    const GradIn p{d_row_stats, d_entropy, d_g_logprob, d_g_entropy, d_dlogits, out_stride, meet};
     cudaStream_t st = (cudaStream_t)stream;
     const bool masked = q.occupied || q.widths;
     cudaError_t e;

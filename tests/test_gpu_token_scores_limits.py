@@ -4,7 +4,7 @@ import pytest
 
 from paper_2506_17506_b200 import synth
 from tests import score_oracle as ref
-from tests.test_gpu_token_scores import U, B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows  # noqa: F401 (B is a fixture)
+from tests.test_gpu_token_scores import U, B, _check_grad, _check_scores, _make, _masks, _oracle_stats, _rows, _type  # noqa: F401 (B is a fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -184,3 +184,28 @@ def test_masks_on_a_side_stream_belong_to_it(B):
             assert all(torch.equal(a, b) for a, b in zip(got, scores) if a is not None)
             del others, got
     gp.close()
+
+
+def test_rows_of_logits_and_gradient_in_turn(B):
+    """Both are columns of one matrix; what is neither's is left as it was, and columns in common are refused."""
+    import torch
+    rng = np.random.default_rng(3)
+    for dtype in ("f32", "bf16"):
+        for R, V in [(5, 24), (70, 37), (1, 50), (4, 1001), (3, 9003)]:
+            big = torch.full((R, 2 * V + 3), float("nan"), dtype=_type(dtype), device="cuda")
+            for a, b in ((0, V), (V + 3, 0), (1, V + 2)):
+                x, out = big[:, a:a + V], big[:, b:b + V]
+                big.fill_(float("nan"))
+                x.copy_(torch.from_numpy(_make(rng, R, V)))
+                keep = x.clone()
+                t = torch.from_numpy(rng.integers(0, V, R)).cuda()
+                f = B.vl_token_logprobs(keep, t)
+                g = torch.ones(R, device="cuda")
+                want = B.vl_token_logprobs_backward(keep, t, f.row_stats, g)
+                got = B.vl_token_logprobs_backward(x, t, f.row_stats, g, out=out)
+                rest = torch.ones(2 * V + 3, dtype=torch.bool, device="cuda")
+                rest[a:a + V] = rest[b:b + V] = False
+                assert torch.equal(got, want) and torch.equal(x, keep) and bool(torch.isnan(big[:, rest]).all())
+            for a, b in ((0, V - 1), (3, 0)):
+                with pytest.raises(B.VlError):
+                    B.vl_token_logprobs_backward(big[:, a:a + V], t, f.row_stats, g, out=big[:, b:b + V])
