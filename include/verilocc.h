@@ -415,10 +415,10 @@ int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_ro
  * (6 + 3 |q|) 2^-24 kl w (1 + exp q).
  */
 typedef struct {
-    double pair_cost, bank_cost;
-    double eps;                 /* above 0 with normalise */
+    double pair_cost, bank_cost; /* -1e20 to 1e20 */
+    double eps;                 /* at least 1e-100 with normalise */
     double clip_lo, clip_hi;    /* at least 0; clip_lo >= 1 or an infinite clip_hi: that side is not clipped */
-    double kl;                  /* 0: no reference model */
+    double kl;                  /* -1e30 to 1e30; 0: no reference model */
     int normalise, per_token;
 } vl_policy_rules;
 

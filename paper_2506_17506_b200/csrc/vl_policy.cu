@@ -411,9 +411,10 @@ extern "C" int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d
     if (((uintptr_t)d_logprob | (uintptr_t)d_old_logprob | (uintptr_t)d_ref_logprob | (uintptr_t)d_loss | (uintptr_t)d_advantage |
          (uintptr_t)d_g_logprob) & 3)
         return VL_ERR_INVALID_ARG;
-    if (!(isfinite(rules->pair_cost) && isfinite(rules->bank_cost) && isfinite(rules->kl))) return VL_ERR_INVALID_ARG;
+    // (so that squares of rewards, a weight in 32 bits and what it is multiplied with are numbers)
+    if (!(fabs(rules->pair_cost) <= 1e20 && fabs(rules->bank_cost) <= 1e20 && fabs(rules->kl) <= 1e30)) return VL_ERR_INVALID_ARG;
     if (!(rules->clip_lo >= 0.0 && rules->clip_hi >= 0.0) || (rules->kl != 0.0 && n_tokens && !d_ref_logprob)) return VL_ERR_INVALID_ARG;
-    if (rules->normalise && !(rules->eps > 0.0 && isfinite(rules->eps))) return VL_ERR_INVALID_ARG;
+    if (rules->normalise && !(rules->eps >= 1e-100 && isfinite(rules->eps))) return VL_ERR_INVALID_ARG;
     if (n_tokens > (1ull << 40)) return VL_ERR_INVALID_ARG;
     uint64_t N = 0;
     for (uint32_t j = 0; j < n; ++j) {

@@ -34,3 +34,23 @@ def test_small_ratios_keep_their_digits(B, N, n, span):
         bad = np.flatnonzero(~(np.abs(g.double().cpu().numpy() - want) <= (6 + 3 * d) * U * np.abs(want)))
         assert len(bad) == 0, (d[bad[:5]], g[bad[:5].tolist()], want[bad[:5]])
         assert abs(float(loss) - want_loss) <= ((6 + 3 * d) * U * np.abs(want)).sum() + 4 * U * abs(want_loss)
+
+
+@pytest.mark.parametrize("kw", [dict(eps=1e-100), dict(eps=1e-100, pair_cost=1e-200), dict(pair_cost=1e20, bank_cost=-1e20), dict(pair_cost=1e20, normalise=False),
+                                dict(eps=1e300)], ids=str)
+def test_rules_at_the_ends_of_their_range(B, kw):
+    """Equal rewards leave exactly nothing, others what the formula says, in numbers.  (Below 2^-126 a 32-bit number is a multiple of 2^-149: a
+    rounding there, of an advantage, of a weight or of its product, is off by up to 2^-150 whatever the value.)"""
+    import torch
+    v = np.array([[1, -1, 0, 0]] * 5 + [[8, 3, 7, 13]] * 5)
+    off, lp = np.arange(11) * 3, np.full(30, -1.0, dtype=np.float32)
+    lp[::2] = -1.125
+    old = np.full(30, -1.0, dtype=np.float32)
+    outs, o, l, ol = _dev([v[:5], v[5:]], off, lp, old)
+    loss, adv, g = B.vl_policy_loss(outs, o, l, ol, ref_logprob=ol, kl=1e30, **kw)
+    assert bool((adv == 0).all()) and bool((g[1::2] == 0).all()) and bool(torch.isfinite(g).all()) and bool(torch.isfinite(loss))
+    outs, o, l, ol = _dev([v], off, lp, old)
+    loss, adv, g = B.vl_policy_loss(outs, o, l, ol, **kw)
+    want_loss, want_adv, want, _ = ref.policy([v], off, lp.astype(float), old.astype(float), **kw)
+    assert np.all(np.abs(adv.double().cpu().numpy() - want_adv) <= 2 * U * np.abs(want_adv) + 2.0 ** -150)
+    assert np.all(np.abs(g.double().cpu().numpy() - want) <= (6 + 3 * 0.125) * U * np.abs(want) + 2.0 ** -148) and bool(torch.isfinite(loss))
