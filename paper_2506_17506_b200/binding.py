@@ -369,7 +369,7 @@ class Program:
         are on the device, a CUDA int32 tensor [n_instrs, ceil(P / 32)] (what vl_token_logprobs takes), without waiting."""
         torch = _Torch.torch or _Torch.load()
         W = (P + 31) // 32
-        with contextlib.nullcontext() if stream is None else _on(stream, row.get_device())[1]:     # the memory is the stream's
+        with _HERE if stream is None else _on(stream, row.get_device())[1]:     # the memory is the stream's
             masks = torch.empty((max(self.n_instrs, 1), W), dtype=torch.int32, device=row.device)
         self._check(_lib.vl_occupied_masks(self._h, row.data_ptr(), masks.data_ptr(), _stream_ptr(stream)),
                     "vl_occupied_masks")
@@ -469,6 +469,7 @@ def vl_resample_stats(outs, ks=(1, 10, 100), device: int = 0, stream=None):
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy row_stats top_ids top_logprobs")
 _LOGITS = struct.Struct("@PiQIQPIPQPPf0P")     # vl_logits
 _RULES = struct.Struct("@6d2i")                # vl_policy_rules
+_HERE = contextlib.nullcontext()
 
 
 class _Torch:
@@ -559,22 +560,22 @@ def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths
     torch = _Torch.torch
     if not 0 <= top <= VL_MAX_ALTERNATIVES:
         _refuse(where, f"top: at most {VL_MAX_ALTERNATIVES} alternatives")
-    sizes = [2 * R, R, R] + [R * top, R * top] * (top > 0)      # one allocation
+    scope = None
     if stream is None:
         ptr = _Torch.current(dev)
-        f = torch.empty(sum(sizes), dtype=torch.float32, device=logits.device)
     else:
         ptr, scope = _on(stream, dev)
-        with scope:
-            f = torch.empty(sum(sizes), dtype=torch.float32, device=logits.device)
-    at = f.data_ptr()
-    rc = _lib.vl_token_logprobs(dev, x, at + 12 * R if tokens is not None else 0, at + 8 * R, at, top, at + 16 * R if top else 0,
-                                at + (16 + 4 * top) * R if top else 0, ptr)
+    with scope or _HERE:        # memory of their own: what is kept keeps nothing else
+        stats = logits.new_empty((R, 2), dtype=torch.float32)
+        ent = stats.new_empty(R)
+        lp = stats.new_empty(R) if tokens is not None else None
+        ids = stats.new_empty((R, top), dtype=torch.int32) if top else None
+        lps = stats.new_empty((R, top)) if top else None
+    rc = _lib.vl_token_logprobs(dev, x, lp.data_ptr() if lp is not None else 0, ent.data_ptr(), stats.data_ptr(), top,
+                                ids.data_ptr() if top else 0, lps.data_ptr() if top else 0, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
-    out = f.split_with_sizes(sizes)
-    return TokenLogprobs(out[2] if tokens is not None else None, out[1], out[0].view(R, 2),
-                         out[3].view(torch.int32).view(R, top) if top else None, out[4].view(R, top) if top else None)
+    return TokenLogprobs(lp, ent, stats, ids, lps)
 
 
 def _row_by_row(out, logits, R: int, V: int, apart: int) -> bool:
@@ -613,7 +614,7 @@ def vl_token_logprobs_backward(logits, tokens, row_stats, g_logprob=None, entrop
     else:
         ptr, scope = _on(stream, dev)
     if out is None:
-        with scope or contextlib.nullcontext():
+        with scope or _HERE:
             out = torch.empty((R, V), dtype=logits.dtype, device=logits.device)
         apart = V
     else:
@@ -651,23 +652,20 @@ def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None,
     old = _vector(old_logprob, "old_logprob", where, dev, T, _Torch.f32)
     ref = _vector(ref_logprob, "ref_logprob", where, dev, T, _Torch.f32)
     off = _vector(token_off, "token_off", where, dev, N + 1, _Torch.i64)
-    work = (int(_lib.vl_policy_work(N, T)) + 15) // 16 * 16
-    size = work + 4 * (T + N + 1)                       # working memory, then the results: the derivative on 16 bytes
+    size = int(_lib.vl_policy_work(N, T))
+    scope = None
     if stream is None:
         ptr = _Torch.current(dev)
-        f = torch.empty(size // 4, dtype=torch.float32, device=logprob.device)
     else:
         ptr, scope = _on(stream, dev)
-        with scope:
-            f = torch.empty(size // 4, dtype=torch.float32, device=logprob.device)
-    at = f.data_ptr()
+    with scope or _HERE:        # memory of their own: what is kept keeps nothing else
+        loss, adv, g, work = logprob.new_empty(()), logprob.new_empty(N), logprob.new_empty(T), logprob.new_empty((size + 3) // 4)
     rc = _lib.vl_policy_loss(dev, n, struct.pack(f"{n}P", *[o.data_ptr() for o in outs]), struct.pack(f"{n}Q", *sizes), off, T, lp, old, ref,
                              _RULES.pack(pair_cost, bank_cost, eps, clip_lo, clip_hi, kl, bool(normalise), bool(per_token)),
-                             at + work + 4 * (T + N), at + work + 4 * T, at + work, at, work, ptr)
+                             loss.data_ptr(), adv.data_ptr(), g.data_ptr(), work.data_ptr(), size, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
-    _, g, adv, loss = f.split_with_sizes([work // 4, T, N, 1])
-    return loss[0], adv, g
+    return loss, adv, g
 
 
 def verdicts_to_numpy(t) -> np.ndarray:

@@ -209,3 +209,18 @@ def test_rows_of_logits_and_gradient_in_turn(B):
             for a, b in ((0, V - 1), (3, 0)):
                 with pytest.raises(B.VlError):
                     B.vl_token_logprobs_backward(big[:, a:a + V], t, f.row_stats, g, out=big[:, b:b + V])
+
+
+@pytest.mark.parametrize("side", [False, True])
+def test_results_that_are_kept_keep_nothing_else(B, side):
+    """A log of losses or log probabilities holds what it shows, not the calls' other results and working memory."""
+    import torch
+    stream = torch.cuda.Stream() if side else None
+    x, t = torch.randn(5000, 64, device="cuda"), torch.zeros(5000, dtype=torch.int64, device="cuda")
+    v, off = torch.zeros(1000, 4, dtype=torch.int32, device="cuda"), torch.arange(0, 5001, 5, device="cuda")
+    torch.cuda.synchronize()
+    o = B.vl_token_logprobs(x, t, top=16, stream=stream)
+    torch.cuda.synchronize()
+    for r in list(o) + list(B.vl_policy_loss([v], off, o.logprob, stream=stream)):
+        assert r.untyped_storage().nbytes() == r.numel() * r.element_size()
+    torch.cuda.synchronize()
