@@ -54,3 +54,44 @@ def test_rules_at_the_ends_of_their_range(B, kw):
     want_loss, want_adv, want, _ = ref.policy([v], off, lp.astype(float), old.astype(float), **kw)
     assert np.all(np.abs(adv.double().cpu().numpy() - want_adv) <= 2 * U * np.abs(want_adv) + 2.0 ** -150)
     assert np.all(np.abs(g.double().cpu().numpy() - want) <= (6 + 3 * 0.125) * U * np.abs(want) + 2.0 ** -148) and bool(torch.isfinite(loss))
+
+
+def test_nothing_else_is_written(B):
+    """Through the C entry point, with guards around the loss, the advantages, the derivative and the working memory, each in memory of its own:
+    offsets that are none lead nowhere, and what is asked for is written whole."""
+    import ctypes as C
+    import torch
+    rng = np.random.default_rng(6)
+    lib, mark, G = B._lib, -7.25e33, 64
+    for sizes, n in [([30], 20), ([300], 40), ([70, 1, 0, 40], 90), ([3000], 3), ([100, 5], 700)]:
+        N = sum(sizes)
+        good = np.concatenate([[0], np.cumsum(rng.poisson(n, N))]).astype(np.int64)
+        T = int(good[-1]) + 5
+        lp, old, rf = (torch.from_numpy((-rng.random(T)).astype(np.float32)).cuda() for _ in range(3))
+        v = np.zeros((N, 4), dtype=np.int32)
+        v[:, 0] = rng.integers(1, 3, N)
+        v[:, 3] = rng.integers(0, 9, N)
+        outs = [o.contiguous() for o in torch.from_numpy(v).cuda().split(sizes)]
+        ptrs = (C.c_void_p * len(sizes))(*[o.data_ptr() if o.numel() else None for o in outs])
+        K = (C.c_uint64 * len(sizes))(*sizes)
+        size = lib.vl_policy_work(N, T)
+        rules = B.vl_policy_rules(eps=1e-6, clip_lo=0.2, clip_hi=0.2, normalise=1, kl=0.1, bank_cost=0.01)
+        bad = [good[::-1].copy(), good - 10 ** 12, good + 10 ** 12, rng.integers(-2 ** 62, 2 ** 62, N + 1), np.full(N + 1, T), np.zeros(N + 1, np.int64)]
+        for off in [good] + bad:
+            o = torch.from_numpy(off).cuda()
+            for want in ((1, 1), (0, 1), (1, 0)):
+                bufs = [torch.full((k + 2 * G,), mark, device="cuda") for k in (1, N, T, (size + 3) // 4)]
+                p = [b.data_ptr() + 4 * G for b in bufs]
+                torch.cuda.synchronize()
+                assert lib.vl_policy_loss(0, len(sizes), ptrs, K, o.data_ptr(), T, lp.data_ptr(), old.data_ptr(), rf.data_ptr(), C.byref(rules), p[0],
+                                          p[1] if want[0] else None, p[2] if want[1] else None, p[3], size, None) == 0
+                torch.cuda.synchronize()
+                for b, asked in zip(bufs, (1,) + want + (1,)):
+                    assert bool((b[:G] == mark).all()) and bool((b[-G:] == mark).all())
+                    assert asked or bool((b == mark).all())
+                for b, asked in zip(bufs[:3], (1,) + want):
+                    assert not asked or not bool((b[G:-G] == mark).any())
+                if off is good and want == (1, 1):
+                    first = [b.clone() for b in bufs[:3]]
+                    loss, adv, g = B.vl_policy_loss(outs, o, lp, old, ref_logprob=rf, kl=0.1, bank_cost=0.01)
+                    assert torch.equal(first[0][G], loss) and torch.equal(first[1][G:-G], adv) and torch.equal(first[2][G:-G], g)

@@ -224,3 +224,55 @@ def test_results_that_are_kept_keep_nothing_else(B, side):
     for r in list(o) + list(B.vl_policy_loss([v], off, o.logprob, stream=stream)):
         assert r.untyped_storage().nbytes() == r.numel() * r.element_size()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("V", [5, 16, 31, 64, 200, 250, 256, 300, 512, 1000, 1024, 2500, 4100, 9001, 40013])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_masks_and_widths_without_alternatives(B, dtype, V):
+    """Several rows a warp, each under a mask and a width of its own, and many long rows: closed logits hold infinities and no numbers, some rows
+    have nothing left, some are under no mask, some are left out."""
+    import torch
+    rng = np.random.default_rng(V)
+    R, n = (70, 9) if V <= 4100 else (5, 5)
+    for share, widths, pad in [(0.5, None, 0), (0.15, [0, 1, 2, 4, 5, 31], 0), (0.004, [32, 33, 64, 65, 200, 255], 8), (None, [1, 3, 40], 5), (0.3, [1, 2], 3)]:
+        m = None if share is None else _masks(rng, n, V, share)
+        if m is not None:
+            m[3], m[4] = 0xFFFFFFFF, 0
+        which = rng.integers(-1, n + 1, R).astype(np.int32)
+        which[:3] = [3, 4, -2 ** 31]
+        w = None if widths is None else rng.choice(widths, R).astype(np.uint8)
+        closed = np.array([ref.closed_entries(V, m[which[r]] if m is not None and 0 <= which[r] < n else None, 1 if w is None else w[r])
+                           for r in range(R)])
+        fill = rng.choice([np.nan, np.inf, -np.inf, {"f32": 3.4e38, "f16": 65504.0, "bf16": 3.3e38}[dtype]], (R, V))
+        x = _rows(np.where(closed, fill, _make(rng, R, V)), dtype, pad=pad, shift=pad % 4)
+        t = rng.integers(0, V, R)
+        t[1] = 65535
+        got = B.vl_token_logprobs(x, torch.from_numpy(t.astype(np.uint16)).cuda(),
+                                  occupied=None if m is None else torch.from_numpy(m.view(np.int32)).cuda(),
+                                  mask_rows=None if m is None else torch.from_numpy(which).cuda(),
+                                  widths=None if w is None else torch.from_numpy(w).cuda())
+        _check_scores(got, x.double().cpu().numpy(), 1.0, closed, t, 0)
+
+
+def test_more_masked_long_rows_than_places(B):
+    """Blocks go from row to row under masks: against the same rows with the closed entries set to minus infinity, bit for bit."""
+    import torch
+    rng = np.random.default_rng(7)
+    for R, V, dtype in [(3000, 9000, "bf16"), (2500, 4500, "f32"), (5000, 5003, "f16"), (90, 70000, "bf16")]:
+        n = 61
+        m = _masks(rng, n, V, 0.4)
+        closed = torch.from_numpy(np.array([ref.closed_entries(V, m[j]) for j in range(n)])).cuda()
+        which = torch.randint(0, n, (R,), device="cuda")
+        x = torch.randn(R, V, device="cuda").to(_type(dtype))
+        t = torch.randint(-1, V, (R,), device="cuda")
+        occ = torch.from_numpy(m.view(np.int32)).cuda()
+        want = B.vl_token_logprobs(x.masked_fill(closed[which], float("-inf")), t)
+        got = B.vl_token_logprobs(x, t, occupied=occ, mask_rows=which.to(torch.int32))
+        assert torch.equal(got.logprob, want.logprob) and torch.equal(got.entropy, want.entropy) and torch.equal(got.row_stats, want.row_stats)
+        lp = torch.log_softmax(x[:50].double().masked_fill(closed[which[:50]], float("-inf")), dim=1)
+        real = t[:50] >= 0
+        exact = lp.gather(1, t[:50].clamp(min=0)[:, None])[:, 0][real]
+        # S of the module's tolerance, and 3 u (|ln p| + 2 L) with L < ln V + 6
+        S = (V / 32 + 40 + 2 * (20 + np.log(V))) * U
+        near = (got.logprob[:50][real].double() - exact).abs() <= S + 3 * U * (exact.abs() + 2 * (np.log(V) + 6))
+        assert bool((near | (got.logprob[:50][real].double() == exact)).all())
