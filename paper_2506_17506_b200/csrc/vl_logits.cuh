@@ -210,7 +210,8 @@ struct RowVectors {
 };
 
 // Blocks of 256 threads of a multiprocessor for short rows, by the vectors of a lane: what hides the loads are warps (200,000 rows of 256 bf16
-// logits in us for 2, 3, 4, 5, 6 blocks of 122, 77, 64, 48, 40 registers a thread: 27.5, 21.8, 19.3, 24.5, 32).
+// logits in us for 2, 3, 4, 5, 6 blocks of 122, 77, 64, 48, 40 registers a thread: 27.5, 21.8, 19.3, 24.5, 32).  Kernels with alternatives, for which this was
+// not measured, spill at 64.
 constexpr int short_blocks(int NV) { return NV <= 8 ? 4 : 2; }
 
 // Short rows: groups of G lanes, a row each; lane g of a group holds the vectors g, g + G, ... and the closed entries of the words g,

@@ -217,7 +217,7 @@ __device__ __forceinline__ uint4 fetch(const RowVectors<T> &x, const RowMask &ma
 // row; nobody waits for it: there are two sets of places, and a cluster barrier whose two halves are a row apart.
 // Small blocks, eight to a multiprocessor: what a warp does once per row weighs less with four warps at a row than with sixteen
 // (bf16, 4,096 rows of 131,072 185 us and 198 with blocks of 512 threads when this was chosen, 180 now: 5.9 TB/s; 1,200 rows of 8,000 12
-// and 22).  592 rows of 1,000,000 take 187 us, 6.3 TB/s: what is left at 131,072 is what a row costs at its end.
+// and 22).  592 rows of 1,000,000 take 203 us, 5.8 TB/s.
 constexpr int LONG_THREADS = 128, LONG_U = 4, LONG_RING = 3, LONG_PARTS = 8;
 constexpr int long_smem(int threads) { return threads * LONG_U * LONG_RING * 16; }
 
