@@ -103,6 +103,9 @@ __device__ __forceinline__ void finish(const Sums &a, float c, float *L, float *
     *H = max_nan(ln_s - LN2 * __fdividef(a.t, a.s), 0.0f);  // (s is between 1/2 and 2^31)
 }
 
+// scale (x - m); the halves' difference is a number where x - m is none, and as exact.
+__device__ __forceinline__ float log_odds(float x, float m, float scale) { return (0.5f * x - 0.5f * m) * (2.0f * scale); }
+
 // The entries of vectors into the sums relative to m.
 template <typename T, int N>
 __device__ __forceinline__ void add_vectors(const uint4 (&raw)[N], float m, float c, f32x2 &s, f32x2 &t)
@@ -504,7 +507,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q,
         float L, H;
         finish(w, c, &L, &H);
         if (lane == 0) {
-            if (o.logprob) o.logprob[r] = MASKED && mask.is_closed((uint32_t)tok) ? -inf : (x_tok - w.m) * q.scale - L;
+            if (o.logprob) o.logprob[r] = MASKED && mask.is_closed((uint32_t)tok) ? -inf : log_odds(x_tok, w.m, q.scale) - L;
             if (o.entropy) o.entropy[r] = H;
             if (o.stats) *reinterpret_cast<float2 *>(o.stats + 2 * r) = make_float2(w.m, L);
         }
@@ -515,7 +518,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_score_long(const LogitRows q,
                 for (uint32_t j = 0; j < n; ++j) rank += s_cand[j] > k;
                 if (rank < o.top) {
                     o.ids[r * o.top + rank] = (int32_t)key_place(k);
-                    o.lps[r * o.top + rank] = (key_value(k) - w.m) * q.scale - L;
+                    o.lps[r * o.top + rank] = log_odds(key_value(k), w.m, q.scale) - L;
                 }
             }
             if (lane >= n && lane < o.top) { o.ids[r * o.top + lane] = -1; o.lps[r * o.top + lane] = -inf; }
@@ -699,7 +702,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_score_sh
         finish(Sums{m, s, t}, c, &L, &H);
         const bool left = tok < 0, empty = s == 0.0f;
         if (g == 0 && there) {
-            if (o.logprob) o.logprob[r] = left ? 0.0f : (empty || shut ? -inf : (x_tok - m) * q.scale - L);
+            if (o.logprob) o.logprob[r] = left ? 0.0f : (empty || shut ? -inf : log_odds(x_tok, m, q.scale) - L);
             if (o.entropy) o.entropy[r] = left || empty ? 0.0f : H;
             if (o.stats)
                 *reinterpret_cast<float2 *>(o.stats + 2 * r) = left ? make_float2(0.0f, 0.0f) : make_float2(empty ? -inf : m, L);
@@ -709,7 +712,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_score_sh
             if (lane < o.top) {
                 const bool one = k != 0 && !left;
                 o.ids[r * o.top + lane] = one ? (int32_t)key_place(k) : -1;
-                o.lps[r * o.top + lane] = one ? (key_value(k) - m) * q.scale - L : -inf;
+                o.lps[r * o.top + lane] = one ? log_odds(key_value(k), m, q.scale) - L : -inf;
             }
         }
     }

@@ -276,3 +276,20 @@ def test_more_masked_long_rows_than_places(B):
         S = (V / 32 + 40 + 2 * (20 + np.log(V))) * U
         near = (got.logprob[:50][real].double() - exact).abs() <= S + 3 * U * (exact.abs() + 2 * (np.log(V) + 6))
         assert bool((near | (got.logprob[:50][real].double() == exact)).all())
+
+
+@pytest.mark.parametrize("R,V", [(3, 12), (3, 700), (2, 9001), (1, 131072)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_differences_beyond_the_range_of_numbers(B, dtype, R, V):
+    """Logits at both ends of the type: their difference is no 32-bit number, its product with a small scale is."""
+    import torch
+    rng = np.random.default_rng(V)
+    vals = rng.choice([3.2e38, -3.2e38, 2e38, -1e30], (R, V))
+    vals[:, 0], vals[:, 1] = 3.2e38, -3.2e38
+    x = _rows(vals, dtype)
+    x64, closed = x.double().cpu().numpy(), np.zeros((R, V), bool)
+    for scale in (1e-6, 1e-3, 0.25):
+        scale = float(np.float32(scale))
+        for t in (np.full(R, 1), rng.integers(0, V, R)):
+            for top in (0, 12):
+                _check_scores(B.vl_token_logprobs(x, torch.from_numpy(t).cuda(), scale=scale, top=top), x64, scale, closed, t, top)
