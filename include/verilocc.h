@@ -394,11 +394,13 @@ int vl_token_logprobs(int device, const vl_logits *x, float *d_logprob, float *d
                       int32_t *d_top_ids, float *d_top_logprobs, void *cuda_stream);
 
 /*
- * The gradient of vl_token_logprobs: from d_g_logprob[r] and d_g_entropy[r] (a loss's derivatives to ln p and entropy of row r; NULL: 0)
- * to d_dlogits (the type of the logits, rows out_stride elements apart), which is written whole: 0 where an entry is not open (infinite
- * derivatives, and statistics that are no numbers, make no difference to that) and in rows that are left out or have nothing open.  ln p of a token that is not open is constant and hands nothing on.  d_row_stats, and
- * d_entropy where d_g_entropy is given, are the forward call's outputs for the same descriptor.  d_dlogits may be the logits themselves
- * (with the same stride); else it has no entry in common with them, though rows of both, at the same stride, may lie in turn.  Each value is rounded once; a p below 2^-126 counts as 0.  Stream order, errors: as vl_token_logprobs.
+ * The gradient of vl_token_logprobs: from d_g_logprob[r] and d_g_entropy[r] (a loss's derivatives to ln p and entropy of row r; NULL: 0) to
+ * d_dlogits (the type of the logits, rows out_stride elements apart), which is written whole: 0 where an entry is not open (infinite
+ * derivatives, and statistics that are no numbers, make no difference to that) and in rows that are left out or have nothing open.  ln p of
+ * a token that is not open is constant and hands nothing on.  d_row_stats, and d_entropy where d_g_entropy is given, are the forward call's
+ * outputs for the same descriptor.  d_dlogits may be the logits themselves (with the same stride); else it has no entry in common with
+ * them, though rows of both, at the same stride, may lie in turn.  Each value is rounded once; a p below 2^-125 may count as 0.  Stream
+ * order, errors: as vl_token_logprobs.
  */
 int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_row_stats, const float *d_entropy,
                                const float *d_g_logprob, const float *d_g_entropy, void *d_dlogits, uint64_t out_stride,
