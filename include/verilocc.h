@@ -407,6 +407,32 @@ int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_ro
                                void *cuda_stream);
 
 /*
+ * One token of every row, drawn with given random numbers: the descriptor is that of vl_token_logprobs without tokens (they must be NULL).
+ * With z = scale * logits and w = exp(z - largest z) over the open entries, in the order of falling logits and, among equals, of rising
+ * numbers, the kept entries are the shortest of these prefixes: the first top_k; those whose sum of w reaches top_p times that of the first
+ * top_k; those with w >= min_p.  With T the sum of w over the kept ones, the token of row r is the lowest kept entry i for which the sum of w
+ * over the kept entries 0..i is above d_uniform[r] * T.  What is decided is what 64-bit arithmetic decides (a sum within 2^-40 of what it is
+ * compared with may count as either side of it).
+ */
+typedef struct {
+    uint32_t top_k; /* 0: all */
+    double top_p;   /* above 0, up to 1; 1: all */
+    double min_p;   /* 0 to 1; 0: all */
+} vl_sampling;
+
+/*
+ * d_uniform [n_rows]: numbers from 0 on, below 1; a row whose number is none of these is left out: token -1, ln p 0, nothing kept.  d_tokens
+ * [n_rows]: token_bytes as in the descriptor; -1 (65535 in 2 bytes, which take at most 65,535 entries) where there is none.  d_logprob:
+ * ln p of the token under the whole row, as vl_token_logprobs gives it; d_drawn_logprob: under what was kept, ln (w / T); d_kept: entries
+ * kept (as int32).  Any of these three may be NULL.  Entries of logit minus infinity are never kept.  A row without possible entries: token
+ * -1, ln p minus infinity, nothing kept; a row with an open logit of plus infinity or that is no number: token -1, ln p no number, nothing
+ * kept.  Stream-ordered on `cuda_stream` of `device`, no synchronisation, no allocation, no working memory: calls may run side by side.
+ * Equal inputs give equal results, bit for bit.  n_rows == 0 is a no-op.  Errors: INVALID_ARG, CUDA.
+ */
+int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens, uint32_t token_bytes,
+                    float *d_logprob, float *d_drawn_logprob, int32_t *d_kept, void *cuda_stream);
+
+/*
  * The verdicts as a training signal (Section 6): a clipped policy objective over sampled candidates.  A candidate's reward is
  * 1 if it passes, else 0, less pair_cost for each conflict pair and bank_cost for each bank conflict of its verdict; its
  * advantage A is the reward less the mean over the samples of its program, with `normalise` divided by their standard deviation (of the
@@ -442,6 +468,41 @@ int vl_policy_loss(int device, uint32_t n, const vl_verdict *const *d_out, const
                    uint64_t n_tokens, const float *d_logprob, const float *d_old_logprob, const float *d_ref_logprob,
                    const vl_policy_rules *rules, float *d_loss, float *d_advantage, float *d_g_logprob, void *d_work,
                    uint64_t work_bytes, void *cuda_stream);
+
+/*
+ * The global norm of a model's gradients, and clipping: what stands between the gradient of the loss above and the step.  A gradient tensor, in
+ * DEVICE memory: n elements side by side, of which the result, if one is asked for, has as many at `out`: x itself, or memory that no
+ * tensor of the call has a byte in.  The descriptors are HOST memory, read during the call.
+ */
+typedef struct {
+    const void *x; /* aligned to its element */
+    void *out;     /* the same; vl_grad_norm does not read it */
+    uint64_t n;    /* up to 2^40 */
+    int dtype;     /* VL_F32, VL_F16 or VL_BF16, of x and out */
+} vl_gradient;
+
+/* Bytes of working memory of a call with n tensors. */
+uint64_t vl_grad_work(uint32_t n);
+
+/*
+ * *d_norm = scale * sqrt(sum of x^2 over all elements of the n tensors), *d_sum_squares = scale^2 * that sum (64 bits; what ranks that
+ * hold a part of the tensors each add up; 8-byte aligned); either may be NULL.  scale: 1 / the loss scale, 1e-18 to 1e18.  Squares are summed up in 64 bits from at
+ * most 64 of a thread in 32; where 32 bits do not hold these, in 64 throughout.  (A norm above the range of 32 bits reads infinity in *d_norm.)  Equal inputs give equal results, bit for bit.
+ * d_work: at least vl_grad_work(n) bytes of device memory, 16-byte aligned, the call's own until its work is done.  Stream-ordered on
+ * `cuda_stream` of `device`, no synchronisation, no allocation.  Errors: INVALID_ARG, CUDA.
+ */
+int vl_grad_norm(int device, uint32_t n, const vl_gradient *tensors, double scale, float *d_norm, double *d_sum_squares, void *d_work,
+                 uint64_t work_bytes, void *cuda_stream);
+
+/*
+ * out = scale * factor * x, rounded to its type (in 16 bits by way of 32), with factor = max_norm / norm where the norm is above max_norm, else 1.  The norm is that of
+ * vl_grad_norm, or, with d_given (DEVICE, 8-byte aligned: a sum of squares as vl_grad_norm gives it, of all ranks together), its root.  *d_norm and *d_factor (either may be
+ * NULL) receive the two.  A norm that is no finite number gives factor 0 and results of 0, whatever the elements are: a step that does
+ * nothing, which the norm tells.  max_norm: 0 or more, infinity for none.  Results that share memory with each other or with another tensor
+ * are refused.  Working memory, stream order, errors: as vl_grad_norm; UNSUPPORTED (no host memory to look for shared bytes).
+ */
+int vl_clip_grads(int device, uint32_t n, const vl_gradient *tensors, double scale, double max_norm, const double *d_given, float *d_norm,
+                  float *d_factor, void *d_work, uint64_t work_bytes, void *cuda_stream);
 
 /*
  * Block-level liveness without any allocation.  (The paper has no counterpart; this exists for

@@ -38,7 +38,8 @@ EXPORTS = ["vl_program_create", "vl_program_destroy", "vl_program_set_option", "
            "vl_resample_stats", "vl_verify_until_pass", "vl_program_set_constraints", "vl_diagnose", "vl_occupied_masks",
            "vl_expand_masks",
            "vl_dict_layout", "vl_verify_dict",
-           "vl_token_logprobs", "vl_token_logprobs_backward", "vl_policy_work", "vl_policy_loss"]
+           "vl_token_logprobs", "vl_token_logprobs_backward", "vl_policy_work", "vl_policy_loss",
+           "vl_token_sample", "vl_grad_work", "vl_grad_norm", "vl_clip_grads"]
 
 VERDICT_DTYPE = np.dtype([("flags", "<u4"), ("first_violation_instr", "<i4"),
                           ("conflict_pairs", "<u4"), ("bank_conflicts", "<u4")])
@@ -127,6 +128,14 @@ class vl_policy_rules(C.Structure):
         ("normalise", C.c_int), ("per_token", C.c_int)]
 
 
+class vl_sampling(C.Structure):
+    _fields_ = [("top_k", C.c_uint32), ("top_p", C.c_double), ("min_p", C.c_double)]
+
+
+class vl_gradient(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("n", C.c_uint64), ("dtype", C.c_int)]
+
+
 _lib.vl_token_logprobs.restype = C.c_int
 _lib.vl_token_logprobs.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 3
 _lib.vl_token_logprobs_backward.restype = C.c_int
@@ -136,6 +145,15 @@ _lib.vl_policy_work.argtypes = [C.c_uint64, C.c_uint64]
 _lib.vl_policy_loss.restype = C.c_int
 _lib.vl_policy_loss.argtypes = ([C.c_int, C.c_uint32] + [C.c_void_p] * 3 + [C.c_uint64] + [C.c_void_p] * 8 +
                                 [C.c_uint64, C.c_void_p])
+_lib.vl_token_sample.restype = C.c_int
+_lib.vl_token_sample.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 4
+_lib.vl_grad_work.restype = C.c_uint64
+_lib.vl_grad_work.argtypes = [C.c_uint32]
+_lib.vl_grad_norm.restype = C.c_int
+_lib.vl_grad_norm.argtypes = [C.c_int, C.c_uint32, C.c_void_p, C.c_double] + [C.c_void_p] * 3 + [C.c_uint64, C.c_void_p]
+_lib.vl_clip_grads.restype = C.c_int
+_lib.vl_clip_grads.argtypes = ([C.c_int, C.c_uint32, C.c_void_p, C.c_double, C.c_double] + [C.c_void_p] * 4 +
+                               [C.c_uint64, C.c_void_p])
 SAMPLE_STATS_DTYPE = np.dtype([("first_pass", "<u8"), ("n_pass", "<u8")])
 
 
@@ -468,7 +486,11 @@ def vl_resample_stats(outs, ks=(1, 10, 100), device: int = 0, stream=None):
 
 TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprob entropy row_stats top_ids top_logprobs")
 _LOGITS = struct.Struct("@PiQIQPIPQPPf0P")     # vl_logits
+TokenSample = collections.namedtuple("TokenSample", "tokens logprob drawn_logprob kept")
+GradNorm = collections.namedtuple("GradNorm", "norm sum_squares")
+Clipped = collections.namedtuple("Clipped", "norm factor outs")
 _RULES = struct.Struct("@6d2i")                # vl_policy_rules
+_SAMPLING = struct.Struct("@Idd")              # vl_sampling
 _HERE = contextlib.nullcontext()
 
 
@@ -578,6 +600,42 @@ def vl_token_logprobs(logits, tokens=None, occupied=None, mask_rows=None, widths
     return TokenLogprobs(lp, ent, stats, ids, lps)
 
 
+def vl_token_sample(logits, uniform, occupied=None, mask_rows=None, widths=None, scale: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                    min_p: float = 0.0, token_dtype=None, stream=None):
+    """One token of every row of logits (as for ``vl_token_logprobs``, with the same masks, widths and ``scale`` = 1 / temperature), drawn
+    with the given numbers ``uniform`` (float32 [rows], from 0 on, below 1; a row whose number is none of these is left out).  Kept are
+    the ``top_k`` best entries (0: all), of these the best whose probabilities sum up to ``top_p`` (1: all), and of these the ones with
+    at least ``min_p`` times the best one's probability (0: all).  ``token_dtype``: int64 (default), int32, or uint16 / int16 as entries of candidate rows.
+    Returns TokenSample(tokens, logprob under the whole row, drawn_logprob under what was kept, kept: entries kept, int32); a row without
+    possible entries has token -1 and log probability minus infinity.  On ``stream`` (default: the current one of the logits'
+    device), without waiting."""
+    where = "vl_token_sample"
+    x, R, V, dev = _logit_rows(where, logits, None, occupied, mask_rows, widths, scale)
+    torch = _Torch.torch
+    u = _vector(uniform, "uniform", where, dev, R, _Torch.f32) if uniform is not None else _refuse(where, "uniform: the numbers to draw with")
+    kind = token_dtype or torch.int64
+    size = _Torch.tokens.get(kind) or _refuse(where, "token_dtype: int64, int32, uint16 or int16")
+    if not 0 <= top_k < 1 << 32:
+        _refuse(where, "top_k: 0 (all) or a number of entries")
+    if not (0 < top_p <= 1 and 0 <= min_p <= 1):
+        _refuse(where, "top_p: above 0, up to 1; min_p: 0 to 1")
+    if size == 2 and V > 65535:
+        _refuse(where, "token_dtype: 65,535 entries at most in 2 bytes")
+    scope = None
+    if stream is None:
+        ptr = _Torch.current(dev)
+    else:
+        ptr, scope = _on(stream, dev)
+    with scope or _HERE:        # memory of their own: what is kept keeps nothing else
+        lp = logits.new_empty(R, dtype=torch.float32)
+        drawn, kept, tokens = lp.new_empty(R), lp.new_empty(R, dtype=torch.int32), lp.new_empty(R, dtype=kind)
+    rc = _lib.vl_token_sample(dev, x, _SAMPLING.pack(top_k, top_p, min_p), u, tokens.data_ptr(), size, lp.data_ptr(), drawn.data_ptr(),
+                              kept.data_ptr(), ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return TokenSample(tokens, lp, drawn, kept)
+
+
 def _row_by_row(out, logits, R: int, V: int, apart: int) -> bool:
     """Whether a matrix is the logits themselves, or shares no entry with them (rows of both may lie in turn)."""
     size, a, b = logits.element_size(), logits.data_ptr(), out.data_ptr()
@@ -666,6 +724,94 @@ def vl_policy_loss(outs, token_off, logprob, old_logprob=None, ref_logprob=None,
     if rc != VL_OK:
         raise VlError(rc, where)
     return loss, adv, g
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's elements fill a piece of memory, in whatever order."""
+    if t.is_contiguous():
+        return True
+    n = 1
+    for step, size in sorted((a, b) for a, b in zip(t.stride(), t.shape) if b != 1):
+        if step != n:
+            return False
+        n *= size
+    return n == t.numel()
+
+
+def _gradients(where, grads, outs):
+    """(descriptors as bytes, their number, device number) of gradient tensors and, with ``outs``, of where their results go."""
+    torch = _Torch.torch or _Torch.load()
+    kinds, dev, flat = _Torch.logits, -1, []
+    if outs is not None and len(outs) != len(grads):
+        _refuse(where, "outs: one for every tensor")
+    for j, g in enumerate(grads):
+        kind = kinds.get(g.dtype)
+        d = g.get_device()
+        if dev < 0:
+            dev = d
+        if kind is None or d < 0 or d != dev or g.is_sparse or not _dense(g):
+            _refuse(where, "grads: dense CUDA tensors of float32, float16 or bfloat16 on one device")
+        at = to = g.data_ptr()
+        if outs is not None:
+            o = outs[j]
+            if o.dtype is not g.dtype or o.get_device() != dev or o.shape != g.shape or (o.stride() != g.stride() and g.numel() > 1):
+                _refuse(where, "outs: tensors like the gradients")
+            to = o.data_ptr()
+        flat += (at, to, g.numel(), kind[0])
+    return struct.pack("@" + "PPQi4x" * len(grads), *flat), len(grads), dev if dev >= 0 else torch.cuda.current_device()
+
+
+def vl_grad_norm(grads, scale: float = 1.0, stream=None):
+    """The global norm of gradient tensors (CUDA, float32 / float16 / bfloat16, dense, on one device) times ``scale`` (1 / the loss scale).
+    Returns GradNorm(norm, a float32 scalar tensor; sum_squares, its square in float64: what ranks that hold a part of the tensors each
+    add up).  On ``stream`` (default: the current one of the tensors' device), without waiting."""
+    where = "vl_grad_norm"
+    grads = grads if isinstance(grads, (list, tuple)) else list(grads)
+    t, n, dev = _gradients(where, grads, None)
+    torch = _Torch.torch
+    scope = None
+    if stream is None:
+        ptr = _Torch.current(dev)
+    else:
+        ptr, scope = _on(stream, dev)
+    size = int(_lib.vl_grad_work(n))
+    with scope or _HERE:
+        work = torch.empty(size // 8, dtype=torch.float64, device=f"cuda:{dev}")
+        norm, squares = work.new_empty((), dtype=torch.float32), work.new_empty(())
+    rc = _lib.vl_grad_norm(dev, n, t, scale, norm.data_ptr(), squares.data_ptr(), work.data_ptr(), size, ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return GradNorm(norm, squares)
+
+
+def vl_clip_grads(grads, max_norm: float, scale: float = 1.0, outs=None, sum_squares=None, stream=None):
+    """Gradient tensors (as for ``vl_grad_norm``) times ``scale``, and times max_norm / norm where their global norm is above ``max_norm``: in
+    place, or into ``outs`` (tensors of the same shapes, types and strides; none shares memory with another one, or with a gradient that
+    is not its own).  With ``sum_squares`` (float64 scalar tensor: of all ranks together) the norm is its root.  A norm that is no finite number
+    makes every result 0.  Returns Clipped(norm, factor: float32 scalar tensors; outs).  On ``stream`` (default: the current one of
+    the tensors' device), without waiting."""
+    where = "vl_clip_grads"
+    grads = grads if isinstance(grads, (list, tuple)) else list(grads)
+    t, n, dev = _gradients(where, grads, outs)
+    torch = _Torch.torch
+    given = 0
+    if sum_squares is not None:
+        if sum_squares.get_device() != dev or sum_squares.dtype != torch.float64 or sum_squares.numel() != 1:
+            _refuse(where, f"sum_squares: one float64 number on cuda:{dev}")
+        given = sum_squares.data_ptr()
+    scope = None
+    if stream is None:
+        ptr = _Torch.current(dev)
+    else:
+        ptr, scope = _on(stream, dev)
+    size = int(_lib.vl_grad_work(n))
+    with scope or _HERE:
+        work = torch.empty(size // 8, dtype=torch.float64, device=f"cuda:{dev}")
+        norm, factor = work.new_empty((), dtype=torch.float32), work.new_empty((), dtype=torch.float32)
+    rc = _lib.vl_clip_grads(dev, n, t, scale, max_norm, given, norm.data_ptr(), factor.data_ptr(), work.data_ptr(), size, ptr)
+    if rc != VL_OK:
+        raise VlError(rc, where)
+    return Clipped(norm, factor, grads if outs is None else outs)
 
 
 def verdicts_to_numpy(t) -> np.ndarray:

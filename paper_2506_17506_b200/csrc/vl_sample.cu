@@ -1,0 +1,23 @@
+// vl_token_sample: checks and dispatch (the kernels are in vl_sample.cuh).
+#include "vl_sample.cuh"
+
+extern "C" int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens,
+                               uint32_t token_bytes, float *d_logprob, float *d_drawn_logprob, int32_t *d_kept, void *stream)
+{
+    LogitRows q;
+    const int rc = vl_logit_rows(x, &q);
+    if (rc != VL_OK) return rc;
+    if (x->tokens || !rules) return VL_ERR_INVALID_ARG;
+    if (!(rules->top_p > 0.0 && rules->top_p <= 1.0) || !(rules->min_p >= 0.0 && rules->min_p <= 1.0)) return VL_ERR_INVALID_ARG;
+    if ((token_bytes != 2 && token_bytes != 4 && token_bytes != 8) || (token_bytes == 2 && q.V > 65535)) return VL_ERR_INVALID_ARG;
+    if ((uintptr_t)d_tokens % token_bytes) return VL_ERR_INVALID_ARG;
+    if (((uintptr_t)d_uniform | (uintptr_t)d_logprob | (uintptr_t)d_drawn_logprob | (uintptr_t)d_kept) & 3) return VL_ERR_INVALID_ARG;
+    if (q.n_rows == 0) return VL_OK;
+    if (!d_uniform || !d_tokens) return VL_ERR_INVALID_ARG;
+    const DeviceScope scope(device);
+    if (scope.error != cudaSuccess) return VL_ERR_CUDA;
+    const SampleRules s{d_uniform, rules->top_k, rules->top_p, rules->min_p};
+    const SampleOut o{d_tokens, token_bytes, d_logprob, d_drawn_logprob, d_kept};
+    const auto launch = x->dtype == VL_F32 ? vl_sample_f32 : x->dtype == VL_F16 ? vl_sample_f16 : vl_sample_bf16;
+    return launch(q, s, o, device, (cudaStream_t)stream) == cudaSuccess ? VL_OK : VL_ERR_CUDA;
+}
