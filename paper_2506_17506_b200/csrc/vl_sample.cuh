@@ -10,7 +10,7 @@
 // Which entries are kept, and which one a number falls on, is decided as in 64 bits: sums of 32-bit terms are off by some 2^-20, which for
 // rows of 100,000 entries is where a number falls on another token every tenth row.
 #pragma once
-#include "vl_logits.cuh"
+#include "vl_rank.cuh"
 
 struct SampleRules {
     const float *uniform;  // [n_rows]
@@ -29,12 +29,6 @@ cudaError_t vl_sample_bf16(const LogitRows &q, const SampleRules &s, const Sampl
 
 namespace {
 
-__device__ __forceinline__ uint32_t ordered(float x)  // ascends with x; zeros of both signs are equal
-{
-    const uint32_t b = __float_as_uint(x + 0.0f);
-    return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
-}
-__device__ __forceinline__ float from_ordered(uint32_t o) { return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o); }
 constexpr uint32_t LEAST_KEY = 0x00800000u;  // of the lowest number; minus infinity lies below
 
 __device__ __forceinline__ void put_sample(const SampleOut &o, uint64_t r, int64_t token, float logprob, float drawn, uint32_t kept)
@@ -317,20 +311,6 @@ __global__ void __launch_bounds__(NT == 32 ? 256 : NT) k_sample_64(const LogitRo
         sample_row_64<T, NT>(q, s, o, r, s_d, s_u);
         if (NT > 32) __syncthreads();  // (the next row's first sums may go where this row's last ones are read)
     }
-}
-
-template <typename T>
-cudaError_t launch_sample(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
-{
-    const uint64_t at_most = 16 * (uint64_t)vl_device_sm_count(device);
-    g_vl_launches.fetch_add(1);
-    if (q.V <= 1024) {
-        const uint64_t blocks = (q.n_rows + 7) / 8;
-        k_sample_64<T, 32><<<(uint32_t)(blocks < at_most ? blocks : at_most), 256, 0, st>>>(q, s, o);
-    } else {
-        k_sample_64<T, 512><<<(uint32_t)(q.n_rows < at_most ? q.n_rows : at_most), 512, 0, st>>>(q, s, o);
-    }
-    return cudaGetLastError();
 }
 
 }  // namespace

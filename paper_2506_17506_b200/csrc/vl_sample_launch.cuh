@@ -1,0 +1,27 @@
+// Which kernel draws from which rows.
+#pragma once
+#include <math.h>
+
+#include "vl_sample_short.cuh"
+
+namespace {
+
+template <typename T>
+cudaError_t launch_sample(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
+{
+    bool aligned;
+    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
+    ShortRules h;
+    h.drop = s.min_p > 0.0 ? log(s.min_p) / (double)q.scale : -INFINITY;
+    h.eps = (float)((45.0 + 1.5 * log2((double)q.V + 1.0)) / 16777216.0);
+    const bool masked = q.occupied || q.widths;
+    if (masked ? (aligned ? launch_sample_short<T, true, true>(q, s, o, h, n, st) : launch_sample_short<T, true, false>(q, s, o, h, n, st))
+               : (aligned ? launch_sample_short<T, false, true>(q, s, o, h, n, st) : launch_sample_short<T, false, false>(q, s, o, h, n, st)))
+        return cudaGetLastError();
+    const uint64_t at_most = 16 * (uint64_t)vl_device_sm_count(device);
+    g_vl_launches.fetch_add(1);
+    k_sample_64<T, 512><<<(uint32_t)(q.n_rows < at_most ? q.n_rows : at_most), 512, 0, st>>>(q, s, o);
+    return cudaGetLastError();
+}
+
+}  // namespace
