@@ -420,17 +420,21 @@ typedef struct {
     double min_p;   /* 0 to 1; 0: all */
 } vl_sampling;
 
+/* Bytes of working memory of a vl_token_sample call. */
+uint64_t vl_sample_work(uint64_t n_rows);
+
 /*
  * d_uniform [n_rows]: numbers from 0 on, below 1; a row whose number is none of these is left out: token -1, ln p 0, nothing kept.  d_tokens
  * [n_rows]: token_bytes as in the descriptor; -1 (65535 in 2 bytes, which take at most 65,535 entries) where there is none.  d_logprob:
  * ln p of the token under the whole row, as vl_token_logprobs gives it; d_drawn_logprob: under what was kept, ln (w / T); d_kept: entries
  * kept (as int32).  Any of these three may be NULL.  Entries of logit minus infinity are never kept.  A row without possible entries: token
  * -1, ln p minus infinity, nothing kept; a row with an open logit of plus infinity or that is no number: token -1, ln p no number, nothing
- * kept.  Stream-ordered on `cuda_stream` of `device`, no synchronisation, no allocation, no working memory: calls may run side by side.
- * Equal inputs give equal results, bit for bit.  n_rows == 0 is a no-op.  Errors: INVALID_ARG, CUDA.
+ * kept.  d_work: at least vl_sample_work bytes of device memory, the call's own until its work is done.  Stream-ordered on `cuda_stream` of
+ * `device`, no synchronisation, no allocation.  Equal inputs give equal results, bit for bit.  n_rows == 0 is a no-op.  Errors: INVALID_ARG,
+ * CUDA.
  */
 int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens, uint32_t token_bytes,
-                    float *d_logprob, float *d_drawn_logprob, int32_t *d_kept, void *cuda_stream);
+                    float *d_logprob, float *d_drawn_logprob, int32_t *d_kept, void *d_work, uint64_t work_bytes, void *cuda_stream);
 
 /*
  * The verdicts as a training signal (Section 6): a clipped policy objective over sampled candidates.  A candidate's reward is

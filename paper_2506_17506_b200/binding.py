@@ -39,7 +39,7 @@ EXPORTS = ["vl_program_create", "vl_program_destroy", "vl_program_set_option", "
            "vl_expand_masks",
            "vl_dict_layout", "vl_verify_dict",
            "vl_token_logprobs", "vl_token_logprobs_backward", "vl_policy_work", "vl_policy_loss",
-           "vl_token_sample", "vl_grad_work", "vl_grad_norm", "vl_clip_grads"]
+           "vl_sample_work", "vl_token_sample", "vl_grad_work", "vl_grad_norm", "vl_clip_grads"]
 
 VERDICT_DTYPE = np.dtype([("flags", "<u4"), ("first_violation_instr", "<i4"),
                           ("conflict_pairs", "<u4"), ("bank_conflicts", "<u4")])
@@ -146,7 +146,9 @@ _lib.vl_policy_loss.restype = C.c_int
 _lib.vl_policy_loss.argtypes = ([C.c_int, C.c_uint32] + [C.c_void_p] * 3 + [C.c_uint64] + [C.c_void_p] * 8 +
                                 [C.c_uint64, C.c_void_p])
 _lib.vl_token_sample.restype = C.c_int
-_lib.vl_token_sample.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 4
+_lib.vl_token_sample.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 4 + [C.c_uint64, C.c_void_p]
+_lib.vl_sample_work.restype = C.c_uint64
+_lib.vl_sample_work.argtypes = [C.c_uint64]
 _lib.vl_grad_work.restype = C.c_uint64
 _lib.vl_grad_work.argtypes = [C.c_uint32]
 _lib.vl_grad_norm.restype = C.c_int
@@ -626,11 +628,13 @@ def vl_token_sample(logits, uniform, occupied=None, mask_rows=None, widths=None,
         ptr = _Torch.current(dev)
     else:
         ptr, scope = _on(stream, dev)
+    work_size = int(_lib.vl_sample_work(R))
     with scope or _HERE:        # memory of their own: what is kept keeps nothing else
         lp = logits.new_empty(R, dtype=torch.float32)
         drawn, kept, tokens = lp.new_empty(R), lp.new_empty(R, dtype=torch.int32), lp.new_empty(R, dtype=kind)
+        work = lp.new_empty(work_size, dtype=torch.uint8)
     rc = _lib.vl_token_sample(dev, x, _SAMPLING.pack(top_k, top_p, min_p), u, tokens.data_ptr(), size, lp.data_ptr(), drawn.data_ptr(),
-                              kept.data_ptr(), ptr)
+                              kept.data_ptr(), work.data_ptr(), work_size, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
     return TokenSample(tokens, lp, drawn, kept)

@@ -2,7 +2,7 @@
 #pragma once
 #include <math.h>
 
-#include "vl_sample_short.cuh"
+#include "vl_sample_long.cuh"
 
 namespace {
 
@@ -18,10 +18,9 @@ cudaError_t launch_sample(const LogitRows &q, const SampleRules &s, const Sample
     if (masked ? (aligned ? launch_sample_short<T, true, true>(q, s, o, h, n, st) : launch_sample_short<T, true, false>(q, s, o, h, n, st))
                : (aligned ? launch_sample_short<T, false, true>(q, s, o, h, n, st) : launch_sample_short<T, false, false>(q, s, o, h, n, st)))
         return cudaGetLastError();
-    const uint64_t at_most = 16 * (uint64_t)vl_device_sm_count(device);
-    g_vl_launches.fetch_add(1);
-    k_sample_64<T, 512><<<(uint32_t)(q.n_rows < at_most ? q.n_rows : at_most), 512, 0, st>>>(q, s, o);
-    return cudaGetLastError();
+    if (s.top_k || s.top_p < 1.0 || s.min_p > 0.0)
+        return masked ? launch_sample_long<T, true, true>(q, s, o, h, device, st) : launch_sample_long<T, false, true>(q, s, o, h, device, st);
+    return masked ? launch_sample_long<T, true, false>(q, s, o, h, device, st) : launch_sample_long<T, false, false>(q, s, o, h, device, st);
 }
 
 }  // namespace

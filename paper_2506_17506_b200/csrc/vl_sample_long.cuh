@@ -1,0 +1,616 @@
+// Drawing from long rows: one pass over the row, and a second look at what matters of it.
+//
+// A block of four warps, or a cluster of such blocks, is at a row; each warp has a run of the row's vectors and cuts it into eight segments.
+// The pass keeps for every segment the sum of its weights (in 64 bits from 32 entries of a lane in 32), and for every lane of it the largest
+// logit: 1,024 groups of a block.
+//   No rules: the sums tell the segment that the number falls into, and that one is read again.
+//   top_k, top_p, min_p: the groups' largest logits, counted in 128 steps below the largest one, bound the cut from below: top_k groups with
+//   such a logit, or groups whose largest entries alone have weight enough, mean that the cut is no lower.  The groups that reach the bound are
+//   read again, and what reaches it is gathered, put in order, and the rules are applied in 64 bits.
+// A row is left to k_sample_rest where a border is nearer to what it is compared with than the 32-bit terms are known (eps, below), where more
+// than LD_CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
+//
+// eps: a weight is within (4 + 1.4 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
+// passes by more than 3; a lane's 32 entries go through 8 additions.  The mean of |y| relative to the largest logit is at most log2(V / S).
+// Sums are therefore within eps S, eps = (20 + 1.4 log2(V / S)) u.
+#pragma once
+#include "vl_sample_short.cuh"
+
+namespace {
+
+constexpr uint32_t LD_THREADS = 128, LD_WARPS = 4, LD_U = 4, LD_RING = 3, LD_SEGS = 8, LD_PARTS = 8;
+constexpr uint32_t LD_STEP = 32 * LD_U;               // vectors of a warp at a time
+constexpr uint32_t LD_CAP = 1024, LD_BINS = 128, LD_GUESS = 256;
+constexpr uint32_t LD_RING_BYTES = LD_THREADS * LD_U * LD_RING * 16;
+// what follows the pass lies where its ring was: keys, then their weights, then the groups
+constexpr uint32_t LD_WEIGHTS_AT = LD_CAP * 8, LD_GROUPS_AT = LD_CAP * 16;
+static_assert(LD_GROUPS_AT + LD_SEGS * LD_THREADS * 2 <= LD_RING_BYTES && LD_CAP * 24 <= LD_RING_BYTES, "fits the ring");
+
+__device__ __forceinline__ void ld_copy(uint32_t to, const uint4 *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void ld_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void ld_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// A block's n keys in falling order (n <= LD_CAP).  Few: each to its rank; many: by halves.  (A key's rank among 256 takes about as many steps as the halves do.)
+__device__ __forceinline__ void sort_keys(key_t64 *keys, uint32_t n)
+{
+    const uint32_t tid = threadIdx.x;
+    if (n <= 256) {
+        key_t64 mine[2];
+        uint32_t rank[2] = {0, 0};
+        mine[0] = tid < n ? keys[tid] : 0ull;
+        mine[1] = tid + 128 < n ? keys[tid + 128] : 0ull;
+        for (uint32_t j = 0; j < n; ++j) {
+            const key_t64 other = keys[j];
+            rank[0] += other > mine[0];
+            rank[1] += other > mine[1];
+        }
+        __syncthreads();
+        if (tid < n) keys[rank[0]] = mine[0];
+        if (tid + 128 < n) keys[rank[1]] = mine[1];
+        __syncthreads();
+        return;
+    }
+    uint32_t N = 512;
+    while (N < n) N *= 2;
+    for (uint32_t i = n + tid; i < N; i += LD_THREADS) keys[i] = 0ull;
+    __syncthreads();
+    for (uint32_t k = 2; k <= N; k *= 2)
+        for (uint32_t d = k / 2; d; d /= 2) {
+            for (uint32_t p = tid; p < N / 2; p += LD_THREADS) {
+                const uint32_t i = 2 * p - (p & (d - 1)), j = i + d;
+                const key_t64 a = keys[i], b = keys[j];
+                if ((a < b) == ((i & k) == 0)) { keys[i] = b; keys[j] = a; }
+            }
+            __syncthreads();
+        }
+}
+
+// In place: sums of the first i + 1 of n numbers (n <= LD_CAP).  s: LD_WARPS numbers.
+__device__ __forceinline__ void sum_up(double *v, uint32_t n, double *s)
+{
+    const uint32_t tid = threadIdx.x, lane = tid & 31, per = (n + LD_THREADS - 1) / LD_THREADS, first = min(n, tid * per), end = min(n, first + per);
+    double own = 0.0;
+    for (uint32_t i = first; i < end; ++i) own += v[i];
+    double up = own;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const double w = __shfl_up_sync(0xffffffffu, up, d);
+        if (lane >= (uint32_t)d) up += w;
+    }
+    if (lane == 31) s[tid >> 5] = up;
+    __syncthreads();
+    double base = __shfl_up_sync(0xffffffffu, up, 1);
+    if (lane == 0) base = 0.0;
+    double front = 0.0;
+    for (uint32_t w = 0; w < tid >> 5; ++w) front += s[w];
+    double run = front + base;
+    for (uint32_t i = first; i < end; ++i) {
+        run += v[i];
+        v[i] = run;
+    }
+    __syncthreads();
+}
+
+// The smallest of a thread's numbers over the block, in every thread; *s is 0xFFFFFFFF before, and a barrier lies between that and the call.
+__device__ __forceinline__ uint32_t block_min(uint32_t v, uint32_t *s)
+{
+    v = __reduce_min_sync(0xffffffffu, v);
+    if ((threadIdx.x & 31) == 0) atomicMin(s, v);
+    __syncthreads();
+    return *s;
+}
+
+// One block: what reaches the bound of a row (n keys in any order) is put in order, cut by the rules, and drawn from.  buffer: keys, weights, keys.
+// False if that is too near to call.
+__device__ __forceinline__ bool draw_listed(unsigned char *buffer, uint32_t n, bool whole, const LogitRows &q, const SampleRules &s, const SampleOut &o,
+                                            uint64_t r, float u, float M, double S, double eps, float least, float L, double *s_four, uint32_t *s_found)
+{
+    key_t64 *const keys = reinterpret_cast<key_t64 *>(buffer), *const second = reinterpret_cast<key_t64 *>(buffer + LD_GROUPS_AT);
+    double *const w = reinterpret_cast<double *>(buffer + LD_WEIGHTS_AT);
+    const uint32_t tid = threadIdx.x;
+    const double scale = (double)q.scale;
+    auto weight = [&](key_t64 k) { return exp(scale * ((double)key_value(k) - (double)M)); };
+    if (tid < 3) s_found[tid] = tid == 2 ? 0u : 0xFFFFFFFFu;
+    sort_keys(keys, n);
+    for (uint32_t i = tid; i < n; i += LD_THREADS) w[i] = weight(keys[i]);
+    __syncthreads();
+    sum_up(w, n, s_four);
+    uint32_t kept = s.top_k ? min(n, s.top_k) : n;
+    if (s.top_p < 1.0) {
+        const double need = s.top_p * (s.top_k ? w[kept - 1] : S), lacks = s.top_k ? 0.0 : eps * need;
+        uint32_t first = 0xFFFFFFFFu;
+        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+            if (w[i] >= need) first = i;
+        first = block_min(first, s_found);
+        if (first != 0xFFFFFFFFu) {
+            if (w[first] < need + lacks || (first && w[first - 1] >= need - lacks)) return false;
+            kept = first + 1;
+        } else if (whole || w[kept - 1] >= need - lacks) {  // (else what is listed is all that min_p leaves)
+            return false;
+        }
+    }
+    if (s.min_p > 0.0) {
+        uint32_t first = 0xFFFFFFFFu;
+        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+            if (key_value(keys[i]) < least) first = i;
+        kept = min(kept, block_min(first, s_found + 1));
+    }
+    const double total = w[kept - 1], at = (double)u * total;
+    for (uint32_t i = tid; i < kept; i += LD_THREADS) second[i] = (key_t64)(0xFFFFFFFFu - key_place(keys[i])) << 32 | i;
+    __syncthreads();
+    sort_keys(second, kept);
+    for (uint32_t i = tid; i < kept; i += LD_THREADS) w[i] = weight(keys[(uint32_t)second[i]]);
+    if (tid == 0) s_found[0] = 0xFFFFFFFFu;
+    __syncthreads();
+    sum_up(w, kept, s_four);
+    uint32_t first = 0xFFFFFFFFu;
+    for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+        if (w[i] > at) first = i;
+    first = block_min(first, s_found);
+    if (first == 0xFFFFFFFFu) return false;
+    if (tid == 0) {
+        const key_t64 k = keys[(uint32_t)second[first]];
+        const float z = log_odds(key_value(k), M, q.scale);
+        put_sample(o, r, (int64_t)key_place(k), min_nan(z - L, 0.0f), min_nan(z - (float)log(total), 0.0f), kept);
+    }
+    return true;
+}
+
+template <typename T, bool MASKED, bool RULES, bool CLUSTER>
+__global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q, const SampleRules s, const SampleOut o, const ShortRules h,
+                                                              uint32_t log_of_parts)
+{
+    constexpr uint32_t NT = LD_THREADS, U = LD_U, RING = LD_RING, MAX_PARTS = CLUSTER ? LD_PARTS : 1;
+    constexpr uint32_t RECS = RULES ? LD_WARPS : LD_WARPS * LD_SEGS;  // sums of a part
+    const uint32_t log_parts = CLUSTER ? log_of_parts : 0, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
+    extern __shared__ __align__(16) uint4 s_ring[];
+    __shared__ T s_most[RULES ? LD_SEGS : 1][RULES ? NT : 1];
+    __shared__ double s_sum[MAX_PARTS * RECS], s_four[LD_WARPS];
+    __shared__ float s_ref[MAX_PARTS * RECS], s_max[MAX_PARTS * LD_WARPS], s_min[MAX_PARTS * LD_WARPS], s_bound;
+    __shared__ uint32_t s_count[MAX_PARTS * LD_WARPS], s_bins[RULES ? LD_BINS : 1], s_mass[RULES ? LD_BINS : 1], s_n[2], s_found[3];
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint64_t step = gridDim.x >> log_parts;
+    const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), margin = 3.0f / c;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + tid * 16;
+    unsigned char *const buffer = reinterpret_cast<unsigned char *>(s_ring);
+    cg::cluster_group cluster = cg::this_cluster();
+    auto away = [&](auto *p, uint32_t b) { return CLUSTER ? cluster.map_shared_rank(p, b) : p; };  // the same place in another block
+    auto meet = [&]() {
+        if (CLUSTER) cluster.sync();
+        else __syncthreads();
+    };
+    pdl_go();
+    if (CLUSTER) cluster.sync();  // (all blocks of the cluster run)
+
+    for (uint64_t r = blockIdx.x >> log_parts; r < q.n_rows; r += step) {
+        const float u = s.uniform[r];
+        if (!drawn_at_all(u)) {
+            if (part == 0 && tid == 0) {
+                put_sample(o, r, -1, 0.0f, 0.0f, 0);
+                s.left[r] = 0;
+            }
+            continue;
+        }
+        const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
+        const RowMask mask = row_mask(q, r);
+        // the block's part of the row, and the warp's run of that, in vectors
+        const uint32_t per_part = (x.n + parts - 1) >> log_parts;
+        const uint32_t p0 = min(x.n, part * per_part), p1 = min(x.n, p0 + per_part);
+        const uint32_t per = ((p1 - p0 + LD_WARPS - 1) / LD_WARPS + 7) & ~7u;
+        const uint32_t v0 = min(p1, p0 + warp * per), v1 = min(p1, v0 + per);
+        const uint32_t steps = (v1 - v0 + LD_STEP - 1) / LD_STEP;
+        const uint32_t seg_steps = ((per + LD_STEP - 1) / LD_STEP + LD_SEGS - 1) / LD_SEGS;  // the same in every warp of the block
+        // a vector that reaches into a neighbouring row is copied whole (and not taken from there), one that may reach out of the matrix is not
+        const uint32_t lo = r == 0 && x.lead ? 1u : 0u, hi = r == q.n_rows - 1 ? (x.lead + x.V) / EPV<T> : x.n;
+        uint32_t in = 0, slot_in = 0, slot_out = 0;
+        auto copy_step = [&]() {
+            if (in < steps) {
+                const uint32_t v = v0 + in * LD_STEP + lane, to = ring + slot_in * (U * NT * 16);
+#pragma unroll
+                for (uint32_t j = 0; j < U; ++j)
+                    if (v + 32 * j < v1 && v + 32 * j >= lo && v + 32 * j < hi) ld_copy(to + j * (NT * 16), x.at(v + 32 * j));
+                slot_in = slot_in + 1 == RING ? 0 : slot_in + 1;
+                ++in;
+            }
+            ld_close();
+        };
+#pragma unroll 1
+        for (uint32_t i = 0; i < RING - 1; ++i) copy_step();
+
+        // the warp's reference; the lane's largest logit, the smallest of its groups', its possible entries
+        float ref = -inf, limit = -inf, most = -inf, least = inf;
+        double total = 0.0;
+        uint32_t at_step = 0, count = 0;
+#pragma unroll 1
+        for (uint32_t seg = 0; seg < LD_SEGS; ++seg) {
+            float group = -inf;
+            const uint32_t end = min(steps, at_step + seg_steps);
+#pragma unroll 1
+            for (; at_step < end; ++at_step) {
+                ld_wait<RING - 2>();
+                const uint32_t first = v0 + at_step * LD_STEP, v = first + lane;
+                const uint4 *slot = s_ring + slot_out * (U * NT) + tid;
+                slot_out = slot_out + 1 == RING ? 0 : slot_out + 1;
+                uint4 raw[U];
+                const bool whole = first + LD_STEP <= v1 && (first > 0 || x.lead == 0) && first + LD_STEP <= (x.lead + x.V) / EPV<T>;
+#pragma unroll
+                for (uint32_t j = 0; j < U; ++j) {
+                    const uint32_t w = v + 32 * j;
+                    raw[j] = slot[j * NT];
+                    if (!whole) {
+                        if (w >= v1) raw[j] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+                        else if (!x.whole(w)) raw[j] = x.part(w);
+                    }
+                    if (MASKED) close_entries<T>(raw[j], w < v1 ? mask.closed_from(x.first(w), EPV<T>) : 0u);
+                }
+                copy_step();
+                const float m = vectors_max<(int)U>(raw, T{});
+                group = fmaxf(group, m);
+                if (__any_sync(0xffffffffu, m > limit)) {
+                    const float top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(m)));
+                    limit = top + margin;
+                    if (top * c > -FAR_OUT) {  // (below, every power of two is 0 as it is)
+                        total *= ref == -inf ? 0.0 : (double)ex2(step_down(ref, top, c));
+                        ref = top;
+                    }
+                }
+                const float b = ref == -inf ? 0.0f : -__fmul_rn(ref, c);
+                const f32x2 c2 = both(c, c), low = both(b, b);
+                f32x2 acc[U];
+#pragma unroll
+                for (uint32_t j = 0; j < U; ++j) {
+                    float e[EPV<T>];
+                    unpack(raw[j], e, T{});
+                    acc[j] = 0ull;
+#pragma unroll
+                    for (int i = 0; i < EPV<T>; i += 2) {
+                        float y0, y1;
+                        apart(fma2(both(e[i], e[i + 1]), c2, low), y0, y1);
+                        acc[j] = add2(acc[j], both(ex2(y0), ex2(y1)));
+                        if (!RULES) count += (e[i] > -inf) + (e[i + 1] > -inf);
+                    }
+                }
+                float a0, a1;
+                apart(add2(add2(acc[0], acc[1]), add2(acc[2], acc[3])), a0, a1);
+                total += (double)(a0 + a1);
+            }
+            most = fmaxf(most, group);
+            if (RULES) {
+                if (group > -inf) least = fminf(least, group);
+                from_f32(s_most[RULES ? seg : 0][RULES ? tid : 0], group);
+            } else {
+#pragma unroll
+                for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+                if (lane < parts) {
+                    *away(&s_sum[RULES ? 0 : part * RECS + warp * LD_SEGS + seg], lane) = total;
+                    *away(&s_ref[RULES ? 0 : part * RECS + warp * LD_SEGS + seg], lane) = ref;
+                }
+                total = 0.0;
+            }
+        }
+        ld_wait<0>();
+        most = from_ordered(__reduce_max_sync(0xffffffffu, ordered(most)));
+        if (RULES) {
+            least = from_ordered(__reduce_min_sync(0xffffffffu, ordered(least)));
+#pragma unroll
+            for (int d = 16; d; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+        } else {
+            count = __reduce_add_sync(0xffffffffu, count);
+        }
+        if (lane < parts) {
+            const uint32_t at = part * LD_WARPS + warp;
+            *away(&s_max[at], lane) = most;
+            if (RULES) {
+                *away(&s_min[at], lane) = least;
+                *away(&s_sum[at], lane) = total;
+                *away(&s_ref[at], lane) = ref;
+            } else {
+                *away(&s_count[at], lane) = count;
+            }
+        }
+        if (RULES) {
+            if (tid < LD_BINS) s_bins[RULES ? tid : 0] = s_mass[RULES ? tid : 0] = 0;
+            if (tid < 2) s_n[tid] = 0;
+        }
+        meet();
+
+        // M and S relative to it, the same in every thread
+        float M = -inf, low = inf;
+        count = 0;
+        for (uint32_t w = 0; w < parts * LD_WARPS; ++w) {
+            M = fmaxf(M, s_max[w]);
+            if (RULES) low = fminf(low, s_min[w]);
+            else count += s_count[w];
+        }
+        const double cM = (double)c * (double)M;
+        auto relative = [&](uint32_t i) {  // (a warp's sums are relative to its rounded product)
+            return s_ref[i] == -inf ? 0.0 : s_sum[i] * exp2((double)__fmul_rn(s_ref[i], c) - cM);
+        };
+        double S = 0.0;
+        for (uint32_t i0 = 0; i0 < parts * RECS; i0 += 32) {
+            double v = i0 + lane < parts * RECS ? relative(i0 + lane) : 0.0;
+#pragma unroll
+            for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+            S += v;
+        }
+        bool settled = false;
+        if (M == -inf && S == 0.0) {
+            if (part == 0 && tid == 0) put_sample(o, r, -1, -inf, -inf, 0);
+            settled = true;
+        } else if (S > 0.0 && S < 1e300 && !far_out(M, c)) {
+            const double eps = (20.0 + 1.4 * log2((double)q.V / S)) * (1.0 / 16777216.0);
+            const float L = max_nan((float)log(S), 0.0f);
+            if (!RULES) {
+                // the segment that the number falls into, and what lies in front of it
+                const double at = (double)u * S;
+                double before = 0.0;
+                uint32_t mine = 0xFFFFFFFFu;
+                for (uint32_t i0 = 0; i0 < parts * RECS && mine == 0xFFFFFFFFu; i0 += 32) {
+                    const double own = relative(i0 + lane);
+                    double up = own;
+#pragma unroll
+                    for (int d = 1; d < 32; d *= 2) {
+                        const double v = __shfl_up_sync(0xffffffffu, up, d);
+                        if (lane >= (uint32_t)d) up += v;
+                    }
+                    const uint32_t past = __ballot_sync(0xffffffffu, before + up > at);
+                    const uint32_t f = past ? __ffs(past) - 1 : 31;
+                    if (past) mine = i0 + f;
+                    const double front = __shfl_sync(0xffffffffu, past ? up - own : up, f);
+                    before += front;
+                }
+                if (mine == 0xFFFFFFFFu) mine = 0;  // (not found: nothing is found there either)
+                if (mine / RECS == part) {  // its block reads it again, in the order of the numbers
+                    if (tid == 0) s_found[0] = 0;
+                    __syncthreads();
+                    const uint32_t w = mine % RECS / LD_SEGS, a = min(p1, p0 + w * per), b = min(p1, a + per);
+                    const uint32_t from = min(b, a + (mine % LD_SEGS) * seg_steps * LD_STEP), to = min(b, from + seg_steps * LD_STEP);
+                    const double back = exp2((double)__fmul_rn(M, c) - cM), slack = 0.5 * eps * S;
+                    for (uint32_t w0 = from; w0 < to; w0 += NT) {
+                        const uint32_t v = w0 + tid;
+                        uint4 raw = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+                        if (v < to) raw = open_vector<T, MASKED>(x, mask, v);
+                        float xs[EPV<T>], e[EPV<T>];
+                        unpack(raw, xs, T{});
+                        powers<T>(xs, M, c, false, e);
+                        const double own = (double)sum_of(e) * back;
+                        double up = own;
+#pragma unroll
+                        for (int d = 1; d < 32; d *= 2) {
+                            const double t = __shfl_up_sync(0xffffffffu, up, d);
+                            if (lane >= (uint32_t)d) up += t;
+                        }
+                        if (lane == 31) s_four[warp] = up;
+                        __syncthreads();
+                        double front = before;
+                        for (uint32_t k = 0; k < LD_WARPS; ++k) {
+                            if (k < warp) front += s_four[k];
+                            before += s_four[k];
+                        }
+                        double cum = front + (up - own);
+                        if (cum <= at && front + up > at) {
+#pragma unroll
+                            for (int i = 0; i < EPV<T>; ++i) {
+                                const double next = cum + (double)e[i] * back;
+                                if (cum <= at && next > at && at >= cum + slack && next >= at + slack) {
+                                    const float lp = min_nan(log_odds(xs[i], M, q.scale) - L, 0.0f);
+                                    put_sample(o, r, (int64_t)x.first(v) + i, lp, lp, count);
+                                    s_found[0] = 1;
+                                }
+                                cum = next;
+                            }
+                        }
+                        __syncthreads();
+                        if (before > at) break;
+                    }
+                    if (tid == 0) s.left[r] = s_found[0] ? 0 : 1;
+                }
+                meet();
+                continue;
+            }
+            // the bound
+            const float range = fminf(M - low, 64.0f / q.scale), width = range * (1.0f / LD_BINS);
+            const float each = width > 1e-30f ? 1.0f / width : 0.0f;
+            if (s.top_k || s.top_p < 1.0) {
+#pragma unroll 1
+                for (uint32_t seg = 0; seg < LD_SEGS; ++seg) {
+                    const float d = M - to_f32(s_most[RULES ? seg : 0][RULES ? tid : 0]);
+                    if (d <= range) {
+                        const uint32_t bin = RULES ? min(LD_BINS - 1, (uint32_t)(d * each)) : 0;
+                        atomicAdd(&s_bins[bin], 1u);
+                        if (!s.top_k) atomicAdd(&s_mass[bin], (uint32_t)(ex2(-d * c) * 0x1p18f));
+                    }
+                }
+            }
+            meet();
+            const float from = fmaxf(__double2float_ru((double)M + h.drop), LOWEST);  // of min_p
+            if (warp == 0) {
+                float bound = LOWEST;
+                if (s.top_k || s.top_p < 1.0) {
+                    constexpr uint32_t PER = LD_BINS / 32;
+                    uint32_t n[PER], m[PER], n_own = 0, m_own = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < PER; ++i) {
+                        n[i] = m[i] = 0;
+                        for (uint32_t p = 0; p < parts; ++p) {
+                            n[i] += *away(&s_bins[RULES ? lane * PER + i : 0], p);
+                            m[i] += *away(&s_mass[RULES ? lane * PER + i : 0], p);
+                        }
+                        n_own += n[i];
+                        m_own += m[i];
+                    }
+                    uint32_t n_up = n_own, m_up = m_own;
+#pragma unroll
+                    for (int d = 1; d < 32; d *= 2) {
+                        const uint32_t a = __shfl_up_sync(0xffffffffu, n_up, d), b = __shfl_up_sync(0xffffffffu, m_up, d);
+                        if (lane >= (uint32_t)d) { n_up += a; m_up += b; }
+                    }
+                    n_up -= n_own;
+                    m_up -= m_own;
+                    const float need = (float)(s.top_p * S) * 0x1p18f;
+                    // no group counted in a bin or above it has a largest logit below the bin's lower end
+                    auto end_of = [&](uint32_t bin) { return M - (float)(bin + 1) * width * (1.0f + 0x1p-20f) - fabsf(M) * 0x1p-22f; };
+                    float sure = -inf, guess = -inf;
+#pragma unroll
+                    for (uint32_t i = 0; i < PER; ++i) {
+                        n_up += n[i];
+                        m_up += m[i];
+                        if (sure == -inf && (s.top_k ? n_up >= s.top_k : (float)m_up >= need)) sure = end_of(lane * PER + i);
+                        if (guess == -inf && n_up >= LD_GUESS) guess = end_of(lane * PER + i);
+                    }
+                    // the weights of a group's other entries are not counted: where the largest ones alone are not enough, what reaches the
+                    // LD_GUESS-th may be
+                    uint32_t reached = __ballot_sync(0xffffffffu, sure > -inf);
+                    if (!reached && !s.top_k) {
+                        reached = __ballot_sync(0xffffffffu, guess > -inf);
+                        sure = guess;
+                    }
+                    if (reached) bound = fmaxf(__shfl_sync(0xffffffffu, sure, __ffs(reached) - 1), LOWEST);
+                }
+                // (with both, the first top_k are listed whole: top_p is of their sum)
+                if (!(s.top_k && s.top_p < 1.0)) bound = fmaxf(bound, from);
+                if (lane == 0) s_bound = bound;
+            }
+            __syncthreads();
+            const float bound = s_bound;
+            const bool all = s.min_p == 0.0 || bound != from;  // (else min_p decides what is listed)
+            // the groups that reach it, and of these the entries
+            uint16_t *const groups = reinterpret_cast<uint16_t *>(buffer + LD_GROUPS_AT);
+#pragma unroll 1
+            for (uint32_t seg = 0; seg < LD_SEGS; ++seg)
+                if (to_f32(s_most[RULES ? seg : 0][RULES ? tid : 0]) >= bound) groups[atomicAdd(&s_n[1], 1u)] = (uint16_t)(seg * NT + tid);
+            __syncthreads();
+            const uint32_t vectors = seg_steps * U, items = s_n[1] * vectors;
+            key_t64 *const list = away(reinterpret_cast<key_t64 *>(buffer), 0);
+            uint32_t *const listed = away(&s_n[0], 0);
+            for (uint32_t i0 = tid; i0 < items; i0 += 4 * NT) {
+                uint4 raw[4];
+                uint32_t at[4];
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const uint32_t item = i0 + k * NT;
+                    raw[k] = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+                    at[k] = 0;
+                    if (item < items) {
+                        const uint32_t id = groups[item / vectors], of = item % vectors, seg = id / NT, t = id % NT;
+                        const uint32_t a = min(p1, p0 + (t >> 5) * per), b = min(p1, a + per);
+                        const uint32_t st = seg * seg_steps + of / U, v = a + st * LD_STEP + (of % U) * 32 + (t & 31);
+                        if (v < b) {
+                            at[k] = v;
+                            raw[k] = open_vector<T, MASKED>(x, mask, v);
+                        }
+                    }
+                }
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    if (!(vector_max(raw[k], T{}) >= bound)) continue;
+                    float e[EPV<T>];
+                    unpack(raw[k], e, T{});
+#pragma unroll
+                    for (int i = 0; i < EPV<T>; ++i)
+                        if (e[i] >= bound) {
+                            const uint32_t place = atomicAdd(listed, 1u);
+                            if (place < LD_CAP) list[place] = rank_key(e[i], (uint32_t)(x.first(at[k]) + i));
+                        }
+                }
+            }
+            meet();
+            if (part == 0 && s_n[0] <= LD_CAP && s_n[0] > 0)
+                settled = draw_listed(buffer, s_n[0], all, q, s, o, r, u, M, S, eps, from, L, s_four, s_found);
+        }
+        if (part == 0 && tid == 0) s.left[r] = !settled;
+        meet();
+    }
+}
+
+// The rows that were left, each to a cluster of blocks, which works them out in 64 bits.
+constexpr uint32_t RS_THREADS = 512;
+template <typename T>
+__global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, const SampleRules s, const SampleOut o, uint32_t log_parts)
+{
+    __shared__ TeamMemory<RS_THREADS> mem;
+    __shared__ uint32_t s_warp[RS_THREADS / 32], s_row[RS_THREADS];
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
+    const uint32_t clusters = gridDim.x >> log_parts, me = blockIdx.x >> log_parts;
+    if (tid < EXP_TABLE) mem.table[tid] = exp2((double)tid / EXP_TABLE);
+    uint64_t number = 0;  // of rows left so far: cluster b takes every clusters-th from b on
+    pdl_wait();
+    if (parts > 1) cg::this_cluster().sync();  // (all blocks of the cluster run)
+    else __syncthreads();
+    for (uint64_t base = 0; base < q.n_rows; base += RS_THREADS) {
+        const bool left = base + tid < q.n_rows && s.left[base + tid];
+        const uint32_t some = __ballot_sync(0xffffffffu, left);
+        if (!__syncthreads_or(some)) continue;
+        if (lane == 0) s_warp[warp] = __popc(some);
+        __syncthreads();
+        uint32_t front = __popc(some & ((1u << lane) - 1)), all = 0;
+        for (uint32_t w = 0; w < RS_THREADS / 32; ++w) {
+            if (w < warp) front += s_warp[w];
+            all += s_warp[w];
+        }
+        // the first of these that is the cluster's, and how many are; in the same order in each of its blocks
+        const uint32_t skip = (uint32_t)((me + clusters - number % clusters) % clusters), n = all > skip ? (all - skip - 1) / clusters + 1 : 0;
+        if (left && front >= skip && (front - skip) % clusters == 0) s_row[(front - skip) / clusters] = tid;
+        number += all;
+        __syncthreads();
+        for (uint32_t i = 0; i < n; ++i) {
+            sample_row_64<T, RS_THREADS>(q, s, o, base + s_row[i], &mem, parts, part);
+            if (parts > 1) cg::this_cluster().sync();  // (the next row's first sums may go where this row's last ones are read)
+            else __syncthreads();
+        }
+    }
+}
+
+template <typename T, bool MASKED, bool RULES, bool CLUSTER>
+cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, uint32_t log_parts, int device,
+                            cudaStream_t st)
+{
+    constexpr auto kernel = k_sample_long<T, MASKED, RULES, CLUSTER>;
+    const cudaError_t e = allow_smem<kernel, (int)LD_RING_BYTES>(device);
+    if (e != cudaSuccess) return e;
+    const uint32_t parts = 1u << log_parts;
+    cudaLaunchAttribute at{};
+    at.id = cudaLaunchAttributeClusterDimension;
+    at.val.clusterDim.x = parts;
+    at.val.clusterDim.y = at.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.blockDim = LD_THREADS; cfg.dynamicSmemBytes = LD_RING_BYTES; cfg.stream = st;
+    cfg.attrs = &at; cfg.numAttrs = CLUSTER ? 1 : 0;
+    const uint64_t most = (8 * (uint64_t)vl_device_sm_count(device)) >> log_parts;
+    cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
+    g_vl_launches.fetch_add(1);
+    return cudaLaunchKernelEx(&cfg, kernel, q, s, o, h, log_parts);
+}
+
+template <typename T, bool MASKED, bool RULES>
+cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, int device, cudaStream_t st)
+{
+    const uint64_t resident = 8 * (uint64_t)vl_device_sm_count(device);
+    const uint32_t n = q.V / EPV<T>;
+    uint32_t log_parts = 0;
+    if (n >= 2048)
+        while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= (n >> (log_parts + 1) > 2048 ? resident : resident * 2 / 5)) ++log_parts;
+    const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true>(q, s, o, h, log_parts, device, st)
+                                    : run_sample_long<T, MASKED, RULES, false>(q, s, o, h, 0, device, st);
+    if (e != cudaSuccess) return e;
+    // few rows: more blocks at each; short ones have nothing to share
+    const uint32_t log_rest = n < 1024 ? 0 : q.n_rows <= 8 ? 3 : 2;
+    const uint64_t clusters = (uint64_t)vl_device_sm_count(device) >> log_rest;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 1u << log_rest;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((uint32_t)(q.n_rows < clusters ? q.n_rows : clusters) << log_rest);
+    cfg.blockDim = RS_THREADS; cfg.stream = st;
+    cfg.attrs = at; cfg.numAttrs = 2;
+    g_vl_launches.fetch_add(1);
+    return cudaLaunchKernelEx(&cfg, k_sample_rest<T>, q, s, o, log_rest);
+}
+
+}  // namespace

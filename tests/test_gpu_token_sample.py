@@ -221,11 +221,61 @@ def test_outputs_are_written_and_nothing_else(B):
         rules = B.vl_sampling(5, 1.0, 0.0)
         outs = [torch.full((R + 8,), 77, device="cuda", dtype=t) for t in (torch.int32, torch.float32, torch.float32, torch.int32)]
         p = [o[4:].data_ptr() for o in outs]
-        assert B._lib.vl_token_sample(0, C.byref(d), C.byref(rules), u.data_ptr(), p[0], 4, p[1], p[2], p[3], None) == B.VL_OK
+        work, size = torch.empty(64, device="cuda", dtype=torch.uint8), 64
+        assert B._lib.vl_token_sample(0, C.byref(d), C.byref(rules), u.data_ptr(), p[0], 4, p[1], p[2], p[3], work.data_ptr(), size, None) == B.VL_OK
         torch.cuda.synchronize()
         for o, wanted in zip(outs, want):
             assert torch.equal(o[4:-4], wanted.to(o.dtype)) and bool((o[:4] == 77).all()) and bool((o[-4:] == 77).all())
         again = torch.empty(R, device="cuda", dtype=torch.int32)
-        assert B._lib.vl_token_sample(0, C.byref(d), C.byref(rules), u.data_ptr(), again.data_ptr(), 4, None, None, None, None) == B.VL_OK
+        assert B._lib.vl_token_sample(0, C.byref(d), C.byref(rules), u.data_ptr(), again.data_ptr(), 4, None, None, None, work.data_ptr(), size, None) == B.VL_OK
         torch.cuda.synchronize()
         assert torch.equal(again, want.tokens)
+
+
+def _peaked(gen, R, V, dtype):
+    """Rows of a model: few favourites, some possible entries, the rest far below; flat ones, one with a single possible favourite, some
+    whose first entries, or all but a few, are shut by large negative logits."""
+    import torch
+    x = torch.randn(R, V, generator=gen, device="cuda") * 2
+    at = torch.randint(0, V, (R, 40), generator=gen, device="cuda")
+    x.scatter_(1, at, torch.rand(R, 40, generator=gen, device="cuda") * 8 + 8)
+    x[::7] = torch.randn(V, generator=gen, device="cuda")
+    x[1::7, V // 2] = 60.0
+    x[2::7, : V - V // 3] = torch.finfo(dtype).min
+    x[3::7, 50:] = -1e4
+    x[4::7, ::2] = -float("inf")
+    return x.to(dtype)
+
+
+@pytest.mark.parametrize("R,V,dtype", [(1, 131072, "bf16"), (3, 100003, "f16"), (20, 65536, "f32"), (150, 32768, "f16"), (600, 16000, "bf16"),
+                                       (1300, 8200, "f32"), (2000, 2100, "bf16")])
+def test_rows_of_a_model(B, R, V, dtype):
+    """Against sorting on the device in 64 bits, and the same again when called again."""
+    import torch
+    kind = B._Torch.load() and {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(R + V)
+    x = _peaked(gen, R, V, kind)
+    u = torch.rand(R, generator=gen, device="cuda")
+    xd = x.double()
+    w = torch.exp((xd - xd.amax(1, keepdim=True)) * float(np.float32(1.1)))
+    order = torch.sort(x.float(), dim=1, descending=True, stable=True).indices
+    ws = w.gather(1, order)
+    possible = (xd > -np.inf).gather(1, order)
+    for rules in RULES + [dict(top_k=50), dict(top_k=1500, top_p=0.9), dict(top_p=0.5), dict(min_p=0.3, top_p=0.95), dict(min_p=1e-9)]:
+        got = B.vl_token_sample(x, u, scale=1.1, **rules)
+        keep = possible & (torch.arange(V, device="cuda")[None] < (rules.get("top_k") or V))
+        sums = torch.cumsum(ws * keep, 1)
+        if rules.get("top_p", 1.0) < 1.0:
+            keep = keep & torch.cat([torch.ones_like(keep[:, :1]), (sums < rules["top_p"] * sums[:, -1:])[:, :-1]], 1)
+        keep = keep & (ws >= rules.get("min_p", 0.0))
+        here = torch.zeros_like(keep).scatter(1, order, keep)
+        sums = torch.cumsum(w * here, 1)
+        T = sums[:, -1:]
+        tok = torch.searchsorted(sums, u[:, None].double() * T, right=True)
+        assert torch.equal(got.kept.long(), keep.sum(1)), rules
+        assert torch.equal(got.tokens, tok[:, 0]), rules
+        z = torch.log(w.gather(1, tok)[:, 0])
+        for a, b in ((got.logprob, z - torch.log(w.sum(1))), (got.drawn_logprob, z - torch.log(T[:, 0]))):
+            assert bool(((a.double() - b).abs() <= _sum_error(V) + 3 * U * 3 * (z.abs() + 20)).all()), rules
+        again = B.vl_token_sample(x, u, scale=1.1, **rules)
+        assert all(torch.equal(a, b) for a, b in zip(got, again)), rules

@@ -19,22 +19,22 @@ def _logits(B, **change):
 def test_bad_draws(B):
     nan, inf = float("nan"), float("inf")
 
-    def call(rules=(0, 1.0, 0.0), uniform=4096, tokens=4096, size=8, lp=4096, drawn=None, kept=None, **change):
+    def call(rules=(0, 1.0, 0.0), uniform=4096, tokens=4096, size=8, lp=4096, drawn=None, kept=None, work=4096, bytes_=64, **change):
         d = _logits(B, **change)
         r = None if rules is None else C.byref(B.vl_sampling(*rules))
-        return B._lib.vl_token_sample(0, C.byref(d), r, uniform, tokens, size, lp, drawn, kept, None)
+        return B._lib.vl_token_sample(0, C.byref(d), r, uniform, tokens, size, lp, drawn, kept, work, bytes_, None)
 
     bad = B.VL_ERR_INVALID_ARG
     for rules in (None, (0, 0.0, 0.0), (0, -0.5, 0.0), (0, 1.0001, 0.0), (0, nan, 0.0), (0, 1.0, -0.1), (0, 1.0, 1.5), (0, 1.0, nan), (0, inf, 0.0)):
         assert call(rules) == bad, rules
     for change in (dict(uniform=None), dict(uniform=4097), dict(tokens=None), dict(tokens=4100), dict(size=1), dict(size=0), dict(size=16),
-                   dict(size=2, tokens=4097), dict(lp=4097), dict(drawn=4098), dict(kept=4097), dict(scale=0.0), dict(scale=nan), dict(logits=None),
+                   dict(size=2, tokens=4097), dict(lp=4097), dict(work=None), dict(bytes_=1), dict(drawn=4098), dict(kept=4097), dict(scale=0.0), dict(scale=nan), dict(logits=None),
                    dict(row_stride=39), dict(dtype=7), dict(n_vocab=0), dict(size=2, n_vocab=65536, row_stride=65536)):
         assert call(**change) == bad, change
     d = _logits(B, tokens=4096, token_bytes=8)
-    assert B._lib.vl_token_sample(0, C.byref(d), C.byref(B.vl_sampling(0, 1.0, 0.0)), 4096, 4096, 8, None, None, None, None) == bad
-    assert B._lib.vl_token_sample(0, None, C.byref(B.vl_sampling(0, 1.0, 0.0)), 4096, 4096, 8, None, None, None, None) == bad
-    assert call(n_rows=0, logits=None, uniform=None, tokens=None, lp=None) == B.VL_OK
+    assert B._lib.vl_token_sample(0, C.byref(d), C.byref(B.vl_sampling(0, 1.0, 0.0)), 4096, 4096, 8, None, None, None, 4096, 64, None) == bad
+    assert B._lib.vl_token_sample(0, None, C.byref(B.vl_sampling(0, 1.0, 0.0)), 4096, 4096, 8, None, None, None, 4096, 64, None) == bad
+    assert call(n_rows=0, logits=None, uniform=None, tokens=None, lp=None, work=None) == B.VL_OK
 
 
 def _tensors(B, *items):
