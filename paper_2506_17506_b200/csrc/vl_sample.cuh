@@ -76,7 +76,7 @@ __device__ __forceinline__ double exp_below_1(double z, const double *table)
 
 // The threads at a row that they read as often as they need it: a warp (NT = 32), or `parts` blocks of a cluster.  Each warp has a run of the
 // row's vectors.  All threads hold the same results; every sum has one order.
-constexpr uint32_t TEAM_PARTS = 8;
+constexpr uint32_t TEAM_PARTS = 8, TEAM_HELD = 16;  // blocks; vectors of a thread that stay in shared memory
 template <int NT>
 struct TeamMemory {
     static constexpr uint32_t NW = NT / 32, ALL = NT == 32 ? 1 : TEAM_PARTS * NW;
@@ -149,7 +149,7 @@ struct Team {
 
 template <typename T, int NT>
 __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules &rules, const SampleOut &o, uint64_t r, TeamMemory<NT> *mem,
-                                           uint32_t parts, uint32_t part)
+                                           uint4 *held, uint32_t parts, uint32_t part)
 {
     Team<NT> team{mem, parts, part, 0};
     typedef typename Team<NT>::Three Three;
@@ -163,37 +163,45 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         if (v >= v1) return make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
         return masked ? open_vector<T, true>(x, mask, v) : open_vector<T, false>(x, mask, v);
     };
-    auto each = [&](float from, auto &&f) {  // f(entry, number) of the possible entries of vectors that have one of at least `from`
-        for (uint32_t w = v0; w < v1; w += 64) {  // two at a time: the second one's load does not wait for the first one's work
-            const uint4 raw[2] = {vector(w + lane), vector(w + 32 + lane)};
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if (!(vector_max(raw[k], T{}) >= from)) continue;
-                float e[EPV<T>];
-                unpack(raw[k], e, T{});
-#pragma unroll
-                for (int i = 0; i < EPV<T>; ++i)
-                    if (e[i] > -inf) f(e[i], x.first(w + 32 * k + lane) + i);
-            }
-        }
+    // the first vectors of a lane are copied into its places of shared memory, if there are any, with what is closed taken out
+    if (NT > 32) {
+#pragma unroll 4
+        for (uint32_t k = 0; k < TEAM_HELD; ++k)
+            if (v0 + 32 * k < v1) held[k * NT + threadIdx.x] = vector(v0 + 32 * k + lane);
+    }
+    auto each_vector = [&](auto &&f) {
+#pragma unroll 1
+        for (uint32_t w = v0, k = 0; w < v1; w += 32, ++k) f(NT > 32 && k < TEAM_HELD ? held[k * NT + threadIdx.x] : vector(w + lane));
     };
-    // the largest, how many there are, and whether something is no number
-    uint32_t most = 0, bad = 0, n = 0;
-    for (uint32_t w = v0; w < v1; w += 32) {
+    auto each = [&](float from, auto &&f) {  // f(entry) of the possible entries of vectors that have one of at least `from`
+        each_vector([&](const uint4 &raw) {
+            if (!(vector_max(raw, T{}) >= from)) return;
+            float e[EPV<T>];
+            unpack(raw, e, T{});
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i)
+                if (e[i] > -inf) f(e[i]);
+        });
+    };
+    // the largest and the smallest, how many there are, and whether something is no number (then the smallest is 0)
+    uint32_t most = 0, least = 0xFFFFFFFFu, n = 0;
+    each_vector([&](const uint4 &raw) {
         float e[EPV<T>];
-        unpack(vector(w + lane), e, T{});
+        unpack(raw, e, T{});
 #pragma unroll
         for (int i = 0; i < EPV<T>; ++i) {
-            if (!(e[i] < inf)) bad = 1;
-            if (e[i] > -inf) { most = max(most, ordered(e[i])); ++n; }
+            const uint32_t key = e[i] < inf ? ordered(e[i]) : 0u;
+            if (key >= LEAST_KEY) { most = max(most, key); ++n; }
+            if (key != LEAST_KEY - 1) least = min(least, key);
         }
-    }
-    const Three first = team.three({n, bad ? 0u : 1u, most});
+    });
+    const Three first = team.three({n, least, most});
     n = first.sum;
     most = first.most;
+    least = first.least;
     const bool leader = part == 0 && (NT == 32 ? lane == 0 : threadIdx.x == 0);
-    if (first.least == 0 || n == 0) {
-        const float v = first.least == 0 ? __int_as_float(0x7fc00000) : -inf;
+    if (least == 0 || n == 0) {
+        const float v = least == 0 ? __int_as_float(0x7fc00000) : -inf;
         if (leader) put_sample(o, r, -1, v, v, 0);
         return;
     }
@@ -202,80 +210,308 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         const double z = scale * ((double)v - M);
         return NT == 32 ? exp(z) : exp_below_1(z, mem->table);
     };
-
-    // all of them
-    double S = 0.0;
-    each(-inf, [&](float v, int) { S += weight(v); });
-    S = team.sum(S);
-
-    // kept: entries whose key is above `cut`, and the first `ties` of those equal to it
-    uint32_t cut = LEAST_KEY - 1, ties = 0;
-    double among = S;  // sum over these
-    auto halve = [&](uint32_t lo, uint32_t hi) {  // between the values, so that it comes near to where they are
-        const uint32_t mid = ordered(0.5f * from_ordered(max(lo, LEAST_KEY)) + 0.5f * from_ordered(hi - 1));
-        return min(max(mid, lo + 1), hi - 1);
-    };
-    if (rules.top_k && rules.top_k < n) {
-        // the largest key that top_k entries reach: at least lo, below hi, which `above` entries reach
-        uint32_t lo = LEAST_KEY - 1, hi = most + 1, above = 0;
-        while (hi - lo > 1) {
-            const uint32_t mid = halve(lo, hi);
-            const float at_lo = from_ordered(max(lo, LEAST_KEY)), at_mid = from_ordered(mid), at_hi = from_ordered(hi - 1);
-            Three t{0u, 0xFFFFFFFFu, 0u};
-            each(at_lo, [&](float v, int) {
-                if (v > at_hi || v < at_lo) return;
-                if (v >= at_mid) { ++t.sum; t.least = min(t.least, ordered(v)); }
-                else t.most = max(t.most, ordered(v));
-            });
-            t = team.three(t);
-            if (above + t.sum >= rules.top_k) {
-                lo = t.least;
-            } else {
-                above += t.sum;
-                hi = max(t.most, lo) + 1;
-            }
-        }
-        cut = lo;
-        ties = rules.top_k - above;
-        const float level = from_ordered(cut);
+    // sum over the entries that `in` takes, of vectors that have one of at least `from`
+    auto add = [&](float from, auto &&in) {
         double sum = 0.0;
-        each(level, [&](float v, int) { if (v > level) sum += weight(v); });
-        among = team.sum(sum) + (double)ties * weight(level);
+        each_vector([&](const uint4 &raw) {
+            if (!(vector_max(raw, T{}) >= from)) return;
+            float e[EPV<T>];
+            unpack(raw, e, T{});
+            double part[EPV<T>];
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i) part[i] = weight(in(e[i]) ? e[i] : -inf);
+#pragma unroll
+            for (int k = EPV<T> / 2; k; k /= 2)
+#pragma unroll
+                for (int i = 0; i < k; ++i) part[i] += part[i + k];
+            sum += part[0];
+        });
+        return sum;
+    };
+
+    // Sixteen sums of every thread's own, which lie behind the held vectors, over all threads: bin k, and the bins up to it, in lane k (and 0 and
+    // all of them in the lanes from 16 on).  A warp of each block adds up a bin.
+    auto bins_up = [&](auto type, double *v, double *up) {
+        __syncthreads();
+        const decltype(type) *const bin = reinterpret_cast<const decltype(type) *>(held + TEAM_HELD * NT) + (threadIdx.x >> 5) * NT + lane;
+        double sum = 0.0;
+#pragma unroll
+        for (uint32_t k = 0; k < NT / 32; ++k) sum += (double)bin[32 * k];
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        double *const d = mem->d[team.turn++ & 1];
+        team.tell(d + warp, sum);
+        team.meet();
+        sum = 0.0;
+        for (uint32_t p = 0; p < parts; ++p) sum += lane < 16 ? d[p * Team<NT>::NW + lane] : 0.0;
+        *v = *up = sum;
+#pragma unroll
+        for (int k = 1; k < 32; k *= 2) {
+            const double w = __shfl_up_sync(0xffffffffu, *up, k);
+            if (lane >= (uint32_t)k) *up += w;
+        }
+    };
+
+    // Among the keys lo .. hi: the largest whose entries, with those above up to hi and *above, have `need` of weight (or, counted, are as
+    // many); lo - 1 if all of them do not.  *above becomes the weight of what is above it.  need(sum of all) is asked for once.
+    auto search = [&](uint32_t lo, uint32_t hi, bool counted, double *above, auto &&need) -> uint32_t {
+        const uint32_t none = lo - 1;
+        double wanted = 0.0;
+        if constexpr (NT == 32) {
+            const double front = *above;
+            auto reach = [&](uint32_t key) {  // the entries from a key on
+                const float from = from_ordered(key), to = from_ordered(hi);
+                if (!counted) return team.sum(add(from, [&](float v) { return v >= from && v <= to; }));
+                uint32_t c = 0;
+                each(from, [&](float v) { c += v >= from && v <= to; });
+                return (double)__reduce_add_sync(0xffffffffu, c);
+            };
+            const double all = lo > hi ? 0.0 : reach(lo);
+            wanted = need(all);
+            if (front + all < wanted) { *above = front + all; return none; }
+            uint32_t under = hi + 1;  // what its entries and those above reach is not enough
+            while (under - lo > 1) {
+                const uint32_t mid = lo + (under - lo) / 2;
+                const double v = front + reach(mid);
+                if (v >= wanted) lo = mid;
+                else { under = mid; *above = v; }
+            }
+            return lo;
+        } else {
+            // sixteen runs of keys at a time, whose weights every thread adds up for its own entries, a warp of each block for all threads
+            double *const own = reinterpret_cast<double *>(held + TEAM_HELD * NT) + threadIdx.x;
+            bool asked = false;
+            while (!asked || lo < hi) {
+                const uint32_t span = hi - lo;
+                const uint32_t shift = lo > hi || span < 16 ? 0 : 28 - __clz(span);
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) own[k * NT] = 0.0;
+                const float from = from_ordered(lo);
+                if (lo <= hi)
+                    each_vector([&](const uint4 &raw) {
+                        if (!(vector_max(raw, T{}) >= from)) return;
+                        float e[EPV<T>];
+                        unpack(raw, e, T{});
+                        double w[EPV<T>];
+                        uint32_t at[EPV<T>], nearest = 16;
+#pragma unroll
+                        for (int i = 0; i < EPV<T>; ++i) {
+                            const uint32_t key = ordered(e[i]);
+                            at[i] = key < lo || key > hi ? 16u : (hi - key) >> shift;
+                            nearest = min(nearest, at[i]);
+                        }
+                        if (nearest == 16) return;
+#pragma unroll
+                        for (int i = 0; i < EPV<T>; ++i) w[i] = counted ? 1.0 : weight(e[i]);
+#pragma unroll
+                        for (int i = 0; i < EPV<T>; ++i)
+                            if (at[i] < 16) own[at[i] * NT] += w[i];
+                    });
+                double v, up;
+                bins_up(double{}, &v, &up);
+                if (!asked) wanted = need(__shfl_sync(0xffffffffu, up, 31));
+                const double prev = __shfl_up_sync(0xffffffffu, up, 1);
+                const uint32_t past = __ballot_sync(0xffffffffu, lane < 16 && *above + up >= wanted), some = __ballot_sync(0xffffffffu, v > 0.0);
+                if (!past && !asked) {
+                    *above += __shfl_sync(0xffffffffu, up, 31);
+                    return none;
+                }
+                asked = true;
+                // (in a narrower run rounding may leave too little: then what is lowest in it)
+                const uint32_t j = past ? __ffs(past) - 1 : 31 - __clz(some | 1u);
+                *above += __shfl_sync(0xffffffffu, lane ? prev : 0.0, j);
+                const uint32_t next_hi = hi - (j << shift), low = (1u << shift) - 1;
+                lo = next_hi - lo > low ? next_hi - low : lo;
+                hi = next_hi;
+            }
+            return lo;
+        }
+    };
+
+    // kept: entries above the logit `level` (whose key is `cut`), and the first `ties` of those equal to it
+    static_assert(NT == 32 || Team<NT>::NW == 16, "a warp for each of the sixteen runs");
+    uint32_t cut = LEAST_KEY - 1, ties = 0;
+    const bool all = !rules.top_k || rules.top_k >= n, shares = rules.top_p < 1.0;
+    double S = 0.0, need = 0.0;  // sum over the row; what the kept entries have to reach
+    if (!(all && shares) && (rules.top_k || rules.min_p > 0.0)) S = team.sum(add(-inf, [](float) { return true; }));
+    if (!all) {
+        double above = 0.0;
+        cut = search(least, most, true, &above, [&](double) { return (double)rules.top_k; });
+        ties = rules.top_k - (uint32_t)above;
     }
-    if (rules.top_p < 1.0) {
-        const double need = rules.top_p * among;
-        uint32_t lo = cut, hi = most + 1;
-        double above = 0.0;  // sum of what is above hi
-        while (hi - lo > 1) {
-            const uint32_t mid = halve(lo, hi);
-            const float at_lo = from_ordered(lo), at_mid = from_ordered(mid), at_hi = from_ordered(hi - 1);
-            Three t{0u, 0xFFFFFFFFu, 0u};
+    const uint32_t first_cut = cut, first_ties = ties;
+    // a lane's weight and entries above `upto`: what is worked out already of what is kept
+    double high = 0.0;
+    uint32_t high_count = 0;
+    float upto = inf;
+    if (shares) {
+        auto needed = [&](double sum) {
+            if (all) S = sum;
+            else sum += (double)ties * weight(from_ordered(cut));
+            return need = rules.top_p * sum;
+        };
+        double above = 0.0;
+        if (NT == 32 || !all) {
+            cut = search(all ? least : cut + 1, most, false, &above, needed);
+        } else {
+            // Where the cut lies as far as 32 bits tell it: the logits in 2^28 steps below the largest one, sixteen runs of steps at a time.  A sum of
+            // 32-bit terms is within NARROW of its value: (4 + 1.4 |y|) u of a weight, |y| up to 40 for what is not nothing, a thread's
+            // additions to a bin (TEAM_HELD vectors; longer rows are not narrowed down).
+            constexpr double NARROW = 2e-5;
+            const float M32 = from_ordered(most), c = q.scale * LOG2E;
+            const float per = 0x1p28f / fmaxf(fminf(M32 - from_ordered(least), 64.0f / q.scale), 1e-30f);
+            auto step_of = [&](float v) { return (uint32_t)fminf((M32 - v) * per, 0x0.ffffffp28f); };
+            uint32_t lo = 0, hi = (1u << 28) - 1;
+            float *const own = reinterpret_cast<float *>(held + TEAM_HELD * NT) + threadIdx.x;
+            double front = 0.0, wanted = 0.0, slack = 0.0;
+            for (uint32_t shift = 24; x.n <= warps * 32 * TEAM_HELD;) {
+#pragma unroll
+                for (uint32_t k = 0; k < 16; ++k) own[k * NT] = 0.0f;
+                each_vector([&](const uint4 &raw) {
+                    float e[EPV<T>];
+                    unpack(raw, e, T{});
+#pragma unroll
+                    for (int i = 0; i < EPV<T>; ++i) {
+                        const uint32_t t = step_of(e[i]), at = (t - lo) >> shift;
+                        if (t >= lo && t <= hi && e[i] > -inf) own[at * NT] += ex2((e[i] - M32) * c);
+                    }
+                });
+                double v, up;
+                bins_up(float{}, &v, &up);
+                if (shift == 24) {
+                    const double sum = __shfl_sync(0xffffffffu, up, 31);
+                    wanted = rules.top_p * sum;
+                    slack = NARROW * sum;
+                }
+                const double prev = __shfl_up_sync(0xffffffffu, up, 1);
+                const uint32_t perhaps = __ballot_sync(0xffffffffu, lane < 16 && front + up + slack >= wanted);
+                const uint32_t sure = __ballot_sync(0xffffffffu, lane < 16 && front + up - slack >= wanted);
+                const uint32_t a = perhaps ? __ffs(perhaps) - 1 : 15, b = sure ? __ffs(sure) - 1 : 15;
+                front += __shfl_sync(0xffffffffu, lane ? prev : 0.0, a);
+                hi = min(hi, lo + ((b + 1) << shift) - 1);
+                lo += a << shift;
+                // (three times: what is left is one logit of 16 bits, or some hundred of 32)
+                if (shift <= 16 || b - a > 3) break;
+                shift = 28 - __clz(hi - lo);
+            }
+            // in 64 bits: the whole sum, and what is above these steps; and which keys lie in them
             double sum = 0.0;
-            each(at_lo, [&](float v, int) {
-                if (v > at_hi || v <= at_lo) return;
-                if (v >= at_mid) { sum += weight(v); t.least = min(t.least, ordered(v)); }
-                else t.most = max(t.most, ordered(v));
+            Three t{0u, 0xFFFFFFFFu, 0u};
+            each_vector([&](const uint4 &raw) {
+                float e[EPV<T>];
+                unpack(raw, e, T{});
+                double w[EPV<T>];
+#pragma unroll
+                for (int i = 0; i < EPV<T>; ++i) w[i] = weight(e[i]);
+#pragma unroll
+                for (int i = 0; i < EPV<T>; ++i) {
+                    const uint32_t at = step_of(e[i]), key = ordered(e[i]);
+                    sum += w[i];
+                    if (at < lo) { high += w[i]; ++high_count; }
+                    if (at >= lo && at <= hi && e[i] > -inf) { t.least = min(t.least, key); t.most = max(t.most, key); }
+                }
             });
-            sum = above + team.sum(sum);
+            S = team.sum(sum);
+            above = team.sum(high);
             t = team.three(t);
-            if (sum >= need && t.least != 0xFFFFFFFFu) {
-                lo = t.least;
-            } else {
-                above = sum;
-                hi = max(t.most, lo) + 1;
+            need = rules.top_p * S;
+            auto same = [&](double) { return need; };
+            cut = LEAST_KEY - 1;
+            if (above < need && t.most) {
+                upto = from_ordered(t.most);
+                cut = search(t.least, t.most, false, &above, same);
+                if (cut < t.least) cut = t.least > least ? search(least, t.least - 1, false, &above, same) : LEAST_KEY - 1;
+            } else {  // (the margin makes this an error of rounding at most)
+                above = 0.0;
+                high = 0.0;
+                high_count = 0;
+                cut = search(least, most, false, &above, same);
             }
         }
-        // (lo is an entry's key, or the cut that was there)
-        const float level = from_ordered(lo);
-        Three t{0u, 0u, 0u};
-        if (lo != cut) each(level, [&](float v, int) { t.sum += v == level; });
-        const uint32_t there = lo == cut ? ties : team.three(t).sum;
-        const double w = lo < LEAST_KEY ? 0.0 : weight(level);
-        const double m = w > 0.0 ? ceil((need - above) / w) : 1.0;
-        ties = lo == cut && ties == 0 ? 0 : (uint32_t)min(max(m, 1.0), (double)there);
-        cut = lo;
+        if (all && cut < least) cut = LEAST_KEY - 1;
     }
-    if (rules.min_p > 0.0 && (cut < LEAST_KEY || weight(from_ordered(cut)) < rules.min_p)) {
+
+    // what the warps' runs hold above the cut and of ties; a run's ties are kept as far as there are some left
+    double sum = 0.0, total = 0.0, base = 0.0, tie = 0.0;
+    uint32_t count = 0, equal = 0, kept = 0, before = 0, mine = warp;
+    float level = -inf;
+    double *d = nullptr;
+    uint32_t(*su)[3] = nullptr;
+    auto runs = [&](auto &&f) {  // f(first run, kept weight of a lane's run, of the runs up to it, ties in front of it, entries above the cut)
+        uint32_t front = 0;
+        for (uint32_t w0 = 0; w0 < warps; w0 += 32) {
+            const bool there = w0 + lane < warps;
+            const uint32_t e = there ? su[w0 + lane][1] : 0u;
+            uint32_t up = e;
+#pragma unroll
+            for (int k = 1; k < 32; k *= 2) {
+                const uint32_t v = __shfl_up_sync(0xffffffffu, up, k);
+                if (lane >= (uint32_t)k) up += v;
+            }
+            const uint32_t b = front + up - e;
+            front += __shfl_sync(0xffffffffu, up, 31);
+            const double own = there ? d[w0 + lane] + (double)min(e, ties - min(ties, b)) * tie : 0.0;
+            double incl = own;
+#pragma unroll
+            for (int k = 1; k < 32; k *= 2) {
+                const double v = __shfl_up_sync(0xffffffffu, incl, k);
+                if (lane >= (uint32_t)k) incl += v;
+            }
+            f(w0, own, incl, b, there ? su[w0 + lane][0] : 0u);
+        }
+        return front;
+    };
+    for (bool by_min = false;;) {
+        level = cut < LEAST_KEY ? -inf : from_ordered(cut);
+        sum = high;
+        count = high_count;
+        equal = 0;
+        each_vector([&](const uint4 &raw) {
+            float e[EPV<T>];
+            unpack(raw, e, T{});
+            uint32_t in = 0;
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i) {
+                in += e[i] > level && e[i] <= upto;
+                equal += e[i] == level && level > -inf;
+            }
+            count += in;
+            if (!in) return;
+            double part[EPV<T>];
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i) part[i] = weight(e[i] > level && e[i] <= upto ? e[i] : -inf);
+#pragma unroll
+            for (int k = EPV<T> / 2; k; k /= 2)
+#pragma unroll
+                for (int i = 0; i < k; ++i) part[i] += part[i + k];
+            sum += part[0];
+        });
+#pragma unroll
+        for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+        count = __reduce_add_sync(0xffffffffu, count);
+        equal = __reduce_add_sync(0xffffffffu, equal);
+        double above = sum;
+        uint32_t there = equal;
+        tie = 0.0;
+        if (NT > 32) {
+            d = mem->d[team.turn & 1];
+            su = mem->u[team.turn++ & 1];
+            team.tell(d + warp, sum);
+            team.tell(&su[warp][0], count);
+            team.tell(&su[warp][1], equal);
+            team.meet();
+            above = 0.0;
+            there = runs([&](uint32_t, double, double incl, uint32_t, uint32_t) { above += __shfl_sync(0xffffffffu, incl, 31); });
+        }
+        if (by_min) break;  // (what is above this cut is kept, and none of its ties)
+        const double w = level > -inf ? weight(level) : 0.0;
+        if (shares && level > -inf) {
+            const uint32_t most_ties = cut == first_cut ? first_ties : there;
+            const double m = w > 0.0 ? ceil((need - above) / w) : 1.0;
+            ties = (uint32_t)min(max(m, 1.0), (double)most_ties);
+        }
+        tie = ties ? w : 0.0;
+        if (!(rules.min_p > 0.0 && w < rules.min_p)) break;
         uint32_t lo = max(cut, LEAST_KEY - 1), hi = most;  // the lowest key whose weight is enough: above lo, at most hi
         while (hi - lo > 1) {
             const uint32_t mid = lo + (hi - lo) / 2;
@@ -284,73 +520,31 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         }
         cut = hi - 1;
         ties = 0;
+        tie = 0.0;
+        high = 0.0;
+        high_count = 0;
+        upto = inf;
+        by_min = true;
     }
-
-    // what the warps' runs hold of them; a run's ties are kept as far as there are some left
-    const float level = cut < LEAST_KEY ? -inf : from_ordered(cut);
-    double sum = 0.0;
-    uint32_t count = 0, equal = 0;
-    each(level, [&](float v, int) {
-        if (v > level) { sum += weight(v); ++count; }
-        equal += v == level;
-    });
-#pragma unroll
-    for (int d = 16; d; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    count = __reduce_add_sync(0xffffffffu, count);
-    equal = __reduce_add_sync(0xffffffffu, equal);
-    const double tie = ties ? weight(level) : 0.0;
-    double total = sum + (double)min(equal, ties) * tie, base = 0.0;
-    uint32_t before = 0, kept = count + min(equal, ties), mine = warp;
-    if (NT > 32) {
-        double *d = mem->d[team.turn & 1];
-        auto s = mem->u[team.turn++ & 1];
-        team.tell(d + warp, sum);
-        team.tell(&s[warp][0], count);
-        team.tell(&s[warp][1], equal);
-        team.meet();
-        // a lane at a run: its kept weight, with the ties in front of it
-        total = 0.0;
-        kept = 0;
-        uint32_t front = 0;
-        double at = 0.0;
-        auto runs = [&](auto &&f) {  // f(weight of 32 runs' kept entries, ties in front of each)
-            front = 0;
-            for (uint32_t w0 = 0; w0 < warps; w0 += 32) {
-                const bool there = w0 + lane < warps;
-                const uint32_t e = there ? s[w0 + lane][1] : 0u;
-                uint32_t up = e;
-#pragma unroll
-                for (int k = 1; k < 32; k *= 2) {
-                    const uint32_t v = __shfl_up_sync(0xffffffffu, up, k);
-                    if (lane >= (uint32_t)k) up += v;
-                }
-                const uint32_t b = front + up - e;
-                front += __shfl_sync(0xffffffffu, up, 31);
-                const double own = there ? d[w0 + lane] + (double)min(e, ties - min(ties, b)) * tie : 0.0;
-                double incl = own;
-#pragma unroll
-                for (int k = 1; k < 32; k *= 2) {
-                    const double v = __shfl_up_sync(0xffffffffu, incl, k);
-                    if (lane >= (uint32_t)k) incl += v;
-                }
-                f(w0, own, incl, b, there ? s[w0 + lane][0] : 0u);
-            }
-        };
-        runs([&](uint32_t, double, double incl, uint32_t, uint32_t c) {
+    if (NT == 32) {
+        total = sum + (double)min(equal, ties) * tie;
+        kept = count + min(equal, ties);
+    } else {
+        const uint32_t there = runs([&](uint32_t, double, double incl, uint32_t, uint32_t n) {
             total += __shfl_sync(0xffffffffu, incl, 31);
-            kept += __reduce_add_sync(0xffffffffu, c);
+            kept += __reduce_add_sync(0xffffffffu, n);
         });
-        kept += min(front, ties);
+        kept += min(there, ties);
         // the run that the number falls into: the first up to whose end the sum is above it, or the last with something kept
-        at = (double)rules.uniform[r] * total;
+        const double at = (double)rules.uniform[r] * total;
         double up = 0.0;
         mine = 0xFFFFFFFFu;
         bool hit = false;
         runs([&](uint32_t w0, double own, double incl, uint32_t b, uint32_t) {
             const uint32_t some = __ballot_sync(0xffffffffu, own > 0.0), past = __ballot_sync(0xffffffffu, own > 0.0 && up + incl > at);
+            const double in_front = __shfl_up_sync(0xffffffffu, incl, 1);
             if (!hit && some) {
                 const uint32_t f = past ? __ffs(past) - 1 : 31 - __clz(some);
-                const double in_front = __shfl_up_sync(0xffffffffu, incl, 1);
                 mine = w0 + f;
                 base = up + __shfl_sync(0xffffffffu, lane ? in_front : 0.0, f);
                 before = __shfl_sync(0xffffffffu, b, f);
@@ -359,6 +553,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             up += __shfl_sync(0xffffffffu, incl, 31);
         });
     }
+    if (!(rules.top_k || rules.top_p < 1.0 || rules.min_p > 0.0)) S = total;
     if (warp != mine) return;
     const double at = (double)rules.uniform[r] * total;
     uint32_t token = 0xFFFFFFFFu;

@@ -103,24 +103,108 @@ __device__ __forceinline__ uint32_t block_min(uint32_t v, uint32_t *s)
     return *s;
 }
 
-// One block: what reaches the bound of a row (n keys in any order) is put in order, cut by the rules, and drawn from.  buffer: keys, weights, keys.
-// False if that is too near to call.
-__device__ __forceinline__ bool draw_listed(unsigned char *buffer, uint32_t n, bool whole, const LogitRows &q, const SampleRules &s, const SampleOut &o,
-                                            uint64_t r, float u, float M, double S, double eps, float least, float L, double *s_four, uint32_t *s_found)
+// What a row's listed entries are drawn with.
+struct Listed {
+    const LogitRows &q;
+    const SampleRules &s;
+    const SampleOut &o;
+    const double *table;
+    uint64_t r;
+    float u, M, least, L;  // least: the lowest logit that min_p keeps
+    double S, eps;
+    bool whole;            // nothing but the bound from top_k and top_p cut the list short
+    __device__ __forceinline__ double weight(key_t64 k) const { return exp_below_1((double)q.scale * ((double)key_value(k) - (double)M), table); }
+    __device__ __forceinline__ void put(key_t64 k, double total, uint32_t kept) const
+    {
+        const float z = log_odds(key_value(k), M, q.scale);
+        put_sample(o, r, (int64_t)key_place(k), min_nan(z - L, 0.0f), min_nan(z - logf((float)total), 0.0f), kept);
+    }
+};
+
+// One block, at most an entry a thread: each to its rank, sums in order, and the sums in the order of the numbers by looking at all of them.
+// buffer: 24 bytes an entry.  False if that is too near to call.
+struct Few {
+    double four[LD_WARPS];
+    uint32_t counts[LD_WARPS][3], places[LD_WARPS];
+};
+__device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, uint32_t n, unsigned char *buffer, Few &f)
 {
-    key_t64 *const keys = reinterpret_cast<key_t64 *>(buffer), *const second = reinterpret_cast<key_t64 *>(buffer + LD_GROUPS_AT);
-    double *const w = reinterpret_cast<double *>(buffer + LD_WEIGHTS_AT);
+    key_t64 *const sorted = reinterpret_cast<key_t64 *>(buffer);
+    double *const w = reinterpret_cast<double *>(buffer + LD_THREADS * 8), *const sums = w + LD_THREADS;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    key_t64 key = tid < n ? keys[tid] : 0ull;
+    double own = tid < n ? a.weight(key) : 0.0;
+    if (warp * 32 < n) {
+        uint32_t rank = 0;
+#pragma unroll 4
+        for (uint32_t j = 0; j < n; ++j) rank += keys[j] > key;
+        if (tid < n) {
+            sorted[rank] = key;
+            w[rank] = own;
+        }
+    }
+    __syncthreads();
+    key = tid < n ? sorted[tid] : 0ull;
+    own = tid < n ? w[tid] : 0.0;
+    double up = own;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const double v = __shfl_up_sync(0xffffffffu, up, d);
+        if (lane >= (uint32_t)d) up += v;
+    }
+    if (lane == 31) f.four[warp] = up;
+    __syncthreads();
+    for (uint32_t k = 0; k < warp; ++k) up += f.four[k];
+    sums[tid] = up;
+    __syncthreads();
+    uint32_t kept = a.s.top_k ? min(n, a.s.top_k) : n;
+    const bool p = a.s.top_p < 1.0;
+    const double need = p ? a.s.top_p * (a.s.top_k ? sums[kept - 1] : a.S) : 0.0, lacks = a.s.top_k ? 0.0 : a.eps * need;
+    // sums that do not reach what is needed, for certain and perhaps; logits that min_p keeps
+    const uint32_t under = __popc(__ballot_sync(0xffffffffu, tid < kept && up < need - lacks));
+    const uint32_t perhaps = __popc(__ballot_sync(0xffffffffu, tid < kept && up < need + lacks));
+    const uint32_t from = __popc(__ballot_sync(0xffffffffu, tid < n && key_value(key) >= a.least));
+    if (lane == 0) { f.counts[warp][0] = under; f.counts[warp][1] = perhaps; f.counts[warp][2] = from; }
+    __syncthreads();
+    uint32_t all[3] = {0, 0, 0};
+#pragma unroll
+    for (uint32_t k = 0; k < LD_WARPS; ++k)
+#pragma unroll
+        for (int j = 0; j < 3; ++j) all[j] += f.counts[k][j];
+    if (p) {
+        if (all[0] != all[1] || (a.whole && all[0] >= kept)) return false;
+        kept = min(kept, all[0] + 1);
+    }
+    kept = min(kept, all[2]);
+    const double total = sums[kept - 1], at = (double)a.u * total;
+    const uint32_t place = tid < kept ? key_place(key) : 0xFFFFFFFFu;
+    uint32_t first = 0xFFFFFFFFu;
+    if (warp * 32 < kept) {
+        double sum = 0.0;
+#pragma unroll 4
+        for (uint32_t j = 0; j < kept; ++j)
+            if (key_place(sorted[j]) <= place) sum += w[j];
+        first = __reduce_min_sync(0xffffffffu, sum > at ? place : 0xFFFFFFFFu);
+    }
+    if (lane == 0) f.places[warp] = first;
+    __syncthreads();
+    first = min(min(f.places[0], f.places[1]), min(f.places[2], f.places[3]));
+    if (place == first && tid < kept) a.put(key, total, kept);
+    return first != 0xFFFFFFFFu;
+}
+
+// The same for n keys in any order (n <= LD_CAP): sorted, summed up, cut; what is kept is sorted by its numbers and summed up again.
+__device__ __forceinline__ bool draw_many(const Listed &a, key_t64 *keys, uint32_t n, double *w, key_t64 *second, double *s_four, uint32_t *s_found)
+{
     const uint32_t tid = threadIdx.x;
-    const double scale = (double)q.scale;
-    auto weight = [&](key_t64 k) { return exp(scale * ((double)key_value(k) - (double)M)); };
-    if (tid < 3) s_found[tid] = tid == 2 ? 0u : 0xFFFFFFFFu;
+    if (tid < 2) s_found[tid] = 0xFFFFFFFFu;
     sort_keys(keys, n);
-    for (uint32_t i = tid; i < n; i += LD_THREADS) w[i] = weight(keys[i]);
+    for (uint32_t i = tid; i < n; i += LD_THREADS) w[i] = a.weight(keys[i]);
     __syncthreads();
     sum_up(w, n, s_four);
-    uint32_t kept = s.top_k ? min(n, s.top_k) : n;
-    if (s.top_p < 1.0) {
-        const double need = s.top_p * (s.top_k ? w[kept - 1] : S), lacks = s.top_k ? 0.0 : eps * need;
+    uint32_t kept = a.s.top_k ? min(n, a.s.top_k) : n;
+    if (a.s.top_p < 1.0) {
+        const double need = a.s.top_p * (a.s.top_k ? w[kept - 1] : a.S), lacks = a.s.top_k ? 0.0 : a.eps * need;
         uint32_t first = 0xFFFFFFFFu;
         for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
             if (w[i] >= need) first = i;
@@ -128,21 +212,21 @@ __device__ __forceinline__ bool draw_listed(unsigned char *buffer, uint32_t n, b
         if (first != 0xFFFFFFFFu) {
             if (w[first] < need + lacks || (first && w[first - 1] >= need - lacks)) return false;
             kept = first + 1;
-        } else if (whole || w[kept - 1] >= need - lacks) {  // (else what is listed is all that min_p leaves)
+        } else if (a.whole || w[kept - 1] >= need - lacks) {  // (else what is listed is all that min_p leaves)
             return false;
         }
     }
-    if (s.min_p > 0.0) {
+    if (a.s.min_p > 0.0) {
         uint32_t first = 0xFFFFFFFFu;
         for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
-            if (key_value(keys[i]) < least) first = i;
+            if (key_value(keys[i]) < a.least) first = i;
         kept = min(kept, block_min(first, s_found + 1));
     }
-    const double total = w[kept - 1], at = (double)u * total;
+    const double total = w[kept - 1], at = (double)a.u * total;
     for (uint32_t i = tid; i < kept; i += LD_THREADS) second[i] = (key_t64)(0xFFFFFFFFu - key_place(keys[i])) << 32 | i;
     __syncthreads();
     sort_keys(second, kept);
-    for (uint32_t i = tid; i < kept; i += LD_THREADS) w[i] = weight(keys[(uint32_t)second[i]]);
+    for (uint32_t i = tid; i < kept; i += LD_THREADS) w[i] = a.weight(keys[(uint32_t)second[i]]);
     if (tid == 0) s_found[0] = 0xFFFFFFFFu;
     __syncthreads();
     sum_up(w, kept, s_four);
@@ -151,11 +235,7 @@ __device__ __forceinline__ bool draw_listed(unsigned char *buffer, uint32_t n, b
         if (w[i] > at) first = i;
     first = block_min(first, s_found);
     if (first == 0xFFFFFFFFu) return false;
-    if (tid == 0) {
-        const key_t64 k = keys[(uint32_t)second[first]];
-        const float z = log_odds(key_value(k), M, q.scale);
-        put_sample(o, r, (int64_t)key_place(k), min_nan(z - L, 0.0f), min_nan(z - (float)log(total), 0.0f), kept);
-    }
+    if (tid == 0) a.put(keys[(uint32_t)second[first]], total, kept);
     return true;
 }
 
@@ -170,7 +250,9 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
     __shared__ T s_most[RULES ? LD_SEGS : 1][RULES ? NT : 1];
     __shared__ double s_sum[MAX_PARTS * RECS], s_four[LD_WARPS];
     __shared__ float s_ref[MAX_PARTS * RECS], s_max[MAX_PARTS * LD_WARPS], s_min[MAX_PARTS * LD_WARPS], s_bound;
-    __shared__ uint32_t s_count[MAX_PARTS * LD_WARPS], s_bins[RULES ? LD_BINS : 1], s_mass[RULES ? LD_BINS : 1], s_n[2], s_found[3];
+    __shared__ uint32_t s_count[MAX_PARTS * LD_WARPS], s_bins[RULES ? LD_BINS : 1], s_mass[RULES ? LD_BINS : 1], s_n[3], s_found[2], s_base;
+    __shared__ double s_table[EXP_TABLE];
+    __shared__ Few s_few;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t step = gridDim.x >> log_parts;
     const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), margin = 3.0f / c;
@@ -183,6 +265,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
         else __syncthreads();
     };
     pdl_go();
+    if (tid < EXP_TABLE) s_table[tid] = exp2((double)tid / EXP_TABLE);
     if (CLUSTER) cluster.sync();  // (all blocks of the cluster run)
 
     for (uint64_t r = blockIdx.x >> log_parts; r < q.n_rows; r += step) {
@@ -313,21 +396,18 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
         }
         if (RULES) {
             if (tid < LD_BINS) s_bins[RULES ? tid : 0] = s_mass[RULES ? tid : 0] = 0;
-            if (tid < 2) s_n[tid] = 0;
+            if (tid < 3) s_n[tid] = 0;
         }
         meet();
 
         // M and S relative to it, the same in every thread
-        float M = -inf, low = inf;
-        count = 0;
-        for (uint32_t w = 0; w < parts * LD_WARPS; ++w) {
-            M = fmaxf(M, s_max[w]);
-            if (RULES) low = fminf(low, s_min[w]);
-            else count += s_count[w];
-        }
+        const uint32_t warps = parts * LD_WARPS;  // at most 32
+        const float M = from_ordered(__reduce_max_sync(0xffffffffu, lane < warps ? ordered(s_max[lane]) : 0u));
+        const float low = RULES ? from_ordered(__reduce_min_sync(0xffffffffu, lane < warps ? ordered(s_min[lane]) : 0xFFFFFFFFu)) : 0.0f;
+        count = RULES ? 0u : __reduce_add_sync(0xffffffffu, lane < warps ? s_count[lane] : 0u);
         const double cM = (double)c * (double)M;
         auto relative = [&](uint32_t i) {  // (a warp's sums are relative to its rounded product)
-            return s_ref[i] == -inf ? 0.0 : s_sum[i] * exp2((double)__fmul_rn(s_ref[i], c) - cM);
+            return s_ref[i] == -inf ? 0.0 : s_sum[i] * exp_below_1(((double)__fmul_rn(s_ref[i], c) - cM) * LN2_64, s_table);
         };
         double S = 0.0;
         for (uint32_t i0 = 0; i0 < parts * RECS; i0 += 32) {
@@ -341,8 +421,8 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             if (part == 0 && tid == 0) put_sample(o, r, -1, -inf, -inf, 0);
             settled = true;
         } else if (S > 0.0 && S < 1e300 && !far_out(M, c)) {
-            const double eps = (20.0 + 1.4 * log2((double)q.V / S)) * (1.0 / 16777216.0);
-            const float L = max_nan((float)log(S), 0.0f);
+            const double eps = (double)((20.5f + 1.4f * __log2f((float)q.V / (float)S)) * 0x1p-24f);
+            const float L = max_nan(logf((float)S), 0.0f);
             if (!RULES) {
                 // the segment that the number falls into, and what lies in front of it
                 const double at = (double)u * S;
@@ -368,7 +448,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                     __syncthreads();
                     const uint32_t w = mine % RECS / LD_SEGS, a = min(p1, p0 + w * per), b = min(p1, a + per);
                     const uint32_t from = min(b, a + (mine % LD_SEGS) * seg_steps * LD_STEP), to = min(b, from + seg_steps * LD_STEP);
-                    const double back = exp2((double)__fmul_rn(M, c) - cM), slack = 0.5 * eps * S;
+                    const double back = exp_below_1(((double)__fmul_rn(M, c) - cM) * LN2_64, s_table), slack = 0.5 * eps * S;
                     for (uint32_t w0 = from; w0 < to; w0 += NT) {
                         const uint32_t v = w0 + tid;
                         uint4 raw = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
@@ -415,7 +495,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             const float range = fminf(M - low, 64.0f / q.scale), width = range * (1.0f / LD_BINS);
             const float each = width > 1e-30f ? 1.0f / width : 0.0f;
             if (s.top_k || s.top_p < 1.0) {
-#pragma unroll 1
+#pragma unroll
                 for (uint32_t seg = 0; seg < LD_SEGS; ++seg) {
                     const float d = M - to_f32(s_most[RULES ? seg : 0][RULES ? tid : 0]);
                     if (d <= range) {
@@ -426,6 +506,19 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                 }
             }
             meet();
+            if (CLUSTER) {  // of all the blocks (the own bins may still be asked for by others: the sums lie where the ring was)
+                uint32_t n = 0, m = 0;
+#pragma unroll
+                for (uint32_t p = 0; p < MAX_PARTS; ++p)
+                    if (p < parts) {
+                        n += *away(&s_bins[RULES ? tid : 0], p);
+                        m += *away(&s_mass[RULES ? tid : 0], p);
+                    }
+                reinterpret_cast<uint32_t *>(buffer)[tid] = n;
+                reinterpret_cast<uint32_t *>(buffer)[LD_BINS + tid] = m;
+                __syncthreads();
+            }
+            const uint32_t *const bins = CLUSTER ? reinterpret_cast<uint32_t *>(buffer) : s_bins, *const mass = CLUSTER ? bins + LD_BINS : s_mass;
             const float from = fmaxf(__double2float_ru((double)M + h.drop), LOWEST);  // of min_p
             if (warp == 0) {
                 float bound = LOWEST;
@@ -434,13 +527,8 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                     uint32_t n[PER], m[PER], n_own = 0, m_own = 0;
 #pragma unroll
                     for (uint32_t i = 0; i < PER; ++i) {
-                        n[i] = m[i] = 0;
-                        for (uint32_t p = 0; p < parts; ++p) {
-                            n[i] += *away(&s_bins[RULES ? lane * PER + i : 0], p);
-                            m[i] += *away(&s_mass[RULES ? lane * PER + i : 0], p);
-                        }
-                        n_own += n[i];
-                        m_own += m[i];
+                        n_own += n[i] = bins[lane * PER + i];
+                        m_own += m[i] = mass[lane * PER + i];
                     }
                     uint32_t n_up = n_own, m_up = m_own;
 #pragma unroll
@@ -459,12 +547,12 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                         n_up += n[i];
                         m_up += m[i];
                         if (sure == -inf && (s.top_k ? n_up >= s.top_k : (float)m_up >= need)) sure = end_of(lane * PER + i);
-                        if (guess == -inf && n_up >= LD_GUESS) guess = end_of(lane * PER + i);
+                        if (guess == -inf && n_up >= LD_GUESS) guess = (float)m_up >= 0.5f * need ? end_of(lane * PER + i) : inf;
                     }
                     // the weights of a group's other entries are not counted: where the largest ones alone are not enough, what reaches the
                     // LD_GUESS-th may be
                     uint32_t reached = __ballot_sync(0xffffffffu, sure > -inf);
-                    if (!reached && !s.top_k) {
+                    if (!reached && !s.top_k) {  // (or, by far not enough, the row is broad: nothing is listed)
                         reached = __ballot_sync(0xffffffffu, guess > -inf);
                         sure = guess;
                     }
@@ -484,8 +572,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                 if (to_f32(s_most[RULES ? seg : 0][RULES ? tid : 0]) >= bound) groups[atomicAdd(&s_n[1], 1u)] = (uint16_t)(seg * NT + tid);
             __syncthreads();
             const uint32_t vectors = seg_steps * U, items = s_n[1] * vectors;
-            key_t64 *const list = away(reinterpret_cast<key_t64 *>(buffer), 0);
-            uint32_t *const listed = away(&s_n[0], 0);
+            key_t64 *list = reinterpret_cast<key_t64 *>(buffer);
             for (uint32_t i0 = tid; i0 < items; i0 += 4 * NT) {
                 uint4 raw[4];
                 uint32_t at[4];
@@ -512,14 +599,29 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
 #pragma unroll
                     for (int i = 0; i < EPV<T>; ++i)
                         if (e[i] >= bound) {
-                            const uint32_t place = atomicAdd(listed, 1u);
+                            const uint32_t place = atomicAdd(&s_n[0], 1u);
                             if (place < LD_CAP) list[place] = rank_key(e[i], (uint32_t)(x.first(at[k]) + i));
                         }
                 }
             }
-            meet();
-            if (part == 0 && s_n[0] <= LD_CAP && s_n[0] > 0)
-                settled = draw_listed(buffer, s_n[0], all, q, s, o, r, u, M, S, eps, from, L, s_four, s_found);
+            __syncthreads();
+            uint32_t n = s_n[0];
+            if (CLUSTER) {  // to the first block
+                if (tid == 0) s_base = atomicAdd(away(&s_n[2], 0), n);
+                __syncthreads();
+                key_t64 *const to = away(reinterpret_cast<key_t64 *>(buffer + LD_WEIGHTS_AT), 0);
+                for (uint32_t i = tid; i < min(n, LD_CAP); i += NT)
+                    if (s_base + i < LD_CAP) to[s_base + i] = list[i];
+                meet();
+                n = s_n[2];
+                list = reinterpret_cast<key_t64 *>(buffer + LD_WEIGHTS_AT);
+            }
+            if (part == 0 && n <= LD_CAP && n > 0) {
+                const Listed a{q, s, o, s_table, r, u, M, from, L, S, eps, all};
+                settled = n <= NT ? draw_few(a, list, n, buffer + LD_GROUPS_AT, s_few)
+                                  : draw_many(a, list, n, reinterpret_cast<double *>(buffer + (CLUSTER ? 0 : LD_WEIGHTS_AT)),
+                                              reinterpret_cast<key_t64 *>(buffer + LD_GROUPS_AT), s_four, s_found);
+            }
         }
         if (part == 0 && tid == 0) s.left[r] = !settled;
         meet();
@@ -527,10 +629,11 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
 }
 
 // The rows that were left, each to a cluster of blocks, which works them out in 64 bits.
-constexpr uint32_t RS_THREADS = 512;
+constexpr uint32_t RS_THREADS = 512, RS_BYTES = TEAM_HELD * RS_THREADS * 16 + 16 * RS_THREADS * 8;
 template <typename T>
 __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, const SampleRules s, const SampleOut o, uint32_t log_parts)
 {
+    extern __shared__ __align__(16) uint4 s_held[];  // [TEAM_HELD][RS_THREADS], then [16][RS_THREADS] sums of 64 bits
     __shared__ TeamMemory<RS_THREADS> mem;
     __shared__ uint32_t s_warp[RS_THREADS / 32], s_row[RS_THREADS];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
@@ -557,7 +660,7 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
         number += all;
         __syncthreads();
         for (uint32_t i = 0; i < n; ++i) {
-            sample_row_64<T, RS_THREADS>(q, s, o, base + s_row[i], &mem, parts, part);
+            sample_row_64<T, RS_THREADS>(q, s, o, base + s_row[i], &mem, s_held, parts, part);
             if (parts > 1) cg::this_cluster().sync();  // (the next row's first sums may go where this row's last ones are read)
             else __syncthreads();
         }
@@ -579,7 +682,7 @@ cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const Samp
     cudaLaunchConfig_t cfg{};
     cfg.blockDim = LD_THREADS; cfg.dynamicSmemBytes = LD_RING_BYTES; cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = CLUSTER ? 1 : 0;
-    const uint64_t most = (8 * (uint64_t)vl_device_sm_count(device)) >> log_parts;
+    const uint64_t most = (1ull << 30) >> log_parts;
     cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
     g_vl_launches.fetch_add(1);
     return cudaLaunchKernelEx(&cfg, kernel, q, s, o, h, log_parts);
@@ -596,6 +699,8 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true>(q, s, o, h, log_parts, device, st)
                                     : run_sample_long<T, MASKED, RULES, false>(q, s, o, h, 0, device, st);
     if (e != cudaSuccess) return e;
+    constexpr auto rest = k_sample_rest<T>;
+    if (const cudaError_t f = allow_smem<rest, (int)RS_BYTES>(device); f != cudaSuccess) return f;
     // few rows: more blocks at each; short ones have nothing to share
     const uint32_t log_rest = n < 1024 ? 0 : q.n_rows <= 8 ? 3 : 2;
     const uint64_t clusters = (uint64_t)vl_device_sm_count(device) >> log_rest;
@@ -607,10 +712,10 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((uint32_t)(q.n_rows < clusters ? q.n_rows : clusters) << log_rest);
-    cfg.blockDim = RS_THREADS; cfg.stream = st;
+    cfg.blockDim = RS_THREADS; cfg.dynamicSmemBytes = RS_BYTES; cfg.stream = st;
     cfg.attrs = at; cfg.numAttrs = 2;
     g_vl_launches.fetch_add(1);
-    return cudaLaunchKernelEx(&cfg, k_sample_rest<T>, q, s, o, log_rest);
+    return cudaLaunchKernelEx(&cfg, rest, q, s, o, log_rest);
 }
 
 }  // namespace

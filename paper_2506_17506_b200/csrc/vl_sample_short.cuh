@@ -69,7 +69,7 @@ struct Keep {
 
 // The token of a row that a group holds, from number u, where one is wanted and the sum S over the whole row (worked out here) is one.  The
 // lane that has the token gets it in `token`, with its logit.  False where a border is too near, in every lane of the group.
-template <typename T, int G, int NV, bool TIES>
+template <typename T, int G, int NV, bool PART, bool TIES>
 __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &keep, const RowVectors<T> &x, float u, float m, float c, float eps,
                                      uint32_t lane, bool wanted, int64_t *token, float *x_tok, float *all, float *total, uint32_t *kept)
 {
@@ -77,47 +77,39 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
     const bool far = far_out(m, c);
     float v[NV];
     uint32_t n = 0;
-    auto weights = [&](const uint4 &vector, uint32_t ties, float (&xs)[EPV<T>], float (&e)[EPV<T>]) {
-        unpack(vector, xs, T{});
-        powers<T>(xs, m, c, far, e);
-#pragma unroll
-        for (int i = 0; i < EPV<T>; ++i) {
-            bool k = xs[i] >= keep.from;
-            if (TIES && xs[i] == keep.level && ties) { k = true; --ties; }
-            if (!k) e[i] = 0.0f;
-        }
-    };
-    float S = 0.0f;
+    // PART: not all of them are kept
+    float S = 0.0f, T_all = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float xs[EPV<T>], e[EPV<T>];
         unpack(raw[j], xs, T{});
         powers<T>(xs, m, c, far, e);
-        S += sum_of(e);
-        uint32_t ties = TIES ? keep.ties[j] : 0u;
+        if (PART) {
+            S += sum_of(e);
+            uint32_t ties = TIES ? keep.ties[j] : 0u;
 #pragma unroll
-        for (int i = 0; i < EPV<T>; ++i) {
-            bool k = xs[i] >= keep.from;
-            if (TIES && xs[i] == keep.level && ties) { k = true; --ties; }
-            if (!k) e[i] = 0.0f;
-            n += k;
+            for (int i = 0; i < EPV<T>; ++i) {
+                bool k = xs[i] >= keep.from;
+                if (TIES && xs[i] == keep.level && ties) { k = true; --ties; }
+                if (!k) e[i] = 0.0f;
+                n += k;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i) n += xs[i] >= LOWEST;
         }
         v[j] = sum_of(e);
+        T_all += v[j];
     }
-    S = group_sum<G>(S);
+    T_all = group_sum<G>(T_all);
+    S = PART ? group_sum<G>(S) : T_all;
     *all = S;
+    *total = T_all;
     const bool some = wanted && S > 0.0f && S < __int_as_float(0x7f800000);
 #pragma unroll
     for (int d = G / 2; d; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
     *kept = n;
-    // the sums of the group's vectors, round by round: the round that the number falls into, and what lies in front of it
-    float round[NV], T_all = 0.0f;
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        round[j] = group_sum<G>(v[j]);
-        T_all += round[j];
-    }
-    *total = T_all;
+    // round by round: the group's vectors that the number falls into, and what lies in front of them
     const float at = u * T_all, margin = 0.5f * eps * T_all;
     float base = 0.0f, up = 0.0f, own = 0.0f;
     uint4 vector = raw[0];
@@ -132,7 +124,7 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
             turn = j;
             if (TIES) ties = keep.ties[j];
         }
-        up += round[j];
+        up += NV == 1 ? T_all : group_sum<G>(v[j]);
         found = found || up > at;
     }
     float incl = own;
@@ -147,11 +139,14 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
     *token = -1;
     if (some && past && g == __ffs(past) - 1u) {
         float xs[EPV<T>], e[EPV<T>], cum = base + (incl - own);
-        weights(vector, ties, xs, e);
+        unpack(vector, xs, T{});
+        powers<T>(xs, m, c, far, e);
         bool open = true;
 #pragma unroll
         for (int i = 0; i < EPV<T>; ++i) {
-            const float next = cum + e[i];
+            bool k = !PART || xs[i] >= keep.from;
+            if (TIES && xs[i] == keep.level && ties) { k = true; --ties; }
+            const float next = k ? cum + e[i] : cum;
             if (open && next > at) {
                 open = false;
                 sure = at >= cum + margin && next >= at + margin;
@@ -175,12 +170,12 @@ __device__ __forceinline__ void settle(const LogitRows &q, const SampleRules &s,
     while (left) {
         const uint64_t which = __shfl_sync(0xffffffffu, (unsigned long long)r, __ffs(left) - 1);
         left &= left - 1;
-        sample_row_64<T, 32>(q, s, o, which, nullptr, 1, 0);
+        sample_row_64<T, 32>(q, s, o, which, nullptr, nullptr, 1, 0);
     }
 }
 
 // No rules, or min_p: what is kept is told by a logit at once.
-template <typename T, bool MASKED, bool ALIGNED, int G, int NV>
+template <typename T, bool MASKED, bool ALIGNED, bool PART, int G, int NV>
 __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_short(const LogitRows q, const SampleRules s, const SampleOut o,
                                                                                     const ShortRules h)
 {
@@ -205,7 +200,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_s
         int64_t token;
         float x_tok = 0.0f, S, T_all;
         uint32_t kept;
-        const bool sure = draw<T, G, NV, false>(raw, keep, x, u, m, c, h.eps, lane, there && drawn, &token, &x_tok, &S, &T_all, &kept);
+        const bool sure = draw<T, G, NV, PART, false>(raw, keep, x, u, m, c, h.eps, lane, there && drawn, &token, &x_tok, &S, &T_all, &kept);
         const bool some = there && drawn && S > 0.0f && S < inf;
         if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, log_of(S, m, c)), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
         if (there && !some && g == 0) {
@@ -216,12 +211,12 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_s
     }
 }
 
-// top_k or top_p: a warp per row.
-template <typename T, bool MASKED, bool ALIGNED, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32, 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o,
+// top_k or top_p: a warp per row.  FEW: up to 32 entries are kept, by top_k.
+template <typename T, bool MASKED, bool ALIGNED, bool FEW, int NV>
+__global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o,
                                                                                   const ShortRules h)
 {
-    __shared__ key_t64 s_cand[SHORT_WARPS][SHORT_CAND];
+    __shared__ key_t64 s_cand[FEW ? SHORT_WARPS : 1][FEW ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), nan = __int_as_float(0x7fc00000);
@@ -270,7 +265,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, 2) k_sample_warp(const Logit
             continue;
         }
         const float L = log_of(S, m, c);
-        if (s.top_k && s.top_k <= 32) {
+        if constexpr (FEW) {
             // the best, one to a lane in order; their weights and all that follows from them in 64 bits
             const key_t64 key = warp_alternatives<T, NV>(raw, own, x, lane, s.top_k, s_cand[warp], &s_n[warp]);
             const uint32_t best = min(n, s.top_k);
@@ -304,8 +299,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, 2) k_sample_warp(const Logit
                 const float lt = (float)log(T_all);
                 put_sample(o, r, tok, log_ratio(xk, m, q.scale, L), log_ratio(xk, m, q.scale, lt), kept);
             }
-            continue;
-        }
+        } else {
         // the cut: a key, and how many of the entries equal to it are kept; found by halves between values, in 32 bits
         const uint32_t most = ordered(m);
         uint32_t cut = LEAST_KEY - 1, ties = 0, there = 0;
@@ -419,13 +413,14 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, 2) k_sample_warp(const Logit
                     keep.ties[j] = front < ties ? ties - front : 0u;
                     before += __shfl_sync(0xffffffffu, incl, 31);
                 }
-                sure = draw<T, 32, NV, true>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
+                sure = draw<T, 32, NV, true, true>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
             } else {
-                sure = draw<T, 32, NV, false>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
+                sure = draw<T, 32, NV, true, false>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
             }
         }
         if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, L), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
-        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, 1, 0);
+        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, nullptr, 1, 0);
+        }
     }
 }
 
@@ -437,13 +432,16 @@ bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleO
         constexpr int G = decltype(g)::value, NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
         const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
-        k_sample_short<T, MASKED, ALIGNED, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        if (s.min_p > 0.0) k_sample_short<T, MASKED, ALIGNED, true, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        else k_sample_short<T, MASKED, ALIGNED, false, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
         g_vl_launches.fetch_add(1);
     };
     auto run_warp = [&](auto, auto v) {
         constexpr int NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS - 1) / SHORT_WARPS;
-        k_sample_warp<T, MASKED, ALIGNED, NV><<<(uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30)), SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
+        if (s.top_k && s.top_k <= 32) k_sample_warp<T, MASKED, ALIGNED, true, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        else k_sample_warp<T, MASKED, ALIGNED, false, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
         g_vl_launches.fetch_add(1);
     };
     return order ? short_shape<true, ALIGNED>(n, q.W, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
