@@ -420,8 +420,8 @@ typedef struct {
     double min_p;   /* 0 to 1; 0: all */
 } vl_sampling;
 
-/* Bytes of working memory of a vl_token_sample call. */
-uint64_t vl_sample_work(uint64_t n_rows);
+/* Bytes of working memory of a vl_token_sample call: 0 for rows of up to 1,020 entries. */
+uint64_t vl_sample_work(uint64_t n_rows, uint32_t n_vocab);
 
 /*
  * d_uniform [n_rows]: numbers from 0 on, below 1; a row whose number is none of these is left out: token -1, ln p 0, nothing kept.  d_tokens
@@ -429,8 +429,8 @@ uint64_t vl_sample_work(uint64_t n_rows);
  * ln p of the token under the whole row, as vl_token_logprobs gives it; d_drawn_logprob: under what was kept, ln (w / T); d_kept: entries
  * kept (as int32).  Any of these three may be NULL.  Entries of logit minus infinity are never kept.  A row without possible entries: token
  * -1, ln p minus infinity, nothing kept; a row with an open logit of plus infinity or that is no number: token -1, ln p no number, nothing
- * kept.  d_work: at least vl_sample_work bytes of device memory, the call's own until its work is done.  Stream-ordered on `cuda_stream` of
- * `device`, no synchronisation, no allocation.  Equal inputs give equal results, bit for bit.  n_rows == 0 is a no-op.  Errors: INVALID_ARG,
+ * kept.  d_work: at least vl_sample_work bytes of device memory, 4-byte aligned, the call's own until its work is done.  Stream-ordered on
+ * `cuda_stream` of `device`, no synchronisation, no allocation.  Equal inputs give equal results, bit for bit.  n_rows == 0 is a no-op.  Errors: INVALID_ARG,
  * CUDA.
  */
 int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens, uint32_t token_bytes,

@@ -7,9 +7,11 @@ Importing this module fails loudly when the library has not been built
 """
 from __future__ import annotations
 
+import array
 import collections
 import contextlib
 import ctypes as C
+import functools
 import os
 import struct
 
@@ -148,7 +150,7 @@ _lib.vl_policy_loss.argtypes = ([C.c_int, C.c_uint32] + [C.c_void_p] * 3 + [C.c_
 _lib.vl_token_sample.restype = C.c_int
 _lib.vl_token_sample.argtypes = [C.c_int] + [C.c_void_p] * 4 + [C.c_uint32] + [C.c_void_p] * 4 + [C.c_uint64, C.c_void_p]
 _lib.vl_sample_work.restype = C.c_uint64
-_lib.vl_sample_work.argtypes = [C.c_uint64]
+_lib.vl_sample_work.argtypes = [C.c_uint64, C.c_uint32]
 _lib.vl_grad_work.restype = C.c_uint64
 _lib.vl_grad_work.argtypes = [C.c_uint32]
 _lib.vl_grad_norm.restype = C.c_int
@@ -504,13 +506,20 @@ class _Torch:
     def load(cls):
         import torch
         cls.logits = {torch.float32: (VL_F32, 4), torch.float16: (VL_F16, 2), torch.bfloat16: (VL_BF16, 2)}
+        cls.kinds = {t: k for t, (k, _) in cls.logits.items()}
         cls.tokens = {torch.uint16: 2, torch.int16: 2, torch.int32: 4, torch.int64: 8}
         cls.words = (torch.int32, torch.uint32)
         cls.f32, cls.i32, cls.i64, cls.u8 = (torch.float32,), (torch.int32,), (torch.int64,), (torch.uint8,)
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         cls.current = raw if raw else staticmethod(lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+        cls.device = functools.lru_cache(64)(lambda dev: torch.device("cuda", dev))
         cls.torch = torch
         return torch
+
+
+@functools.lru_cache(64)
+def _grad_work(n: int) -> int:
+    return int(_lib.vl_grad_work(n))
 
 
 def _refuse(where: str, what: str):
@@ -628,13 +637,13 @@ def vl_token_sample(logits, uniform, occupied=None, mask_rows=None, widths=None,
         ptr = _Torch.current(dev)
     else:
         ptr, scope = _on(stream, dev)
-    work_size = int(_lib.vl_sample_work(R))
+    work_size = int(_lib.vl_sample_work(R, V)) if V > 1020 else 0
     with scope or _HERE:        # memory of their own: what is kept keeps nothing else
         lp = logits.new_empty(R, dtype=torch.float32)
         drawn, kept, tokens = lp.new_empty(R), lp.new_empty(R, dtype=torch.int32), lp.new_empty(R, dtype=kind)
-        work = lp.new_empty(work_size, dtype=torch.uint8)
+        work = lp.new_empty(work_size, dtype=torch.uint8) if work_size else None
     rc = _lib.vl_token_sample(dev, x, _SAMPLING.pack(top_k, top_p, min_p), u, tokens.data_ptr(), size, lp.data_ptr(), drawn.data_ptr(),
-                              kept.data_ptr(), work.data_ptr(), work_size, ptr)
+                              kept.data_ptr(), work.data_ptr() if work_size else 0, work_size, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
     return TokenSample(tokens, lp, drawn, kept)
@@ -743,26 +752,42 @@ def _dense(t) -> bool:
 
 
 def _gradients(where, grads, outs):
-    """(descriptors as bytes, their number, device number) of gradient tensors and, with ``outs``, of where their results go."""
+    """(vl_gradient descriptors as an array, their number, device number) of gradient tensors and, with ``outs``, of where their results go."""
     torch = _Torch.torch or _Torch.load()
-    kinds, dev, flat = _Torch.logits, -1, []
-    if outs is not None and len(outs) != len(grads):
-        _refuse(where, "outs: one for every tensor")
-    for j, g in enumerate(grads):
-        kind = kinds.get(g.dtype)
-        d = g.get_device()
-        if dev < 0:
-            dev = d
-        if kind is None or d < 0 or d != dev or g.is_sparse or not _dense(g):
-            _refuse(where, "grads: dense CUDA tensors of float32, float16 or bfloat16 on one device")
-        at = to = g.data_ptr()
-        if outs is not None:
-            o = outs[j]
-            if o.dtype is not g.dtype or o.get_device() != dev or o.shape != g.shape or (o.stride() != g.stride() and g.numel() > 1):
-                _refuse(where, "outs: tensors like the gradients")
-            to = o.data_ptr()
-        flat += (at, to, g.numel(), kind[0])
-    return struct.pack("@" + "PPQi4x" * len(grads), *flat), len(grads), dev if dev >= 0 else torch.cuda.current_device()
+    each = torch.Tensor
+    if not grads:
+        if outs:
+            _refuse(where, "outs: one for every tensor")
+        return array.array("Q", (0,)), 0, torch.cuda.current_device()
+    dev = grads[0].get_device()
+    types = [g.dtype for g in grads]
+    kinds = list(map(_Torch.kinds.get, types))
+    what = "grads: dense CUDA tensors of float32, float16 or bfloat16 on one device"
+    if dev < 0 or None in kinds or set(map(each.get_device, grads)) != {dev}:
+        _refuse(where, what)
+    try:
+        at, n = list(map(each.data_ptr, grads)), list(map(each.numel, grads))
+        plain = all(map(each.is_contiguous, grads))
+        if not plain and not all(map(_dense, grads)):
+            _refuse(where, what)
+    except (RuntimeError, NotImplementedError):     # (sparse ones have no memory of their own)
+        _refuse(where, what)
+    to = at
+    if outs is not None:
+        what = "outs: tensors of the gradients' types and sizes, with their elements in the same order"
+        if len(outs) != len(grads) or [o.dtype for o in outs] != types or set(map(each.get_device, outs)) != {dev}:
+            _refuse(where, what)
+        if list(map(each.numel, outs)) != n:
+            _refuse(where, what)
+        if not (plain and all(map(each.is_contiguous, outs))):
+            for o, g in zip(outs, grads):
+                if not (o.is_contiguous() and g.is_contiguous()) and (o.shape != g.shape or (o.stride() != g.stride() and g.numel() > 1)):
+                    _refuse(where, what)
+        to = list(map(each.data_ptr, outs))
+    # (a descriptor is four words: two addresses, the size, and the type in the low half of the last)
+    words = [0] * (4 * len(grads))
+    words[0::4], words[1::4], words[2::4], words[3::4] = at, to, n, kinds
+    return array.array("Q", words), len(grads), dev
 
 
 def vl_grad_norm(grads, scale: float = 1.0, stream=None):
@@ -778,11 +803,11 @@ def vl_grad_norm(grads, scale: float = 1.0, stream=None):
         ptr = _Torch.current(dev)
     else:
         ptr, scope = _on(stream, dev)
-    size = int(_lib.vl_grad_work(n))
+    size = _grad_work(n)
     with scope or _HERE:
-        work = torch.empty(size // 8, dtype=torch.float64, device=f"cuda:{dev}")
+        work = torch.empty(size // 8, dtype=torch.float64, device=_Torch.device(dev))
         norm, squares = work.new_empty((), dtype=torch.float32), work.new_empty(())
-    rc = _lib.vl_grad_norm(dev, n, t, scale, norm.data_ptr(), squares.data_ptr(), work.data_ptr(), size, ptr)
+    rc = _lib.vl_grad_norm(dev, n, t.buffer_info()[0], scale, norm.data_ptr(), squares.data_ptr(), work.data_ptr(), size, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
     return GradNorm(norm, squares)
@@ -790,8 +815,8 @@ def vl_grad_norm(grads, scale: float = 1.0, stream=None):
 
 def vl_clip_grads(grads, max_norm: float, scale: float = 1.0, outs=None, sum_squares=None, stream=None):
     """Gradient tensors (as for ``vl_grad_norm``) times ``scale``, and times max_norm / norm where their global norm is above ``max_norm``: in
-    place, or into ``outs`` (tensors of the same shapes, types and strides; none shares memory with another one, or with a gradient that
-    is not its own).  With ``sum_squares`` (float64 scalar tensor: of all ranks together) the norm is its root.  A norm that is no finite number
+    place, or into ``outs`` (tensors of the same types and sizes, contiguous or of the gradient's strides; none shares memory with another
+    one, or with a gradient that is not its own).  With ``sum_squares`` (float64 scalar tensor: of all ranks together) the norm is its root.  A norm that is no finite number
     makes every result 0.  Returns Clipped(norm, factor: float32 scalar tensors; outs).  On ``stream`` (default: the current one of
     the tensors' device), without waiting."""
     where = "vl_clip_grads"
@@ -808,11 +833,11 @@ def vl_clip_grads(grads, max_norm: float, scale: float = 1.0, outs=None, sum_squ
         ptr = _Torch.current(dev)
     else:
         ptr, scope = _on(stream, dev)
-    size = int(_lib.vl_grad_work(n))
+    size = _grad_work(n)
     with scope or _HERE:
-        work = torch.empty(size // 8, dtype=torch.float64, device=f"cuda:{dev}")
+        work = torch.empty(size // 8, dtype=torch.float64, device=_Torch.device(dev))
         norm, factor = work.new_empty((), dtype=torch.float32), work.new_empty((), dtype=torch.float32)
-    rc = _lib.vl_clip_grads(dev, n, t, scale, max_norm, given, norm.data_ptr(), factor.data_ptr(), work.data_ptr(), size, ptr)
+    rc = _lib.vl_clip_grads(dev, n, t.buffer_info()[0], scale, max_norm, given, norm.data_ptr(), factor.data_ptr(), work.data_ptr(), size, ptr)
     if rc != VL_OK:
         raise VlError(rc, where)
     return Clipped(norm, factor, grads if outs is None else outs)

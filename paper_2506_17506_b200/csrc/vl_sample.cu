@@ -1,7 +1,8 @@
 // vl_token_sample: checks and dispatch (the kernels are in vl_sample.cuh).
 #include "vl_sample.cuh"
 
-extern "C" uint64_t vl_sample_work(uint64_t n_rows) { return (n_rows + 16) & ~(uint64_t)15; }
+// (rows of that many entries are short ones, whatever their type and wherever they start: at most 256 vectors)
+extern "C" uint64_t vl_sample_work(uint64_t n_rows, uint32_t n_vocab) { return n_vocab <= 1020 ? 0 : 4 * n_rows; }
 
 extern "C" int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens,
                                uint32_t token_bytes, float *d_logprob, float *d_drawn_logprob, int32_t *d_kept, void *d_work, uint64_t work_bytes,
@@ -16,10 +17,11 @@ extern "C" int vl_token_sample(int device, const vl_logits *x, const vl_sampling
     if ((uintptr_t)d_tokens % token_bytes) return VL_ERR_INVALID_ARG;
     if (((uintptr_t)d_uniform | (uintptr_t)d_logprob | (uintptr_t)d_drawn_logprob | (uintptr_t)d_kept) & 3) return VL_ERR_INVALID_ARG;
     if (q.n_rows == 0) return VL_OK;
-    if (!d_uniform || !d_tokens || !d_work || work_bytes < vl_sample_work(q.n_rows)) return VL_ERR_INVALID_ARG;
+    const uint64_t work = vl_sample_work(q.n_rows, q.V);
+    if (!d_uniform || !d_tokens || (work && (!d_work || ((uintptr_t)d_work & 3) || work_bytes < work))) return VL_ERR_INVALID_ARG;
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
-    const SampleRules s{d_uniform, rules->top_k, rules->top_p, rules->min_p, static_cast<uint8_t *>(d_work)};
+    const SampleRules s{d_uniform, rules->top_k, rules->top_p, rules->min_p, static_cast<uint32_t *>(d_work)};
     const SampleOut o{d_tokens, token_bytes, d_logprob, d_drawn_logprob, d_kept};
     const auto launch = x->dtype == VL_F32 ? vl_sample_f32 : x->dtype == VL_F16 ? vl_sample_f16 : vl_sample_bf16;
     return launch(q, s, o, device, (cudaStream_t)stream) == cudaSuccess ? VL_OK : VL_ERR_CUDA;

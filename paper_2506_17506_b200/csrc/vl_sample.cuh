@@ -18,7 +18,7 @@ struct SampleRules {
     const float *uniform;  // [n_rows]
     uint32_t top_k;        // 0: all
     double top_p, min_p;
-    uint8_t *left;         // [n_rows] working memory: rows that one kernel leaves to another
+    uint32_t *left;        // [n_rows] working memory: 0, or a row that one kernel leaves to another: the key of its largest logit, 1 if that is not known
 };
 struct SampleOut {
     void *tokens;
@@ -80,8 +80,8 @@ constexpr uint32_t TEAM_PARTS = 8, TEAM_HELD = 16;  // blocks; vectors of a thre
 template <int NT>
 struct TeamMemory {
     static constexpr uint32_t NW = NT / 32, ALL = NT == 32 ? 1 : TEAM_PARTS * NW;
-    double d[2][ALL], table[EXP_TABLE];
-    uint32_t u[2][ALL][3];
+    double d[2][ALL], second[ALL], table[EXP_TABLE];
+    uint32_t u[2][ALL][3], best[NW], cut, listed;
 };
 template <int NT>
 struct Team {
@@ -149,7 +149,7 @@ struct Team {
 
 template <typename T, int NT>
 __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules &rules, const SampleOut &o, uint64_t r, TeamMemory<NT> *mem,
-                                           uint4 *held, uint32_t parts, uint32_t part)
+                                           uint4 *held, uint32_t parts, uint32_t part, uint32_t known)
 {
     Team<NT> team{mem, parts, part, 0};
     typedef typename Team<NT>::Three Three;
@@ -168,6 +168,8 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
 #pragma unroll 4
         for (uint32_t k = 0; k < TEAM_HELD; ++k)
             if (v0 + 32 * k < v1) held[k * NT + threadIdx.x] = vector(v0 + 32 * k + lane);
+        if (threadIdx.x == 0) mem->listed = 0;
+        __syncthreads();
     }
     auto each_vector = [&](auto &&f) {
 #pragma unroll 1
@@ -183,27 +185,31 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                 if (e[i] > -inf) f(e[i]);
         });
     };
-    // the largest and the smallest, how many there are, and whether something is no number (then the smallest is 0)
-    uint32_t most = 0, least = 0xFFFFFFFFu, n = 0;
-    each_vector([&](const uint4 &raw) {
-        float e[EPV<T>];
-        unpack(raw, e, T{});
-#pragma unroll
-        for (int i = 0; i < EPV<T>; ++i) {
-            const uint32_t key = e[i] < inf ? ordered(e[i]) : 0u;
-            if (key >= LEAST_KEY) { most = max(most, key); ++n; }
-            if (key != LEAST_KEY - 1) least = min(least, key);
-        }
-    });
-    const Three first = team.three({n, least, most});
-    n = first.sum;
-    most = first.most;
-    least = first.least;
+    // the largest and the smallest, how many there are (which is asked for with top_k), and whether something is no number (then the smallest is
+    // 0); unless the largest is known, and with it that all are numbers
+    uint32_t most = known, least = LEAST_KEY, n = 1;
     const bool leader = part == 0 && (NT == 32 ? lane == 0 : threadIdx.x == 0);
-    if (least == 0 || n == 0) {
-        const float v = least == 0 ? __int_as_float(0x7fc00000) : -inf;
-        if (leader) put_sample(o, r, -1, v, v, 0);
-        return;
+    if (rules.top_k || known < LEAST_KEY) {
+        Three t{0u, 0xFFFFFFFFu, 0u};
+        each_vector([&](const uint4 &raw) {
+            float e[EPV<T>];
+            unpack(raw, e, T{});
+#pragma unroll
+            for (int i = 0; i < EPV<T>; ++i) {
+                const uint32_t key = e[i] < inf ? ordered(e[i]) : 0u;
+                if (key >= LEAST_KEY) { t.most = max(t.most, key); ++t.sum; }
+                if (key != LEAST_KEY - 1) t.least = min(t.least, key);
+            }
+        });
+        t = team.three(t);
+        n = t.sum;
+        most = t.most;
+        least = t.least;
+        if (least == 0 || n == 0) {
+            const float v = least == 0 ? __int_as_float(0x7fc00000) : -inf;
+            if (leader) put_sample(o, r, -1, v, v, 0);
+            return;
+        }
     }
     const double M = (double)from_ordered(most), scale = (double)q.scale;
     auto weight = [&](float v) {
@@ -358,6 +364,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             // 32-bit terms is within NARROW of its value: (4 + 1.4 |y|) u of a weight, |y| up to 40 for what is not nothing, a thread's
             // additions to a bin (TEAM_HELD vectors; longer rows are not narrowed down).
             constexpr double NARROW = 2e-5;
+            constexpr uint32_t LISTED = NT;  // entries that are looked at one by one
             const float M32 = from_ordered(most), c = q.scale * LOG2E;
             const float per = 0x1p28f / fmaxf(fminf(M32 - from_ordered(least), 64.0f / q.scale), 1e-30f);
             auto step_of = [&](float v) { return (uint32_t)fminf((M32 - v) * per, 0x0.ffffffp28f); };
@@ -390,11 +397,14 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                 front += __shfl_sync(0xffffffffu, lane ? prev : 0.0, a);
                 hi = min(hi, lo + ((b + 1) << shift) - 1);
                 lo += a << shift;
-                // (three times: what is left is one logit of 16 bits, or some hundred of 32)
-                if (shift <= 16 || b - a > 3) break;
+                // (four times: what is left is one logit of 16 bits, or some dozen of 32)
+                if (shift <= 12 || b - a > 3) break;
                 shift = 28 - __clz(hi - lo);
             }
-            // in 64 bits: the whole sum, and what is above these steps; and which keys lie in them
+            __syncthreads();  // (the last sums have been read)
+            // in 64 bits: the whole sum, and what is above these steps; and which keys lie in them, with a list of the first ones of each block
+            uint32_t *const list_keys = reinterpret_cast<uint32_t *>(held + TEAM_HELD * NT);
+            double *const list_weights = reinterpret_cast<double *>(list_keys + 4 * LISTED);
             double sum = 0.0;
             Three t{0u, 0xFFFFFFFFu, 0u};
             each_vector([&](const uint4 &raw) {
@@ -408,19 +418,90 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                     const uint32_t at = step_of(e[i]), key = ordered(e[i]);
                     sum += w[i];
                     if (at < lo) { high += w[i]; ++high_count; }
-                    if (at >= lo && at <= hi && e[i] > -inf) { t.least = min(t.least, key); t.most = max(t.most, key); }
+                    if (at >= lo && at <= hi && e[i] > -inf) {
+                        ++t.sum;
+                        t.least = min(t.least, key);
+                        t.most = max(t.most, key);
+                        const uint32_t place = atomicAdd(&mem->listed, 1u);
+                        if (place < LISTED) {
+                            list_keys[place] = key;
+                            list_weights[place] = w[i];
+                        }
+                    }
                 }
             });
-            S = team.sum(sum);
-            above = team.sum(high);
-            t = team.three(t);
+            // (all at once: three numbers of a warp, two sums)
+            double above_own = high;
+#pragma unroll
+            for (int k = 16; k; k >>= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                above_own += __shfl_xor_sync(0xffffffffu, above_own, k);
+            }
+            t = Team<NT>::of_warp(t);
+            double *const d0 = mem->d[team.turn & 1];
+            uint32_t(*const u0)[3] = mem->u[team.turn++ & 1];
+            team.tell(d0 + warp, sum);
+            team.tell(mem->second + warp, above_own);
+            team.tell(&u0[warp][0], t.sum);
+            team.tell(&u0[warp][1], t.least);
+            team.tell(&u0[warp][2], t.most);
+            team.meet();
+            t = Three{0u, 0xFFFFFFFFu, 0u};
+            S = above = 0.0;
+            for (uint32_t w = lane; w < warps; w += 32) {
+                S += d0[w];
+                above += mem->second[w];
+                t.sum += u0[w][0];
+                t.least = min(t.least, u0[w][1]);
+                t.most = max(t.most, u0[w][2]);
+            }
+#pragma unroll
+            for (int k = 16; k; k >>= 1) {
+                S += __shfl_xor_sync(0xffffffffu, S, k);
+                above += __shfl_xor_sync(0xffffffffu, above, k);
+            }
+            t = Team<NT>::of_warp(t);
             need = rules.top_p * S;
             auto same = [&](double) { return need; };
-            cut = LEAST_KEY - 1;
+            cut = 0;
             if (above < need && t.most) {
                 upto = from_ordered(t.most);
-                cut = search(t.least, t.most, false, &above, same);
-                if (cut < t.least) cut = t.least > least ? search(least, t.least - 1, false, &above, same) : LEAST_KEY - 1;
+                if (t.least == t.most) {
+                    cut = t.least;
+                } else if (t.sum <= LISTED) {  // the first block looks at all of them
+                    if (part == 0) {
+                        uint32_t *const all_keys = list_keys + 2 * LISTED;
+                        double *const all_weights = list_weights + LISTED;
+                        uint32_t front = 0;
+                        for (uint32_t p = 0; p < parts; ++p) {
+                            const uint32_t m = *cg::this_cluster().map_shared_rank(&mem->listed, p);
+                            if (threadIdx.x < m) {
+                                all_keys[front + threadIdx.x] = cg::this_cluster().map_shared_rank(list_keys, p)[threadIdx.x];
+                                all_weights[front + threadIdx.x] = cg::this_cluster().map_shared_rank(list_weights, p)[threadIdx.x];
+                            }
+                            front += m;
+                        }
+                        __syncthreads();
+                        uint32_t best = 0;
+                        if (threadIdx.x < t.sum) {
+                            const uint32_t key = all_keys[threadIdx.x];
+                            double up = above;
+                            for (uint32_t j = 0; j < t.sum; ++j) up += all_keys[j] >= key ? all_weights[j] : 0.0;
+                            if (up >= need) best = key;
+                        }
+                        best = __reduce_max_sync(0xffffffffu, best);
+                        if (lane == 0) mem->best[threadIdx.x >> 5] = best;
+                        __syncthreads();
+                        best = __reduce_max_sync(0xffffffffu, lane < Team<NT>::NW ? mem->best[lane] : 0u);
+                        if (threadIdx.x < parts) *cg::this_cluster().map_shared_rank(&mem->cut, threadIdx.x) = best;
+                    }
+                    team.meet();
+                    cut = mem->cut;
+                }
+                if (cut == 0) {
+                    cut = search(t.least, t.most, false, &above, same);
+                    if (cut < t.least) cut = t.least > least ? search(least, t.least - 1, false, &above, same) : LEAST_KEY - 1;
+                }
             } else {  // (the margin makes this an error of rounding at most)
                 above = 0.0;
                 high = 0.0;

@@ -18,6 +18,7 @@ cudaError_t launch_sample(const LogitRows &q, const SampleRules &s, const Sample
     if (masked ? (aligned ? launch_sample_short<T, true, true>(q, s, o, h, n, st) : launch_sample_short<T, true, false>(q, s, o, h, n, st))
                : (aligned ? launch_sample_short<T, false, true>(q, s, o, h, n, st) : launch_sample_short<T, false, false>(q, s, o, h, n, st)))
         return cudaGetLastError();
+    if (!s.left) return cudaErrorInvalidValue;  // (vl_sample_work is 0 for short rows alone)
     if (s.top_k || s.top_p < 1.0 || s.min_p > 0.0)
         return masked ? launch_sample_long<T, true, true>(q, s, o, h, device, st) : launch_sample_long<T, false, true>(q, s, o, h, device, st);
     return masked ? launch_sample_long<T, true, false>(q, s, o, h, device, st) : launch_sample_long<T, false, false>(q, s, o, h, device, st);

@@ -20,7 +20,7 @@ namespace {
 
 constexpr uint32_t LD_THREADS = 128, LD_WARPS = 4, LD_U = 4, LD_RING = 3, LD_SEGS = 8, LD_PARTS = 8;
 constexpr uint32_t LD_STEP = 32 * LD_U;               // vectors of a warp at a time
-constexpr uint32_t LD_CAP = 1024, LD_BINS = 128, LD_GUESS = 256;
+constexpr uint32_t LD_CAP = 1024, LD_BINS = 128, LD_GUESS = 320;
 constexpr uint32_t LD_RING_BYTES = LD_THREADS * LD_U * LD_RING * 16;
 // what follows the pass lies where its ring was: keys, then their weights, then the groups
 constexpr uint32_t LD_WEIGHTS_AT = LD_CAP * 8, LD_GROUPS_AT = LD_CAP * 16;
@@ -417,10 +417,11 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             S += v;
         }
         bool settled = false;
+        const bool number = S > 0.0 && S < 1e300 && !far_out(M, c);
         if (M == -inf && S == 0.0) {
             if (part == 0 && tid == 0) put_sample(o, r, -1, -inf, -inf, 0);
             settled = true;
-        } else if (S > 0.0 && S < 1e300 && !far_out(M, c)) {
+        } else if (number) {
             const double eps = (double)((20.5f + 1.4f * __log2f((float)q.V / (float)S)) * 0x1p-24f);
             const float L = max_nan(logf((float)S), 0.0f);
             if (!RULES) {
@@ -486,7 +487,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                         __syncthreads();
                         if (before > at) break;
                     }
-                    if (tid == 0) s.left[r] = s_found[0] ? 0 : 1;
+                    if (tid == 0) s.left[r] = s_found[0] ? 0u : ordered(M);
                 }
                 meet();
                 continue;
@@ -541,18 +542,19 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                     const float need = (float)(s.top_p * S) * 0x1p18f;
                     // no group counted in a bin or above it has a largest logit below the bin's lower end
                     auto end_of = [&](uint32_t bin) { return M - (float)(bin + 1) * width * (1.0f + 0x1p-20f) - fabsf(M) * 0x1p-22f; };
+                    const uint32_t m_all = __shfl_sync(0xffffffffu, m_up + m_own, 31);
                     float sure = -inf, guess = -inf;
 #pragma unroll
                     for (uint32_t i = 0; i < PER; ++i) {
                         n_up += n[i];
                         m_up += m[i];
                         if (sure == -inf && (s.top_k ? n_up >= s.top_k : (float)m_up >= need)) sure = end_of(lane * PER + i);
-                        if (guess == -inf && n_up >= LD_GUESS) guess = (float)m_up >= 0.5f * need ? end_of(lane * PER + i) : inf;
+                        if (guess == -inf && (m_up >= m_all - (m_all >> 6) || n_up > LD_GUESS)) guess = n_up <= LD_GUESS ? end_of(lane * PER + i) : inf;
                     }
                     // the weights of a group's other entries are not counted: where the largest ones alone are not enough, what reaches the
-                    // LD_GUESS-th may be
+                    // groups that have nearly all of these may be; if they are many, the row is broad, and nothing is listed
                     uint32_t reached = __ballot_sync(0xffffffffu, sure > -inf);
-                    if (!reached && !s.top_k) {  // (or, by far not enough, the row is broad: nothing is listed)
+                    if (!reached && !s.top_k) {
                         reached = __ballot_sync(0xffffffffu, guess > -inf);
                         sure = guess;
                     }
@@ -623,7 +625,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                                               reinterpret_cast<key_t64 *>(buffer + LD_GROUPS_AT), s_four, s_found);
             }
         }
-        if (part == 0 && tid == 0) s.left[r] = !settled;
+        if (part == 0 && tid == 0) s.left[r] = settled ? 0u : number ? ordered(M) : 1u;
         meet();
     }
 }
@@ -635,7 +637,7 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
 {
     extern __shared__ __align__(16) uint4 s_held[];  // [TEAM_HELD][RS_THREADS], then [16][RS_THREADS] sums of 64 bits
     __shared__ TeamMemory<RS_THREADS> mem;
-    __shared__ uint32_t s_warp[RS_THREADS / 32], s_row[RS_THREADS];
+    __shared__ uint32_t s_warp[RS_THREADS / 32], s_row[RS_THREADS], s_known[RS_THREADS];
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
     const uint32_t clusters = gridDim.x >> log_parts, me = blockIdx.x >> log_parts;
     if (tid < EXP_TABLE) mem.table[tid] = exp2((double)tid / EXP_TABLE);
@@ -644,7 +646,8 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
     if (parts > 1) cg::this_cluster().sync();  // (all blocks of the cluster run)
     else __syncthreads();
     for (uint64_t base = 0; base < q.n_rows; base += RS_THREADS) {
-        const bool left = base + tid < q.n_rows && s.left[base + tid];
+        const uint32_t known = base + tid < q.n_rows ? s.left[base + tid] : 0u;
+        const bool left = known != 0;
         const uint32_t some = __ballot_sync(0xffffffffu, left);
         if (!__syncthreads_or(some)) continue;
         if (lane == 0) s_warp[warp] = __popc(some);
@@ -656,11 +659,14 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
         }
         // the first of these that is the cluster's, and how many are; in the same order in each of its blocks
         const uint32_t skip = (uint32_t)((me + clusters - number % clusters) % clusters), n = all > skip ? (all - skip - 1) / clusters + 1 : 0;
-        if (left && front >= skip && (front - skip) % clusters == 0) s_row[(front - skip) / clusters] = tid;
+        if (left && front >= skip && (front - skip) % clusters == 0) {
+            s_row[(front - skip) / clusters] = tid;
+            s_known[(front - skip) / clusters] = known;
+        }
         number += all;
         __syncthreads();
         for (uint32_t i = 0; i < n; ++i) {
-            sample_row_64<T, RS_THREADS>(q, s, o, base + s_row[i], &mem, s_held, parts, part);
+            sample_row_64<T, RS_THREADS>(q, s, o, base + s_row[i], &mem, s_held, parts, part, s_known[i]);
             if (parts > 1) cg::this_cluster().sync();  // (the next row's first sums may go where this row's last ones are read)
             else __syncthreads();
         }

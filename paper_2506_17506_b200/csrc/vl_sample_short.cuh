@@ -170,7 +170,7 @@ __device__ __forceinline__ void settle(const LogitRows &q, const SampleRules &s,
     while (left) {
         const uint64_t which = __shfl_sync(0xffffffffu, (unsigned long long)r, __ffs(left) - 1);
         left &= left - 1;
-        sample_row_64<T, 32>(q, s, o, which, nullptr, nullptr, 1, 0);
+        sample_row_64<T, 32>(q, s, o, which, nullptr, nullptr, 1, 0, 0);
     }
 }
 
@@ -419,7 +419,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2)
             }
         }
         if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, L), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
-        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, nullptr, 1, 0);
+        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, nullptr, 1, 0, 0);
         }
     }
 }

@@ -28,7 +28,7 @@ def test_bad_draws(B):
     for rules in (None, (0, 0.0, 0.0), (0, -0.5, 0.0), (0, 1.0001, 0.0), (0, nan, 0.0), (0, 1.0, -0.1), (0, 1.0, 1.5), (0, 1.0, nan), (0, inf, 0.0)):
         assert call(rules) == bad, rules
     for change in (dict(uniform=None), dict(uniform=4097), dict(tokens=None), dict(tokens=4100), dict(size=1), dict(size=0), dict(size=16),
-                   dict(size=2, tokens=4097), dict(lp=4097), dict(work=None), dict(bytes_=1), dict(drawn=4098), dict(kept=4097), dict(scale=0.0), dict(scale=nan), dict(logits=None),
+                   dict(size=2, tokens=4097), dict(lp=4097), dict(work=None, n_vocab=1021, row_stride=2000), dict(bytes_=7, n_vocab=1021, row_stride=2000), dict(work=4098, n_vocab=1021, row_stride=2000), dict(drawn=4098), dict(kept=4097), dict(scale=0.0), dict(scale=nan), dict(logits=None),
                    dict(row_stride=39), dict(dtype=7), dict(n_vocab=0), dict(size=2, n_vocab=65536, row_stride=65536)):
         assert call(**change) == bad, change
     d = _logits(B, tokens=4096, token_bytes=8)
