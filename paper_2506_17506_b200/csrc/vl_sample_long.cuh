@@ -8,7 +8,7 @@
 //   such a logit, or groups whose largest entries alone have weight enough, mean that the cut is no lower.  The groups that reach the bound are
 //   read again, and what reaches it is gathered, put in order, and the rules are applied in 64 bits.
 // A row is left to k_sample_rest where a border is nearer to what it is compared with than the 32-bit terms are known (eps, below), where more
-// than LD_CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
+// than CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
 //
 // eps: a weight is within (4 + 1.4 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
 // passes by more than 3; a lane's 32 entries go through 8 additions.  The mean of |y| relative to the largest logit is at most log2(V / S).
@@ -18,13 +18,15 @@
 
 namespace {
 
-constexpr uint32_t LD_THREADS = 128, LD_WARPS = 4, LD_U = 4, LD_RING = 3, LD_SEGS = 8, LD_PARTS = 8;
+constexpr uint32_t LD_U = 4, LD_RING = 3, LD_SEGS = 8, LD_PARTS = 8;
 constexpr uint32_t LD_STEP = 32 * LD_U;               // vectors of a warp at a time
-constexpr uint32_t LD_CAP = 1024, LD_BINS = 128, LD_GUESS = 320;
-constexpr uint32_t LD_RING_BYTES = LD_THREADS * LD_U * LD_RING * 16;
-// what follows the pass lies where its ring was: keys, then their weights, then the groups
-constexpr uint32_t LD_WEIGHTS_AT = LD_CAP * 8, LD_GROUPS_AT = LD_CAP * 16;
-static_assert(LD_GROUPS_AT + LD_SEGS * LD_THREADS * 2 <= LD_RING_BYTES && LD_CAP * 24 <= LD_RING_BYTES, "fits the ring");
+constexpr uint32_t LD_BINS = 128, LD_GUESS = 320;
+// A block of NT threads: its ring, and what lies there after the pass: up to CAP keys, then their weights, then the groups.
+template <uint32_t NT>
+struct Long {
+    static constexpr uint32_t WARPS = NT / 32, RING_BYTES = NT * LD_U * LD_RING * 16, CAP = 8 * NT, WEIGHTS_AT = CAP * 8, GROUPS_AT = CAP * 16;
+    static_assert(GROUPS_AT + LD_SEGS * NT * 2 <= RING_BYTES && CAP * 24 <= RING_BYTES && NT * 24 <= RING_BYTES - GROUPS_AT, "fits the ring");
+};
 
 __device__ __forceinline__ void ld_copy(uint32_t to, const uint4 *from)
 {
@@ -33,15 +35,68 @@ __device__ __forceinline__ void ld_copy(uint32_t to, const uint4 *from)
 __device__ __forceinline__ void ld_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void ld_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A block's n keys in falling order (n <= LD_CAP).  Few: each to its rank; many: by halves.  (A key's rank among 256 takes about as many steps as the halves do.)
+// The smallest of several vectors' elements.
+template <int N>
+__device__ __forceinline__ float vectors_min(const uint4 (&r)[N], float)
+{
+    float m = __uint_as_float(r[0].x);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        m = fminf(m, fminf(fminf(__uint_as_float(r[j].x), __uint_as_float(r[j].y)), fminf(__uint_as_float(r[j].z), __uint_as_float(r[j].w))));
+    return m;
+}
+template <typename P, int N>
+__device__ __forceinline__ P halves_min(const uint4 (&r)[N])
+{
+    P m[4];
+    memcpy(m, &r[0], 16);
+#pragma unroll
+    for (int j = 1; j < N; ++j) {
+        P h[4];
+        memcpy(h, &r[j], 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = __hmin2(m[i], h[i]);
+    }
+    return __hmin2(__hmin2(m[0], m[1]), __hmin2(m[2], m[3]));
+}
+template <int N>
+__device__ __forceinline__ float vectors_min(const uint4 (&r)[N], __half)
+{
+    const __half2 m = halves_min<__half2>(r);
+    return fminf(__low2float(m), __high2float(m));
+}
+template <int N>
+__device__ __forceinline__ float vectors_min(const uint4 (&r)[N], __nv_bfloat16)
+{
+    const __nv_bfloat162 m = halves_min<__nv_bfloat162>(r);
+    return fminf(__low2float(m), __high2float(m));
+}
+
+// A vector's entries of minus infinity.
+template <typename T>
+__device__ __forceinline__ uint32_t impossible(const uint4 &r, T)
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    uint32_t n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        if (sizeof(T) == 4) n += w[j] == MINUS_INF2<T>;
+        else n += (w[j] << 16 == MINUS_INF2<T> << 16) + (w[j] >> 16 == MINUS_INF2<T> >> 16);
+    }
+    return n;
+}
+
+// A block's n keys in falling order (n <= CAP).  Few: each to its rank; many: by halves.  (A key's rank among 256 takes about as many steps as
+// the halves do.)
+template <uint32_t NT>
 __device__ __forceinline__ void sort_keys(key_t64 *keys, uint32_t n)
 {
     const uint32_t tid = threadIdx.x;
-    if (n <= 256) {
+    if (n <= 2 * NT) {
         key_t64 mine[2];
         uint32_t rank[2] = {0, 0};
         mine[0] = tid < n ? keys[tid] : 0ull;
-        mine[1] = tid + 128 < n ? keys[tid + 128] : 0ull;
+        mine[1] = tid + NT < n ? keys[tid + NT] : 0ull;
         for (uint32_t j = 0; j < n; ++j) {
             const key_t64 other = keys[j];
             rank[0] += other > mine[0];
@@ -49,17 +104,17 @@ __device__ __forceinline__ void sort_keys(key_t64 *keys, uint32_t n)
         }
         __syncthreads();
         if (tid < n) keys[rank[0]] = mine[0];
-        if (tid + 128 < n) keys[rank[1]] = mine[1];
+        if (tid + NT < n) keys[rank[1]] = mine[1];
         __syncthreads();
         return;
     }
-    uint32_t N = 512;
+    uint32_t N = 4 * NT;
     while (N < n) N *= 2;
-    for (uint32_t i = n + tid; i < N; i += LD_THREADS) keys[i] = 0ull;
+    for (uint32_t i = n + tid; i < N; i += NT) keys[i] = 0ull;
     __syncthreads();
     for (uint32_t k = 2; k <= N; k *= 2)
         for (uint32_t d = k / 2; d; d /= 2) {
-            for (uint32_t p = tid; p < N / 2; p += LD_THREADS) {
+            for (uint32_t p = tid; p < N / 2; p += NT) {
                 const uint32_t i = 2 * p - (p & (d - 1)), j = i + d;
                 const key_t64 a = keys[i], b = keys[j];
                 if ((a < b) == ((i & k) == 0)) { keys[i] = b; keys[j] = a; }
@@ -68,10 +123,11 @@ __device__ __forceinline__ void sort_keys(key_t64 *keys, uint32_t n)
         }
 }
 
-// In place: sums of the first i + 1 of n numbers (n <= LD_CAP).  s: LD_WARPS numbers.
+// In place: sums of the first i + 1 of n numbers (n <= CAP).  s: a number for each warp.
+template <uint32_t NT>
 __device__ __forceinline__ void sum_up(double *v, uint32_t n, double *s)
 {
-    const uint32_t tid = threadIdx.x, lane = tid & 31, per = (n + LD_THREADS - 1) / LD_THREADS, first = min(n, tid * per), end = min(n, first + per);
+    const uint32_t tid = threadIdx.x, lane = tid & 31, per = (n + NT - 1) / NT, first = min(n, tid * per), end = min(n, first + per);
     double own = 0.0;
     for (uint32_t i = first; i < end; ++i) own += v[i];
     double up = own;
@@ -123,14 +179,17 @@ struct Listed {
 
 // One block, at most an entry a thread: each to its rank, sums in order, and the sums in the order of the numbers by looking at all of them.
 // buffer: 24 bytes an entry.  False if that is too near to call.
+template <uint32_t NT>
 struct Few {
-    double four[LD_WARPS];
-    uint32_t counts[LD_WARPS][3], places[LD_WARPS];
+    static constexpr uint32_t NW = NT / 32;
+    double sums[NW];
+    uint32_t counts[NW][3], places[NW];
 };
-__device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, uint32_t n, unsigned char *buffer, Few &f)
+template <uint32_t NT>
+__device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, uint32_t n, unsigned char *buffer, Few<NT> &f)
 {
     key_t64 *const sorted = reinterpret_cast<key_t64 *>(buffer);
-    double *const w = reinterpret_cast<double *>(buffer + LD_THREADS * 8), *const sums = w + LD_THREADS;
+    double *const w = reinterpret_cast<double *>(buffer + NT * 8), *const sums = w + NT;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     key_t64 key = tid < n ? keys[tid] : 0ull;
     double own = tid < n ? a.weight(key) : 0.0;
@@ -152,9 +211,9 @@ __device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, u
         const double v = __shfl_up_sync(0xffffffffu, up, d);
         if (lane >= (uint32_t)d) up += v;
     }
-    if (lane == 31) f.four[warp] = up;
+    if (lane == 31) f.sums[warp] = up;
     __syncthreads();
-    for (uint32_t k = 0; k < warp; ++k) up += f.four[k];
+    for (uint32_t k = 0; k < warp; ++k) up += f.sums[k];
     sums[tid] = up;
     __syncthreads();
     uint32_t kept = a.s.top_k ? min(n, a.s.top_k) : n;
@@ -168,7 +227,7 @@ __device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, u
     __syncthreads();
     uint32_t all[3] = {0, 0, 0};
 #pragma unroll
-    for (uint32_t k = 0; k < LD_WARPS; ++k)
+    for (uint32_t k = 0; k < NT / 32; ++k)
 #pragma unroll
         for (int j = 0; j < 3; ++j) all[j] += f.counts[k][j];
     if (p) {
@@ -180,33 +239,36 @@ __device__ __forceinline__ bool draw_few(const Listed &a, const key_t64 *keys, u
     const uint32_t place = tid < kept ? key_place(key) : 0xFFFFFFFFu;
     uint32_t first = 0xFFFFFFFFu;
     if (warp * 32 < kept) {
-        double sum = 0.0;
-#pragma unroll 4
-        for (uint32_t j = 0; j < kept; ++j)
-            if (key_place(sorted[j]) <= place) sum += w[j];
+        double part[4] = {0.0, 0.0, 0.0, 0.0};  // (four additions under way)
+        for (uint32_t j0 = 0; j0 < kept; j0 += 4)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                if (j0 + j < kept && key_place(sorted[j0 + j]) <= place) part[j] += w[j0 + j];
+        const double sum = (part[0] + part[1]) + (part[2] + part[3]);
         first = __reduce_min_sync(0xffffffffu, sum > at ? place : 0xFFFFFFFFu);
     }
     if (lane == 0) f.places[warp] = first;
     __syncthreads();
-    first = min(min(f.places[0], f.places[1]), min(f.places[2], f.places[3]));
+    for (uint32_t k = 0; k < NT / 32; ++k) first = min(first, f.places[k]);
     if (place == first && tid < kept) a.put(key, total, kept);
     return first != 0xFFFFFFFFu;
 }
 
-// The same for n keys in any order (n <= LD_CAP): sorted, summed up, cut; what is kept is sorted by its numbers and summed up again.
-__device__ __forceinline__ bool draw_many(const Listed &a, key_t64 *keys, uint32_t n, double *w, key_t64 *second, double *s_four, uint32_t *s_found)
+// The same for n keys in any order (n <= CAP): sorted, summed up, cut; what is kept is sorted by its numbers and summed up again.
+template <uint32_t NT>
+__device__ __forceinline__ bool draw_many(const Listed &a, key_t64 *keys, uint32_t n, double *w, key_t64 *second, double *s_sums, uint32_t *s_found)
 {
     const uint32_t tid = threadIdx.x;
     if (tid < 2) s_found[tid] = 0xFFFFFFFFu;
-    sort_keys(keys, n);
-    for (uint32_t i = tid; i < n; i += LD_THREADS) w[i] = a.weight(keys[i]);
+    sort_keys<NT>(keys, n);
+    for (uint32_t i = tid; i < n; i += NT) w[i] = a.weight(keys[i]);
     __syncthreads();
-    sum_up(w, n, s_four);
+    sum_up<NT>(w, n, s_sums);
     uint32_t kept = a.s.top_k ? min(n, a.s.top_k) : n;
     if (a.s.top_p < 1.0) {
         const double need = a.s.top_p * (a.s.top_k ? w[kept - 1] : a.S), lacks = a.s.top_k ? 0.0 : a.eps * need;
         uint32_t first = 0xFFFFFFFFu;
-        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += NT)
             if (w[i] >= need) first = i;
         first = block_min(first, s_found);
         if (first != 0xFFFFFFFFu) {
@@ -218,20 +280,20 @@ __device__ __forceinline__ bool draw_many(const Listed &a, key_t64 *keys, uint32
     }
     if (a.s.min_p > 0.0) {
         uint32_t first = 0xFFFFFFFFu;
-        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+        for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += NT)
             if (key_value(keys[i]) < a.least) first = i;
         kept = min(kept, block_min(first, s_found + 1));
     }
     const double total = w[kept - 1], at = (double)a.u * total;
-    for (uint32_t i = tid; i < kept; i += LD_THREADS) second[i] = (key_t64)(0xFFFFFFFFu - key_place(keys[i])) << 32 | i;
+    for (uint32_t i = tid; i < kept; i += NT) second[i] = (key_t64)(0xFFFFFFFFu - key_place(keys[i])) << 32 | i;
     __syncthreads();
-    sort_keys(second, kept);
-    for (uint32_t i = tid; i < kept; i += LD_THREADS) w[i] = a.weight(keys[(uint32_t)second[i]]);
+    sort_keys<NT>(second, kept);
+    for (uint32_t i = tid; i < kept; i += NT) w[i] = a.weight(keys[(uint32_t)second[i]]);
     if (tid == 0) s_found[0] = 0xFFFFFFFFu;
     __syncthreads();
-    sum_up(w, kept, s_four);
+    sum_up<NT>(w, kept, s_sums);
     uint32_t first = 0xFFFFFFFFu;
-    for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += LD_THREADS)
+    for (uint32_t i = tid; i < kept && first == 0xFFFFFFFFu; i += NT)
         if (w[i] > at) first = i;
     first = block_min(first, s_found);
     if (first == 0xFFFFFFFFu) return false;
@@ -239,20 +301,88 @@ __device__ __forceinline__ bool draw_many(const Listed &a, key_t64 *keys, uint32
     return true;
 }
 
-template <typename T, bool MASKED, bool RULES, bool CLUSTER>
-__global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q, const SampleRules s, const SampleOut o, const ShortRules h,
+// An entry of a vector's word.
+__device__ __forceinline__ float entry_of(uint32_t word, int, float) { return __uint_as_float(word); }
+__device__ __forceinline__ float entry_of(uint32_t word, int high, __half) { return __half2float(__ushort_as_half((unsigned short)(high ? word >> 16 : word))); }
+__device__ __forceinline__ float entry_of(uint32_t word, int high, __nv_bfloat16) { return __uint_as_float(high ? word & 0xFFFF0000u : word << 16); }
+
+// A block reads the vectors from .. to - 1 of a row again, NT at a time, in the order of the numbers, for the entry up to which the sum is above
+// `at`; before: the sum in front of them; back: a weight's part that its rounded reference lacks.  *found becomes 1 if no border is nearer than slack.
+struct Segment {
+    uint64_t r;
+    uint32_t from, to, kept;
+    double before, at, slack, back;
+    float M, L;
+};
+template <typename T, bool MASKED, uint32_t NT>
+__device__ __forceinline__ void find_in_segment(const LogitRows &q, const SampleOut &o, const Segment g, double *s_sums, uint32_t *found)
+{
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const RowVectors<T> x(static_cast<const T *>(q.x) + g.r * q.stride, q.V);
+    const RowMask mask = row_mask(q, g.r);
+    double before = g.before;
+    for (uint32_t w0 = g.from; w0 < g.to; w0 += NT) {
+        const uint32_t v = w0 + tid;
+        uint4 raw = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
+        if (v < g.to) raw = open_vector<T, MASKED>(x, mask, v);
+        float xs[EPV<T>], e[EPV<T>];
+        unpack(raw, xs, T{});
+        powers<T>(xs, g.M, q.scale * LOG2E, false, e);
+        const double own = (double)sum_of(e) * g.back;
+        double up = own;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const double t = __shfl_up_sync(0xffffffffu, up, d);
+            if (lane >= (uint32_t)d) up += t;
+        }
+        if (lane == 31) s_sums[warp] = up;
+        __syncthreads();
+        double front = before;
+        for (uint32_t k = 0; k < NT / 32; ++k) {
+            if (k < warp) front += s_sums[k];
+            before += s_sums[k];
+        }
+        double cum = front + (up - own);
+        if (cum <= g.at && front + up > g.at) {
+            const float c = q.scale * LOG2E, b = -__fmul_rn(g.M, c);
+#pragma unroll 1
+            for (int i = 0; i < EPV<T>; ++i) {  // (one lane, once a row: few registers)
+                const int at = i / (EPV<T> / 4);
+                const uint32_t word = at == 0 ? raw.x : at == 1 ? raw.y : at == 2 ? raw.z : raw.w;
+                const float v = entry_of(word, i & 1, T{});
+                const double next = cum + (double)ex2(__fmaf_rn(v, c, b)) * g.back;
+                if (next > g.at) {
+                    if (g.at >= cum + g.slack && next >= g.at + g.slack) {
+                        const float lp = min_nan(log_odds(v, g.M, q.scale) - g.L, 0.0f);
+                        put_sample(o, g.r, (int64_t)x.first(w0 + tid) + i, lp, lp, g.kept);
+                        *found = 1;
+                    }
+                    break;
+                }
+                cum = next;
+            }
+        }
+        __syncthreads();
+        if (before > g.at) break;
+    }
+}
+
+template <typename T, bool MASKED, bool RULES, bool CLUSTER, uint32_t NT>
+__global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q, const SampleRules s, const SampleOut o, const ShortRules h,
                                                               uint32_t log_of_parts)
 {
-    constexpr uint32_t NT = LD_THREADS, U = LD_U, RING = LD_RING, MAX_PARTS = CLUSTER ? LD_PARTS : 1;
-    constexpr uint32_t RECS = RULES ? LD_WARPS : LD_WARPS * LD_SEGS;  // sums of a part
+    typedef Long<NT> K;
+    constexpr uint32_t U = LD_U, RING = LD_RING, NW = K::WARPS, MAX_PARTS = CLUSTER ? LD_PARTS : 1;
+    static_assert(!CLUSTER || NT == LD_BINS, "a thread for each bin");
+    constexpr uint32_t RECS = RULES ? NW : NW * LD_SEGS;  // sums of a part
     const uint32_t log_parts = CLUSTER ? log_of_parts : 0, parts = 1u << log_parts, part = blockIdx.x & (parts - 1);
     extern __shared__ __align__(16) uint4 s_ring[];
     __shared__ T s_most[RULES ? LD_SEGS : 1][RULES ? NT : 1];
-    __shared__ double s_sum[MAX_PARTS * RECS], s_four[LD_WARPS];
-    __shared__ float s_ref[MAX_PARTS * RECS], s_max[MAX_PARTS * LD_WARPS], s_min[MAX_PARTS * LD_WARPS], s_bound;
-    __shared__ uint32_t s_count[MAX_PARTS * LD_WARPS], s_bins[RULES ? LD_BINS : 1], s_mass[RULES ? LD_BINS : 1], s_n[3], s_found[2], s_base;
+    __shared__ double s_sum[MAX_PARTS * RECS], s_sums[NW];
+    __shared__ float s_ref[MAX_PARTS * RECS], s_max[MAX_PARTS * NW], s_min[MAX_PARTS * NW], s_bound;
+    __shared__ uint32_t s_count[MAX_PARTS * NW], s_bins[RULES ? LD_BINS : 1], s_mass[RULES ? LD_BINS : 1], s_n[3], s_found[2], s_base;
     __shared__ double s_table[EXP_TABLE];
-    __shared__ Few s_few;
+    __shared__ Few<NT> s_few;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const uint64_t step = gridDim.x >> log_parts;
     const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), margin = 3.0f / c;
@@ -265,7 +395,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
         else __syncthreads();
     };
     pdl_go();
-    if (tid < EXP_TABLE) s_table[tid] = exp2((double)tid / EXP_TABLE);
+    for (uint32_t i = tid; i < EXP_TABLE; i += NT) s_table[i] = exp2((double)i / EXP_TABLE);
     if (CLUSTER) cluster.sync();  // (all blocks of the cluster run)
 
     for (uint64_t r = blockIdx.x >> log_parts; r < q.n_rows; r += step) {
@@ -282,7 +412,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
         // the block's part of the row, and the warp's run of that, in vectors
         const uint32_t per_part = (x.n + parts - 1) >> log_parts;
         const uint32_t p0 = min(x.n, part * per_part), p1 = min(x.n, p0 + per_part);
-        const uint32_t per = ((p1 - p0 + LD_WARPS - 1) / LD_WARPS + 7) & ~7u;
+        const uint32_t per = ((p1 - p0 + NW - 1) / NW + 7) & ~7u;
         const uint32_t v0 = min(p1, p0 + warp * per), v1 = min(p1, v0 + per);
         const uint32_t steps = (v1 - v0 + LD_STEP - 1) / LD_STEP;
         const uint32_t seg_steps = ((per + LD_STEP - 1) / LD_STEP + LD_SEGS - 1) / LD_SEGS;  // the same in every warp of the block
@@ -332,6 +462,13 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                 copy_step();
                 const float m = vectors_max<(int)U>(raw, T{});
                 group = fmaxf(group, m);
+                if (!RULES) {  // impossible entries are few: they are looked for where the smallest is one
+                    count += U * EPV<T>;
+                    if (vectors_min<(int)U>(raw, T{}) == -inf) {
+#pragma unroll
+                        for (uint32_t j = 0; j < U; ++j) count -= impossible(raw[j], T{});
+                    }
+                }
                 if (__any_sync(0xffffffffu, m > limit)) {
                     const float top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(m)));
                     limit = top + margin;
@@ -353,7 +490,6 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                         float y0, y1;
                         apart(fma2(both(e[i], e[i + 1]), c2, low), y0, y1);
                         acc[j] = add2(acc[j], both(ex2(y0), ex2(y1)));
-                        if (!RULES) count += (e[i] > -inf) + (e[i + 1] > -inf);
                     }
                 }
                 float a0, a1;
@@ -384,7 +520,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             count = __reduce_add_sync(0xffffffffu, count);
         }
         if (lane < parts) {
-            const uint32_t at = part * LD_WARPS + warp;
+            const uint32_t at = part * NW + warp;
             *away(&s_max[at], lane) = most;
             if (RULES) {
                 *away(&s_min[at], lane) = least;
@@ -395,13 +531,13 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             }
         }
         if (RULES) {
-            if (tid < LD_BINS) s_bins[RULES ? tid : 0] = s_mass[RULES ? tid : 0] = 0;
+            for (uint32_t i = tid; i < LD_BINS; i += NT) s_bins[RULES ? i : 0] = s_mass[RULES ? i : 0] = 0;
             if (tid < 3) s_n[tid] = 0;
         }
         meet();
 
         // M and S relative to it, the same in every thread
-        const uint32_t warps = parts * LD_WARPS;  // at most 32
+        const uint32_t warps = parts * NW;  // at most 32
         const float M = from_ordered(__reduce_max_sync(0xffffffffu, lane < warps ? ordered(s_max[lane]) : 0u));
         const float low = RULES ? from_ordered(__reduce_min_sync(0xffffffffu, lane < warps ? ordered(s_min[lane]) : 0xFFFFFFFFu)) : 0.0f;
         count = RULES ? 0u : __reduce_add_sync(0xffffffffu, lane < warps ? s_count[lane] : 0u);
@@ -430,7 +566,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                 double before = 0.0;
                 uint32_t mine = 0xFFFFFFFFu;
                 for (uint32_t i0 = 0; i0 < parts * RECS && mine == 0xFFFFFFFFu; i0 += 32) {
-                    const double own = relative(i0 + lane);
+                    const double own = i0 + lane < parts * RECS ? relative(i0 + lane) : 0.0;
                     double up = own;
 #pragma unroll
                     for (int d = 1; d < 32; d *= 2) {
@@ -449,44 +585,8 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                     __syncthreads();
                     const uint32_t w = mine % RECS / LD_SEGS, a = min(p1, p0 + w * per), b = min(p1, a + per);
                     const uint32_t from = min(b, a + (mine % LD_SEGS) * seg_steps * LD_STEP), to = min(b, from + seg_steps * LD_STEP);
-                    const double back = exp_below_1(((double)__fmul_rn(M, c) - cM) * LN2_64, s_table), slack = 0.5 * eps * S;
-                    for (uint32_t w0 = from; w0 < to; w0 += NT) {
-                        const uint32_t v = w0 + tid;
-                        uint4 raw = make_uint4(MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>, MINUS_INF2<T>);
-                        if (v < to) raw = open_vector<T, MASKED>(x, mask, v);
-                        float xs[EPV<T>], e[EPV<T>];
-                        unpack(raw, xs, T{});
-                        powers<T>(xs, M, c, false, e);
-                        const double own = (double)sum_of(e) * back;
-                        double up = own;
-#pragma unroll
-                        for (int d = 1; d < 32; d *= 2) {
-                            const double t = __shfl_up_sync(0xffffffffu, up, d);
-                            if (lane >= (uint32_t)d) up += t;
-                        }
-                        if (lane == 31) s_four[warp] = up;
-                        __syncthreads();
-                        double front = before;
-                        for (uint32_t k = 0; k < LD_WARPS; ++k) {
-                            if (k < warp) front += s_four[k];
-                            before += s_four[k];
-                        }
-                        double cum = front + (up - own);
-                        if (cum <= at && front + up > at) {
-#pragma unroll
-                            for (int i = 0; i < EPV<T>; ++i) {
-                                const double next = cum + (double)e[i] * back;
-                                if (cum <= at && next > at && at >= cum + slack && next >= at + slack) {
-                                    const float lp = min_nan(log_odds(xs[i], M, q.scale) - L, 0.0f);
-                                    put_sample(o, r, (int64_t)x.first(v) + i, lp, lp, count);
-                                    s_found[0] = 1;
-                                }
-                                cum = next;
-                            }
-                        }
-                        __syncthreads();
-                        if (before > at) break;
-                    }
+                    const double back = exp_below_1(((double)__fmul_rn(M, c) - cM) * LN2_64, s_table);
+                    find_in_segment<T, MASKED, NT>(q, o, Segment{r, from, to, count, before, at, 0.5 * eps * S, back, M, L}, s_sums, s_found);
                     if (tid == 0) s.left[r] = s_found[0] ? 0u : ordered(M);
                 }
                 meet();
@@ -568,7 +668,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             const float bound = s_bound;
             const bool all = s.min_p == 0.0 || bound != from;  // (else min_p decides what is listed)
             // the groups that reach it, and of these the entries
-            uint16_t *const groups = reinterpret_cast<uint16_t *>(buffer + LD_GROUPS_AT);
+            uint16_t *const groups = reinterpret_cast<uint16_t *>(buffer + K::GROUPS_AT);
 #pragma unroll 1
             for (uint32_t seg = 0; seg < LD_SEGS; ++seg)
                 if (to_f32(s_most[RULES ? seg : 0][RULES ? tid : 0]) >= bound) groups[atomicAdd(&s_n[1], 1u)] = (uint16_t)(seg * NT + tid);
@@ -602,7 +702,7 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
                     for (int i = 0; i < EPV<T>; ++i)
                         if (e[i] >= bound) {
                             const uint32_t place = atomicAdd(&s_n[0], 1u);
-                            if (place < LD_CAP) list[place] = rank_key(e[i], (uint32_t)(x.first(at[k]) + i));
+                            if (place < K::CAP) list[place] = rank_key(e[i], (uint32_t)(x.first(at[k]) + i));
                         }
                 }
             }
@@ -611,18 +711,18 @@ __global__ void __launch_bounds__(LD_THREADS, 8) k_sample_long(const LogitRows q
             if (CLUSTER) {  // to the first block
                 if (tid == 0) s_base = atomicAdd(away(&s_n[2], 0), n);
                 __syncthreads();
-                key_t64 *const to = away(reinterpret_cast<key_t64 *>(buffer + LD_WEIGHTS_AT), 0);
-                for (uint32_t i = tid; i < min(n, LD_CAP); i += NT)
-                    if (s_base + i < LD_CAP) to[s_base + i] = list[i];
+                key_t64 *const to = away(reinterpret_cast<key_t64 *>(buffer + K::WEIGHTS_AT), 0);
+                for (uint32_t i = tid; i < min(n, K::CAP); i += NT)
+                    if (s_base + i < K::CAP) to[s_base + i] = list[i];
                 meet();
                 n = s_n[2];
-                list = reinterpret_cast<key_t64 *>(buffer + LD_WEIGHTS_AT);
+                list = reinterpret_cast<key_t64 *>(buffer + K::WEIGHTS_AT);
             }
-            if (part == 0 && n <= LD_CAP && n > 0) {
+            if (part == 0 && n <= K::CAP && n > 0) {
                 const Listed a{q, s, o, s_table, r, u, M, from, L, S, eps, all};
-                settled = n <= NT ? draw_few(a, list, n, buffer + LD_GROUPS_AT, s_few)
-                                  : draw_many(a, list, n, reinterpret_cast<double *>(buffer + (CLUSTER ? 0 : LD_WEIGHTS_AT)),
-                                              reinterpret_cast<key_t64 *>(buffer + LD_GROUPS_AT), s_four, s_found);
+                settled = n <= NT ? draw_few<NT>(a, list, n, buffer + K::GROUPS_AT, s_few)
+                                  : draw_many<NT>(a, list, n, reinterpret_cast<double *>(buffer + (CLUSTER ? 0 : K::WEIGHTS_AT)),
+                                              reinterpret_cast<key_t64 *>(buffer + K::GROUPS_AT), s_sums, s_found);
             }
         }
         if (part == 0 && tid == 0) s.left[r] = settled ? 0u : number ? ordered(M) : 1u;
@@ -673,12 +773,12 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
     }
 }
 
-template <typename T, bool MASKED, bool RULES, bool CLUSTER>
+template <typename T, bool MASKED, bool RULES, bool CLUSTER, uint32_t NT>
 cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, uint32_t log_parts, int device,
                             cudaStream_t st)
 {
-    constexpr auto kernel = k_sample_long<T, MASKED, RULES, CLUSTER>;
-    const cudaError_t e = allow_smem<kernel, (int)LD_RING_BYTES>(device);
+    constexpr auto kernel = k_sample_long<T, MASKED, RULES, CLUSTER, NT>;
+    const cudaError_t e = allow_smem<kernel, (int)Long<NT>::RING_BYTES>(device);
     if (e != cudaSuccess) return e;
     const uint32_t parts = 1u << log_parts;
     cudaLaunchAttribute at{};
@@ -686,7 +786,7 @@ cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const Samp
     at.val.clusterDim.x = parts;
     at.val.clusterDim.y = at.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.blockDim = LD_THREADS; cfg.dynamicSmemBytes = LD_RING_BYTES; cfg.stream = st;
+    cfg.blockDim = NT; cfg.dynamicSmemBytes = Long<NT>::RING_BYTES; cfg.stream = st;
     cfg.attrs = &at; cfg.numAttrs = CLUSTER ? 1 : 0;
     const uint64_t most = (1ull << 30) >> log_parts;
     cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
@@ -694,16 +794,19 @@ cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const Samp
     return cudaLaunchKernelEx(&cfg, kernel, q, s, o, h, log_parts);
 }
 
+constexpr uint32_t SMALL_ROWS = 2048;
 template <typename T, bool MASKED, bool RULES>
 cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, int device, cudaStream_t st)
 {
-    const uint64_t resident = 8 * (uint64_t)vl_device_sm_count(device);
     const uint32_t n = q.V / EPV<T>;
     uint32_t log_parts = 0;
+    const uint64_t sms = (uint64_t)vl_device_sm_count(device);
     if (n >= 2048)
-        while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= (n >> (log_parts + 1) > 2048 ? resident : resident * 2 / 5)) ++log_parts;
-    const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true>(q, s, o, h, log_parts, device, st)
-                                    : run_sample_long<T, MASKED, RULES, false>(q, s, o, h, 0, device, st);
+        while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= sms * 8 / 3 && n >> log_parts >= 4096) ++log_parts;
+    const bool small = n <= SMALL_ROWS && q.n_rows >= 4 * sms;
+    const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true, 128>(q, s, o, h, log_parts, device, st)
+                          : small   ? run_sample_long<T, MASKED, RULES, false, 32>(q, s, o, h, 0, device, st)
+                                    : run_sample_long<T, MASKED, RULES, false, 128>(q, s, o, h, 0, device, st);
     if (e != cudaSuccess) return e;
     constexpr auto rest = k_sample_rest<T>;
     if (const cudaError_t f = allow_smem<rest, (int)RS_BYTES>(device); f != cudaSuccess) return f;
