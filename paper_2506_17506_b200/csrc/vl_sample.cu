@@ -1,4 +1,6 @@
 // vl_token_sample: checks and dispatch (the kernels are in vl_sample.cuh).
+#include <math.h>
+
 #include "vl_sample.cuh"
 
 // (rows of that many entries are short ones, whatever their type and wherever they start: at most 256 vectors)
@@ -21,7 +23,8 @@ extern "C" int vl_token_sample(int device, const vl_logits *x, const vl_sampling
     if (!d_uniform || !d_tokens || (work && (!d_work || ((uintptr_t)d_work & 3) || work_bytes < work))) return VL_ERR_INVALID_ARG;
     const DeviceScope scope(device);
     if (scope.error != cudaSuccess) return VL_ERR_CUDA;
-    const SampleRules s{d_uniform, rules->top_k, rules->top_p, rules->min_p, static_cast<uint32_t *>(d_work)};
+    const SampleRules s{d_uniform, rules->top_k, rules->top_p, rules->min_p,
+                        rules->min_p > 0.0 ? log(rules->min_p) / (double)x->scale : -HUGE_VAL, static_cast<uint32_t *>(d_work)};
     const SampleOut o{d_tokens, token_bytes, d_logprob, d_drawn_logprob, d_kept};
     const auto launch = x->dtype == VL_F32 ? vl_sample_f32 : x->dtype == VL_F16 ? vl_sample_f16 : vl_sample_bf16;
     return launch(q, s, o, device, (cudaStream_t)stream) == cudaSuccess ? VL_OK : VL_ERR_CUDA;

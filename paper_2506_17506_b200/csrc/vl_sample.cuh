@@ -17,7 +17,7 @@
 struct SampleRules {
     const float *uniform;  // [n_rows]
     uint32_t top_k;        // 0: all
-    double top_p, min_p;
+    double top_p, min_p, drop;  // drop: ln min_p / scale, minus infinity without min_p
     uint32_t *left;        // [n_rows] working memory: 0, or a row that one kernel leaves to another: the key of its largest logit, 1 if that is not known
 };
 struct SampleOut {
@@ -542,7 +542,17 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         }
         return front;
     };
-    for (bool by_min = false;;) {
+    // min_p keeps the logits from `lowest` on: where the cut is lower, these alone decide
+    const uint32_t lowest = ordered(fmaxf(__double2float_ru(M + rules.drop), LOWEST));
+    const bool by_min = rules.min_p > 0.0 && cut < lowest;
+    if (by_min) {
+        cut = lowest - 1;
+        ties = 0;
+        high = 0.0;
+        high_count = 0;
+        upto = inf;
+    }
+    {
         level = cut < LEAST_KEY ? -inf : from_ordered(cut);
         sum = high;
         count = high_count;
@@ -584,28 +594,13 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             above = 0.0;
             there = runs([&](uint32_t, double, double incl, uint32_t, uint32_t) { above += __shfl_sync(0xffffffffu, incl, 31); });
         }
-        if (by_min) break;  // (what is above this cut is kept, and none of its ties)
         const double w = level > -inf ? weight(level) : 0.0;
-        if (shares && level > -inf) {
+        if (shares && level > -inf && !by_min) {
             const uint32_t most_ties = cut == first_cut ? first_ties : there;
             const double m = w > 0.0 ? ceil((need - above) / w) : 1.0;
             ties = (uint32_t)min(max(m, 1.0), (double)most_ties);
         }
         tie = ties ? w : 0.0;
-        if (!(rules.min_p > 0.0 && w < rules.min_p)) break;
-        uint32_t lo = max(cut, LEAST_KEY - 1), hi = most;  // the lowest key whose weight is enough: above lo, at most hi
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (exp(scale * ((double)from_ordered(mid) - M)) >= rules.min_p) hi = mid;
-            else lo = mid;
-        }
-        cut = hi - 1;
-        ties = 0;
-        tie = 0.0;
-        high = 0.0;
-        high_count = 0;
-        upto = inf;
-        by_min = true;
     }
     if (NT == 32) {
         total = sum + (double)min(equal, ties) * tie;

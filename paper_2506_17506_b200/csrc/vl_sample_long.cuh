@@ -11,8 +11,9 @@
 // than CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
 //
 // eps: a weight is within (4 + 1.4 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
-// passes by more than 3; a lane's 32 entries go through 8 additions.  The mean of |y| relative to the largest logit is at most log2(V / S).
-// Sums are therefore within eps S, eps = (20 + 1.4 log2(V / S)) u.
+// passes by more than 3; a lane's 32 entries go through 8 additions, and 64 bits hold what these make.  The mean of |y| relative to the largest logit
+// is at most log2(V / S).  S is therefore known to eps S, eps = (16 + 1.4 (log2(V / S) + 3)) u, and a border between two parts of it as in the
+// short rows.
 #pragma once
 #include "vl_sample_short.cuh"
 
@@ -368,7 +369,7 @@ __device__ __forceinline__ void find_in_segment(const LogitRows &q, const Sample
 }
 
 template <typename T, bool MASKED, bool RULES, bool CLUSTER, uint32_t NT>
-__global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q, const SampleRules s, const SampleOut o, const ShortRules h,
+__global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q, const SampleRules s, const SampleOut o,
                                                               uint32_t log_of_parts)
 {
     typedef Long<NT> K;
@@ -558,7 +559,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
             if (part == 0 && tid == 0) put_sample(o, r, -1, -inf, -inf, 0);
             settled = true;
         } else if (number) {
-            const double eps = (double)((20.5f + 1.4f * __log2f((float)q.V / (float)S)) * 0x1p-24f);
+            const float mean = 1.4f * __log2f((float)q.V / (float)S) + 5.0f;  // (of what a weight's power of two costs; the references add up to 3)
+            const double eps = (double)((16.0f + mean) * 0x1p-24f);
+            // what a border between two parts of S is known to
+            const double slack = S * (double)(0x1p-24f * (8.0f * u * (1.0f - u) + mean * fmaxf(u, 1.0f - u) + 24.0f * u + 4.0f));
             const float L = max_nan(logf((float)S), 0.0f);
             if (!RULES) {
                 // the segment that the number falls into, and what lies in front of it
@@ -586,7 +590,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
                     const uint32_t w = mine % RECS / LD_SEGS, a = min(p1, p0 + w * per), b = min(p1, a + per);
                     const uint32_t from = min(b, a + (mine % LD_SEGS) * seg_steps * LD_STEP), to = min(b, from + seg_steps * LD_STEP);
                     const double back = exp_below_1(((double)__fmul_rn(M, c) - cM) * LN2_64, s_table);
-                    find_in_segment<T, MASKED, NT>(q, o, Segment{r, from, to, count, before, at, 0.5 * eps * S, back, M, L}, s_sums, s_found);
+                    find_in_segment<T, MASKED, NT>(q, o, Segment{r, from, to, count, before, at, slack, back, M, L}, s_sums, s_found);
                     if (tid == 0) s.left[r] = s_found[0] ? 0u : ordered(M);
                 }
                 meet();
@@ -620,7 +624,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
                 __syncthreads();
             }
             const uint32_t *const bins = CLUSTER ? reinterpret_cast<uint32_t *>(buffer) : s_bins, *const mass = CLUSTER ? bins + LD_BINS : s_mass;
-            const float from = fmaxf(__double2float_ru((double)M + h.drop), LOWEST);  // of min_p
+            const float from = fmaxf(__double2float_ru((double)M + s.drop), LOWEST);  // of min_p
             if (warp == 0) {
                 float bound = LOWEST;
                 if (s.top_k || s.top_p < 1.0) {
@@ -774,7 +778,7 @@ __global__ void __launch_bounds__(RS_THREADS) k_sample_rest(const LogitRows q, c
 }
 
 template <typename T, bool MASKED, bool RULES, bool CLUSTER, uint32_t NT>
-cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, uint32_t log_parts, int device,
+cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, uint32_t log_parts, int device,
                             cudaStream_t st)
 {
     constexpr auto kernel = k_sample_long<T, MASKED, RULES, CLUSTER, NT>;
@@ -791,12 +795,12 @@ cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const Samp
     const uint64_t most = (1ull << 30) >> log_parts;
     cfg.gridDim = dim3((uint32_t)((q.n_rows < most ? q.n_rows : most) * parts));
     g_vl_launches.fetch_add(1);
-    return cudaLaunchKernelEx(&cfg, kernel, q, s, o, h, log_parts);
+    return cudaLaunchKernelEx(&cfg, kernel, q, s, o, log_parts);
 }
 
 constexpr uint32_t SMALL_ROWS = 2048;
 template <typename T, bool MASKED, bool RULES>
-cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, int device, cudaStream_t st)
+cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
 {
     const uint32_t n = q.V / EPV<T>;
     uint32_t log_parts = 0;
@@ -804,9 +808,9 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     if (n >= 2048)
         while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= sms * 8 / 3 && n >> log_parts >= 4096) ++log_parts;
     const bool small = n <= SMALL_ROWS && q.n_rows >= 4 * sms;
-    const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true, 128>(q, s, o, h, log_parts, device, st)
-                          : small   ? run_sample_long<T, MASKED, RULES, false, 32>(q, s, o, h, 0, device, st)
-                                    : run_sample_long<T, MASKED, RULES, false, 128>(q, s, o, h, 0, device, st);
+    const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true, 128>(q, s, o, log_parts, device, st)
+                          : small   ? run_sample_long<T, MASKED, RULES, false, 32>(q, s, o, 0, device, st)
+                                    : run_sample_long<T, MASKED, RULES, false, 128>(q, s, o, 0, device, st);
     if (e != cudaSuccess) return e;
     constexpr auto rest = k_sample_rest<T>;
     if (const cudaError_t f = allow_smem<rest, (int)RS_BYTES>(device); f != cudaSuccess) return f;

@@ -1,20 +1,15 @@
 // Drawing from short rows: a group of lanes, or a warp, holds a row in registers.
 //
-// Weights and sums are in 32 bits.  Each weight is within (4 + 1.4 |y|) u of its value relatively, u = 2^-24 and y its power of two (two
-// roundings in y, and the exponential's own error); the mean of |y| over the row's probabilities is at most log2 of its entries; a sum goes
-// through at most 40 additions.  So what two sums that make up a whole T differ from a border between them is known to eps T with
-// eps = (45 + 1.5 log2 entries) u: where a border is nearer than that to what it is compared with, the warp works out the row in 64 bits
-// (200,000 rows of 256 entries: some 100).
+// Weights and sums are in 32 bits, u = 2^-24.  A weight is within (4 + 1.4 |y|) u of its value relatively, y its power of two (two
+// roundings in y, and the exponential's own error), and the mean of |y| over a row's probabilities is at most log2(entries / S), S the sum relative to
+// the largest one (their entropy is at most that of equal ones).  With C the sum up to a border and T the whole one, C - a T is then known to
+//     u T (4 * 2 a (1 - a) + 1.4 log2(entries / S) max(a, 1 - a) + a (additions of C and of T) + 4):
+// the equal part of the errors is shared by C and T, the other one may be all on one side.  Where a border is nearer than that to the number
+// that it is compared with, the warp works out the row in 64 bits (some hundred of 200,000 rows of 256 entries).
 #pragma once
 #include "vl_sample.cuh"
 
 namespace {
-
-// What short kernels need beside the rules: ln min_p / scale, and eps.
-struct ShortRules {
-    double drop;
-    float eps;
-};
 
 // Powers of two of a vector's entries relative to m.
 template <typename T>
@@ -53,6 +48,55 @@ __device__ __forceinline__ float log_of(float s, float m, float c)
 }
 __device__ __forceinline__ float log_ratio(float x, float m, float scale, float l) { return min_nan((0.5f * x - 0.5f * m) * (2.0f * scale) - l, 0.0f); }
 
+// A vector's entries from a logit on, counted up: halves two at a time, as numbers of their own type (up to 64 of each half, which bf16 holds).
+struct Count {
+    uint32_t n;
+    __device__ __forceinline__ explicit Count(float) : n(0) {}
+    __device__ __forceinline__ void add(const uint4 &r, float from)
+    {
+        float x[4];
+        unpack(r, x, 0.0f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n += x[i] >= from;
+    }
+    __device__ __forceinline__ uint32_t sum() const { return n; }
+};
+template <typename P, typename T>
+struct CountPairs {
+    P n;
+    __device__ __forceinline__ void add(const uint4 &r, const P &from)
+    {
+        P h[4];
+        memcpy(h, &r, 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) n = __hadd2(n, __hge2(h[i], from));
+    }
+};
+template <typename T>
+struct Counter {
+    Count c{0.0f};
+    float from;
+    __device__ __forceinline__ explicit Counter(float f) : from(f) {}
+    __device__ __forceinline__ void add(const uint4 &r) { c.add(r, from); }
+    __device__ __forceinline__ uint32_t sum() const { return c.n; }
+};
+template <>
+struct Counter<__half> {
+    CountPairs<__half2, __half> c;
+    __half2 from;
+    __device__ __forceinline__ explicit Counter(float f) : from(__half2half2(__float2half_ru(f))) { c.n = __float2half2_rn(0.0f); }
+    __device__ __forceinline__ void add(const uint4 &r) { c.add(r, from); }
+    __device__ __forceinline__ uint32_t sum() const { return (uint32_t)(__low2float(c.n) + __high2float(c.n)); }
+};
+template <>
+struct Counter<__nv_bfloat16> {
+    CountPairs<__nv_bfloat162, __nv_bfloat16> c;
+    __nv_bfloat162 from;
+    __device__ __forceinline__ explicit Counter(float f) : from(__bfloat162bfloat162(__float2bfloat16_ru(f))) { c.n = __float2bfloat162_rn(0.0f); }
+    __device__ __forceinline__ void add(const uint4 &r) { c.add(r, from); }
+    __device__ __forceinline__ uint32_t sum() const { return (uint32_t)(__low2float(c.n) + __high2float(c.n)); }
+};
+
 template <int G> __device__ __forceinline__ float group_sum(float v)
 {
 #pragma unroll
@@ -70,7 +114,7 @@ struct Keep {
 // The token of a row that a group holds, from number u, where one is wanted and the sum S over the whole row (worked out here) is one.  The
 // lane that has the token gets it in `token`, with its logit.  False where a border is too near, in every lane of the group.
 template <typename T, int G, int NV, bool PART, bool TIES>
-__device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &keep, const RowVectors<T> &x, float u, float m, float c, float eps,
+__device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &keep, const RowVectors<T> &x, float u, float m, float c,
                                      uint32_t lane, bool wanted, int64_t *token, float *x_tok, float *all, float *total, uint32_t *kept)
 {
     const uint32_t g = lane % G;
@@ -79,11 +123,13 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
     uint32_t n = 0;
     // PART: not all of them are kept
     float S = 0.0f, T_all = 0.0f;
+    Counter<T> counter(LOWEST);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         float xs[EPV<T>], e[EPV<T>];
         unpack(raw[j], xs, T{});
         powers<T>(xs, m, c, far, e);
+        if (!PART) counter.add(raw[j]);
         if (PART) {
             S += sum_of(e);
             uint32_t ties = TIES ? keep.ties[j] : 0u;
@@ -94,13 +140,11 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
                 if (!k) e[i] = 0.0f;
                 n += k;
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < EPV<T>; ++i) n += xs[i] >= LOWEST;
         }
         v[j] = sum_of(e);
         T_all += v[j];
     }
+    if (!PART) n = counter.sum();
     T_all = group_sum<G>(T_all);
     S = PART ? group_sum<G>(S) : T_all;
     *all = S;
@@ -110,7 +154,9 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
     for (int d = G / 2; d; d >>= 1) n += __shfl_xor_sync(0xffffffffu, n, d);
     *kept = n;
     // round by round: the group's vectors that the number falls into, and what lies in front of them
-    const float at = u * T_all, margin = 0.5f * eps * T_all;
+    constexpr float ADDS = EPV<T> / 2 + NV + (G == 4 ? 2 : G == 8 ? 3 : G == 16 ? 4 : 5), MORE = ADDS - EPV<T> / 2 + EPV<T> + 1;  // of T, and of C beyond
+    const float at = u * T_all;
+    const float margin = T_all * 0x1p-24f * (8.0f * u * (1.0f - u) + 1.4f * fmaxf(u, 1.0f - u) * __log2f((float)x.V / S) + u * (2.0f * ADDS + MORE) + 4.5f);
     float base = 0.0f, up = 0.0f, own = 0.0f;
     uint4 vector = raw[0];
     uint32_t ties = TIES ? keep.ties[0] : 0u, turn = 0;
@@ -164,25 +210,29 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
 
 // Rows that a group could not settle, one after another by the whole warp.
 template <typename T, int G>
-__device__ __forceinline__ void settle(const LogitRows &q, const SampleRules &s, const SampleOut &o, uint64_t r, bool open, uint32_t lane)
+__device__ __forceinline__ void settle(const LogitRows &q, const SampleRules &s, const SampleOut &o, uint64_t r, float m, bool open, uint32_t lane)
 {
     uint32_t left = __ballot_sync(0xffffffffu, open && lane % G == 0);
     while (left) {
         const uint64_t which = __shfl_sync(0xffffffffu, (unsigned long long)r, __ffs(left) - 1);
+        const uint32_t known = ordered(__shfl_sync(0xffffffffu, m, __ffs(left) - 1));
         left &= left - 1;
-        sample_row_64<T, 32>(q, s, o, which, nullptr, nullptr, 1, 0, 0);
+        sample_row_64<T, 32>(q, s, o, which, nullptr, nullptr, 1, 0, known);
     }
 }
 
 // No rules, or min_p: what is kept is told by a logit at once.
 template <typename T, bool MASKED, bool ALIGNED, bool PART, int G, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_short(const LogitRows q, const SampleRules s, const SampleOut o,
-                                                                                    const ShortRules h)
+__global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_short(const LogitRows q, const SampleRules s, const SampleOut o)
 {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane % G;
     const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), nan = __int_as_float(0x7fc00000);
-    const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS * (32 / G);
-    for (uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G); r0 < q.n_rows; r0 += step) {
+    const uint64_t r0 = ((uint64_t)blockIdx.x * SHORT_WARPS + warp) * (32 / G);
+    if (r0 >= q.n_rows) return;
+    uint64_t row = 0;
+    float most = 0.0f;
+    bool left;
+    {
         const uint64_t r = min(r0 + lane / G, q.n_rows - 1);
         const bool there = r0 + lane / G < q.n_rows;  // (the warp's last rows may not be: it works on the last one instead)
         const RowVectors<T> x(static_cast<const T *>(q.x) + r * q.stride, q.V);
@@ -196,25 +246,30 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_s
         if (m == -inf) m = 0.0f;  // (nothing possible: every power is 0)
         const bool drawn = drawn_at_all(u);
         Keep<NV> keep;
-        keep.from = fmaxf(__double2float_ru((double)m + h.drop), LOWEST);
+        keep.from = fmaxf(__double2float_ru((double)m + s.drop), LOWEST);
         int64_t token;
         float x_tok = 0.0f, S, T_all;
         uint32_t kept;
-        const bool sure = draw<T, G, NV, PART, false>(raw, keep, x, u, m, c, h.eps, lane, there && drawn, &token, &x_tok, &S, &T_all, &kept);
+        const bool sure = draw<T, G, NV, PART, false>(raw, keep, x, u, m, c, lane, there && drawn, &token, &x_tok, &S, &T_all, &kept);
         const bool some = there && drawn && S > 0.0f && S < inf;
-        if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, log_of(S, m, c)), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
+        if (token >= 0) {
+            const float lp = log_ratio(x_tok, m, q.scale, log_of(S, m, c));
+            put_sample(o, r, token, lp, PART ? log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)) : lp, kept);
+        }
         if (there && !some && g == 0) {
             const float v = !drawn ? 0.0f : S == 0.0f ? -inf : nan;
             put_sample(o, r, -1, v, v, 0);
         }
-        settle<T, G>(q, s, o, r, some && !sure, lane);
+        left = some && !sure;
+        row = r;
+        most = m;
     }
+    settle<T, G>(q, s, o, row, most, left, lane);
 }
 
 // top_k or top_p: a warp per row.  FEW: up to 32 entries are kept, by top_k.
 template <typename T, bool MASKED, bool ALIGNED, bool FEW, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o,
-                                                                                  const ShortRules h)
+__global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : NV == 1 ? 4 : NV == 5 ? 3 : 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o)
 {
     __shared__ key_t64 s_cand[FEW ? SHORT_WARPS : 1][FEW ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
@@ -346,7 +401,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2)
             among = warp_sum(sum) + (float)ties * __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(w)));
         }
         if (s.top_p < 1.0) {
-            const float need = (float)s.top_p * among, margin = h.eps * among;
+            const float need = (float)s.top_p * among, margin = among * 0x1p-24f * (60.0f + 1.4f * __log2f((float)q.V));  // (40 additions and the weights' errors)
             uint32_t lo = cut, hi = most + 1;
             float above = 0.0f;
             while (hi - lo > 1) {
@@ -385,7 +440,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2)
             }
         }
         Keep<NV> keep;
-        const float least = fmaxf(__double2float_ru((double)m + h.drop), LOWEST);
+        const float least = fmaxf(__double2float_ru((double)m + s.drop), LOWEST);
         keep.level = cut < LEAST_KEY ? -inf : from_ordered(cut);
         keep.from = cut < LEAST_KEY ? LOWEST : ties == there ? keep.level : from_ordered(cut + 1);
         const bool some_ties = sure && ties < there && keep.level >= least && cut >= LEAST_KEY;
@@ -413,9 +468,9 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2)
                     keep.ties[j] = front < ties ? ties - front : 0u;
                     before += __shfl_sync(0xffffffffu, incl, 31);
                 }
-                sure = draw<T, 32, NV, true, true>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
+                sure = draw<T, 32, NV, true, true>(raw, keep, x, u, m, c, lane, true, &token, &x_tok, &S, &T_all, &kept);
             } else {
-                sure = draw<T, 32, NV, true, false>(raw, keep, x, u, m, c, h.eps, lane, true, &token, &x_tok, &S, &T_all, &kept);
+                sure = draw<T, 32, NV, true, false>(raw, keep, x, u, m, c, lane, true, &token, &x_tok, &S, &T_all, &kept);
             }
         }
         if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, L), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
@@ -425,23 +480,23 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : 2)
 }
 
 template <typename T, bool MASKED, bool ALIGNED>
-bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleOut &o, const ShortRules &h, uint32_t n, cudaStream_t st)
+bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleOut &o, uint32_t n, cudaStream_t st)
 {
     const bool order = s.top_k || s.top_p < 1.0;
     auto run = [&](auto g, auto v) {
         constexpr int G = decltype(g)::value, NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS * (32 / G) - 1) / (SHORT_WARPS * (32 / G));
-        const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
-        if (s.min_p > 0.0) k_sample_short<T, MASKED, ALIGNED, true, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
-        else k_sample_short<T, MASKED, ALIGNED, false, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        const uint32_t grid = (uint32_t)blocks;  // (2^31 blocks have more rows than there is memory)
+        if (s.min_p > 0.0) k_sample_short<T, MASKED, ALIGNED, true, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
+        else k_sample_short<T, MASKED, ALIGNED, false, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
         g_vl_launches.fetch_add(1);
     };
     auto run_warp = [&](auto, auto v) {
         constexpr int NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS - 1) / SHORT_WARPS;
         const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
-        if (s.top_k && s.top_k <= 32) k_sample_warp<T, MASKED, ALIGNED, true, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
-        else k_sample_warp<T, MASKED, ALIGNED, false, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o, h);
+        if (s.top_k && s.top_k <= 32) k_sample_warp<T, MASKED, ALIGNED, true, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
+        else k_sample_warp<T, MASKED, ALIGNED, false, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
         g_vl_launches.fetch_add(1);
     };
     return order ? short_shape<true, ALIGNED>(n, q.W, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
