@@ -814,8 +814,10 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     if (e != cudaSuccess) return e;
     constexpr auto rest = k_sample_rest<T>;
     if (const cudaError_t f = allow_smem<rest, (int)RS_BYTES>(device); f != cudaSuccess) return f;
-    // few rows: more blocks at each; short ones have nothing to share
-    const uint32_t log_rest = n < 1024 ? 0 : q.n_rows <= 8 ? 3 : 2;
+    // Blocks at a row: where few rows can be left, or a thread would have more than eight vectors of it.  A pass over a row takes a block 2 us and
+    // more whatever the row is, and a cluster another 1: 5,000 rows of 8,192 bf16 logits of which a third is left take
+    // 213 us with one block at each, 953 with four.
+    const uint32_t log_rest = q.n_rows <= 8 && n >= 2048 ? 3 : n < 4096 ? 0 : n < 8192 ? 1 : 2;
     const uint64_t clusters = (uint64_t)vl_device_sm_count(device) >> log_rest;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

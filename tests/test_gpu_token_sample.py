@@ -279,3 +279,24 @@ def test_rows_of_a_model(B, R, V, dtype):
             assert bool(((a.double() - b).abs() <= _sum_error(V) + 3 * U * 3 * (z.abs() + 20)).all()), rules
         again = B.vl_token_sample(x, u, scale=1.1, **rules)
         assert all(torch.equal(a, b) for a, b in zip(got, again)), rules
+
+
+@pytest.mark.parametrize("R,V,dtype", [(2, 600000, "bf16"), (9, 300000, "f32"), (40, 9000, "f16"), (3, 140000, "f16")])
+def test_broad_rows_that_no_list_holds(B, R, V, dtype):
+    """Tens of thousands of entries are kept, ties among them, of rows up to ones that no shared memory holds; the same in a graph."""
+    import torch
+    kind = B._Torch.load() and {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn(R, V, generator=gen, device="cuda").mul_(1.5).to(kind)
+    x[0] = (x[0].float() * 2).round().to(kind)          # some dozen values
+    x[-1, V // 3:] = x[-1, V // 2]                      # most entries alike
+    u = torch.rand(R, generator=gen, device="cuda")
+    zeros = np.zeros((R, V), bool)
+    for rules in [dict(), dict(top_p=0.95), dict(top_p=0.4), dict(top_k=5000), dict(top_k=3000, top_p=0.7), dict(min_p=0.02, top_p=0.9), dict(min_p=0.001)]:
+        got = B.vl_token_sample(x, u, scale=0.9, **rules)
+        check(got, x.double().cpu().numpy(), 0.9, zeros, u.cpu().numpy(), rules, rows=range(min(R, 6)))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            again = B.vl_token_sample(x, u, scale=0.9, **rules)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(got, again)), rules
