@@ -184,22 +184,28 @@ def main() -> int:
         tok_off = torch.arange(0, S * D + 1, D, device="cuda")
         args_ = dict(occupied=masks, mask_rows=which, widths=widths)
 
+        uniform = torch.rand(S * D, device="cuda")
+
         def train():
+            vl.vl_token_sample(logits, uniform, top_p=0.95, **args_)    # what would have drawn the samples
+            et[4].record(stream)
             sc = vl.vl_token_logprobs(logits, tokens, **args_)
             et[1].record(stream)
             _, _, g = vl.vl_policy_loss([outs[0][:S]], tok_off, sc.logprob, bank_cost=1e-5)
             et[2].record(stream)
             vl.vl_token_logprobs_backward(logits, tokens, sc.row_stats, g, out=dlogits, **args_)
+            et[3].record(stream)
+            vl.vl_clip_grads([dlogits], 1e-3)
 
-        et = [torch.cuda.Event(enable_timing=True) for _ in range(4)]
+        et = [torch.cuda.Event(enable_timing=True) for _ in range(6)]
         parts = []
         for _ in range(3 + args.steps):
             et[0].record(stream)
             train()
-            et[3].record(stream)
+            et[5].record(stream)
             torch.cuda.synchronize()
-            parts.append([et[j].elapsed_time(et[j + 1]) * 1e3 for j in range(3)])
-        score_us, loss_us, grad_us = (float(np.median([p[j] for p in parts[3:]])) for j in range(3))
+            parts.append([et[a].elapsed_time(et[b]) * 1e3 for a, b in ((0, 4), (4, 1), (1, 2), (2, 3), (3, 5))])
+        sample_us, score_us, loss_us, grad_us, clip_us = (float(np.median([p[j] for p in parts[3:]])) for j in range(5))
         dict_bytes = (2 * d_host.shape[1] + 16) * wl.K
         occupied_us = eo[0].elapsed_time(eo[1]) / args.steps * 1e3
         diagnose_us = ed[0].elapsed_time(ed[1]) / args.steps * 1e3
@@ -225,8 +231,9 @@ def main() -> int:
             "until_pass_first_passing_row": first_pass,
             "diagnose_one_row_us": diagnose_us,
             "occupied_masks_one_row_us": occupied_us,
-            "training_step_20_samples": {"rows": S * D, "registers": int(prog.P), "token_logprobs_us": score_us, "policy_loss_us": loss_us,
-                                         "backward_us": grad_us},
+            "training_step_20_samples": {"rows": S * D, "registers": int(prog.P), "token_sample_us": sample_us,
+                                         "token_logprobs_us": score_us, "policy_loss_us": loss_us,
+                                         "backward_us": grad_us, "clip_us": clip_us},
             "dict_form_first_program": {"columns": int(len(layout[1])), "verify_dict_ms": dict_ms,
                                         "verifications_per_sec": wl.K / (dict_ms * 1e-3),
                                         "gb_per_sec": dict_bytes / (dict_ms * 1e-3) / 1e9,
