@@ -269,10 +269,11 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, short_blocks(NV)) k_sample_s
 
 // top_k or top_p: a warp per row.  FEW: up to 32 entries are kept, by top_k.
 template <typename T, bool MASKED, bool ALIGNED, bool FEW, int NV>
-__global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : NV == 1 ? 4 : NV == 5 ? 3 : 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o)
+__global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 4 ? 4 : 3) : NV <= 2 ? 4 : NV == 4 ? 3 : 2) k_sample_warp(const LogitRows q, const SampleRules s, const SampleOut o)
 {
     __shared__ key_t64 s_cand[FEW ? SHORT_WARPS : 1][FEW ? SHORT_CAND : 1];
     __shared__ uint32_t s_n[SHORT_WARPS];
+    __shared__ float s_runs[FEW ? 1 : SHORT_WARPS][FEW ? 1 : 1024];
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float c = q.scale * LOG2E, inf = __int_as_float(0x7f800000), nan = __int_as_float(0x7fc00000);
     const uint64_t step = (uint64_t)gridDim.x * SHORT_WARPS;
@@ -401,10 +402,95 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : NV
             among = warp_sum(sum) + (float)ties * __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(w)));
         }
         if (s.top_p < 1.0) {
-            const float need = (float)s.top_p * among, margin = among * 0x1p-24f * (60.0f + 1.4f * __log2f((float)q.V));  // (40 additions and the weights' errors)
+            // Where the cut lies: weights in 32 runs of half a power of two below the largest one, added up by every lane for its own entries and by a
+            // lane for each run.  What is in the run of the cut, if a warp can hold it, is put in order; else the halves begin from it.
+            const float need = (float)s.top_p * among, margin = among * 0x1p-24f * ((float)(NV * EPV<T>) + 50.0f + 1.4f * __log2f((float)q.V));  // (a lane's additions, the warp's, and the weights' errors)
             uint32_t lo = cut, hi = most + 1;
             float above = 0.0f;
-            while (hi - lo > 1) {
+            const float over = cut < LEAST_KEY ? -inf : from_ordered(cut);
+            float *const runs = s_runs[FEW ? 0 : warp] + lane;
+#pragma unroll
+            for (uint32_t k = 0; k < 32; ++k) runs[FEW ? 0 : 32 * k] = 0.0f;
+            auto run_of = [&](float v) { return (uint32_t)fminf((m - v) * c * 2.0f, 31.0f); };
+            each([&](float v, float e) {
+                if (v > over) runs[FEW ? 0 : 32 * run_of(v)] += e;
+            });
+            __syncwarp();
+            float in_run = 0.0f;
+#pragma unroll
+            for (uint32_t k = 0; k < 32; ++k) in_run += s_runs[FEW ? 0 : warp][FEW ? 0 : 32 * lane + ((k + lane) & 31)];
+            __syncwarp();
+            float up_to = in_run;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const float v = __shfl_up_sync(0xffffffffu, up_to, d);
+                if (lane >= (uint32_t)d) up_to += v;
+            }
+            const uint32_t past = __ballot_sync(0xffffffffu, up_to >= need);
+            bool listed = false;
+            if (past) {
+                const uint32_t run = __ffs(past) - 1;
+                const float front = __shfl_up_sync(0xffffffffu, up_to, 1);
+                above = __shfl_sync(0xffffffffu, lane ? front : 0.0f, run);
+                float least = inf, largest = -inf;
+                uint32_t mine = 0;
+                each([&](float v, float) {
+                    if (v > over && run_of(v) == run) {
+                        ++mine;
+                        least = fminf(least, v);
+                        largest = fmaxf(largest, v);
+                    }
+                });
+                const uint32_t all = __reduce_add_sync(0xffffffffu, mine);
+                uint32_t place = mine;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const uint32_t v = __shfl_up_sync(0xffffffffu, place, d);
+                    if (lane >= (uint32_t)d) place += v;
+                }
+                place -= mine;
+                if (all <= 32) {
+                    listed = true;
+                    float *const list = s_runs[FEW ? 0 : warp];
+                    if (mine)
+                        each([&](float v, float) {
+                            if (v > over && run_of(v) == run) list[FEW ? 0 : place++] = v;
+                        });
+                    __syncwarp();
+                    // the values in falling order, a lane at each, and their weights
+                    const bool there_is = lane < all;
+                    uint32_t key = there_is ? ordered(list[FEW ? 0 : lane]) : 0u;
+#pragma unroll
+                    for (uint32_t k = 2; k <= 32; k *= 2)
+#pragma unroll
+                        for (uint32_t d = k / 2; d; d /= 2) {
+                            const uint32_t other = __shfl_xor_sync(0xffffffffu, key, d);
+                            key = ((lane & d) == 0) == ((lane & k) == 0) ? max(key, other) : min(key, other);
+                        }
+                    const float v = there_is ? from_ordered(key) : m;
+                    float w[EPV<T>], vs[EPV<T>];
+#pragma unroll
+                    for (int i = 0; i < EPV<T>; ++i) vs[i] = v;
+                    powers<T>(vs, m, c, far, w);
+                    float sum = there_is ? w[0] : 0.0f;
+#pragma unroll
+                    for (int d = 1; d < 32; d *= 2) {
+                        const float t = __shfl_up_sync(0xffffffffu, sum, d);
+                        if (lane >= (uint32_t)d) sum += t;
+                    }
+                    const uint32_t enough = __ballot_sync(0xffffffffu, there_is && above + sum >= need);
+                    // (rounding: then it is the next run's first, which 64 bits find)
+                    const uint32_t at = enough ? __ffs(enough) - 1 : 0;
+                    lo = enough ? __shfl_sync(0xffffffffu, key, at) : LEAST_KEY - 1;
+                    const uint32_t higher = __popc(__ballot_sync(0xffffffffu, there_is && key > lo));
+                    above += higher ? __shfl_sync(0xffffffffu, sum, (higher - 1) & 31) : 0.0f;
+                    __syncwarp();
+                } else {
+                    lo = __reduce_min_sync(0xffffffffu, ordered(least));
+                    hi = __reduce_max_sync(0xffffffffu, ordered(largest)) + 1;
+                }
+            }
+            while (!listed && hi - lo > 1) {
                 const float mid = from_ordered(halve(lo, hi)), low = from_ordered(lo);
                 float sum = 0.0f, least = inf, below = -inf;
                 each([&](float v, float e) {
@@ -479,6 +565,18 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 5 ? 4 : 3) : NV
     }
 }
 
+// The vectors of a lane for rows of at most n vectors that a warp holds (a lane for every word of a mask up to four of them).
+template <typename F>
+bool warp_shape(uint32_t n, F &&f)
+{
+    using std::integral_constant;
+    if (n <= 32) f(integral_constant<int, 1>{});
+    else if (n <= 64) f(integral_constant<int, 2>{});
+    else if (n <= 128) f(integral_constant<int, 4>{});
+    else if (n <= 256) f(integral_constant<int, 8>{});
+    return n <= 256;
+}
+
 template <typename T, bool MASKED, bool ALIGNED>
 bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleOut &o, uint32_t n, cudaStream_t st)
 {
@@ -491,7 +589,7 @@ bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleO
         else k_sample_short<T, MASKED, ALIGNED, false, G, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
         g_vl_launches.fetch_add(1);
     };
-    auto run_warp = [&](auto, auto v) {
+    auto run_warp = [&](auto v) {
         constexpr int NV = decltype(v)::value;
         const uint64_t blocks = (q.n_rows + SHORT_WARPS - 1) / SHORT_WARPS;
         const uint32_t grid = (uint32_t)(blocks < (1u << 30) ? blocks : (1u << 30));
@@ -499,7 +597,7 @@ bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleO
         else k_sample_warp<T, MASKED, ALIGNED, false, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
         g_vl_launches.fetch_add(1);
     };
-    return order ? short_shape<true, ALIGNED>(n, q.W, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
+    return order ? warp_shape(n, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
 }
 
 }  // namespace
