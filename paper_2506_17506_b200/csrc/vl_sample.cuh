@@ -149,7 +149,7 @@ struct Team {
 
 template <typename T, int NT>
 __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules &rules, const SampleOut &o, uint64_t r, TeamMemory<NT> *mem,
-                                           uint4 *held, uint32_t parts, uint32_t part, uint32_t known)
+                                           uint4 *held, uint32_t parts, uint32_t part, uint32_t known, uint32_t near = 0)
 {
     Team<NT> team{mem, parts, part, 0};
     typedef typename Team<NT>::Three Three;
@@ -357,7 +357,32 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             return need = rules.top_p * sum;
         };
         double above = 0.0;
-        if (NT == 32 || !all) {
+        if (NT == 32 && near > cut) {
+            // 32 bits have found a key that the cut is at or next to: looked at as it is, and from neighbour to neighbour
+            const uint32_t none = all ? LEAST_KEY - 1 : cut;
+            double sum = team.sum(add(-inf, [&](float v) { return ordered(v) > none; }));
+            const double wanted = needed(sum);
+            uint32_t at = near;
+            bool found = false;
+            for (int tries = 0; tries < 8 && !found; ++tries) {
+                const float here = from_ordered(at);
+                double over = team.sum(add(here, [&](float v) { return v > here; })), with = over;
+                Three t{0u, 0xFFFFFFFFu, 0u};  // entries equal to it, the next key above and below
+                each(-inf, [&](float v) {
+                    const uint32_t key = ordered(v);
+                    t.sum += key == at;
+                    if (key > at) t.least = min(t.least, key);
+                    if (key < at && key > none) t.most = max(t.most, key);
+                });
+                t = team.three(t);
+                with += (double)t.sum * weight(here);
+                if (over >= wanted && t.least != 0xFFFFFFFFu) at = t.least;
+                else if (with < wanted && t.most) at = t.most;
+                else found = true;
+                if (found) cut = with >= wanted ? at : none;
+            }
+            if (!found) cut = search(all ? least : cut + 1, most, false, &above, [&](double) { return wanted; });
+        } else if (NT == 32 || !all) {
             cut = search(all ? least : cut + 1, most, false, &above, needed);
         } else {
             // Where the cut lies as far as 32 bits tell it: the logits in 2^28 steps below the largest one, sixteen runs of steps at a time.  A sum of

@@ -560,7 +560,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 4 ? 4 : 3) : NV
             }
         }
         if (token >= 0) put_sample(o, r, token, log_ratio(x_tok, m, q.scale, L), log_ratio(x_tok, m, q.scale, log_of(T_all, m, c)), kept);
-        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, nullptr, 1, 0, 0);
+        if (!sure) sample_row_64<T, 32>(q, s, o, r, nullptr, nullptr, 1, 0, ordered(m), s.top_p < 1.0 ? cut : 0u);
         }
     }
 }
