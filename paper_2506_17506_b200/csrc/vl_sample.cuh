@@ -75,7 +75,8 @@ __device__ __forceinline__ double exp_below_1(double z, const double *table)
 }
 
 // The threads at a row that they read as often as they need it: a warp (NT = 32), or `parts` blocks of a cluster.  Each warp has a run of the
-// row's vectors.  All threads hold the same results; every sum has one order.
+// row's vectors.  All threads hold the same results; every sum has one order.  A row of 131,072 bf16 logits of which 40,000 are kept takes four
+// blocks 57 us, 14 without rules: ten passes of 2 to 5 us over shared memory, one of 11 with every weight in 64 bits, a barrier after each.
 constexpr uint32_t TEAM_PARTS = 8, TEAM_HELD = 16;  // blocks; vectors of a thread that stay in shared memory
 template <int NT>
 struct TeamMemory {

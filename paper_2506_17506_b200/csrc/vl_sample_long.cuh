@@ -14,6 +14,10 @@
 // passes by more than 3; a lane's 32 entries go through 8 additions, and 64 bits hold what these make.  The mean of |y| relative to the largest logit
 // is at most log2(V / S).  S is therefore known to eps S, eps = (16 + 1.4 (log2(V / S) + 3)) u, and a border between two parts of it as in the
 // short rows.
+//
+// What bounds it: the pass reads the logits once (1,024 rows of 131,072 bf16: 42 us after the median of the rows, 65 after the last, for a floor of
+// 42: one wave of blocks, each at a row, seven to a multiprocessor), then every row has an end of about 15 us under load, most of it waiting (barriers, the second
+// look's loads, 64-bit operations one behind the other), 78 us in all; with one warp at a row, 28 ends run side by side.
 #pragma once
 #include "vl_sample_short.cuh"
 
@@ -798,15 +802,20 @@ cudaError_t run_sample_long(const LogitRows &q, const SampleRules &s, const Samp
     return cudaLaunchKernelEx(&cfg, kernel, q, s, o, log_parts);
 }
 
-constexpr uint32_t SMALL_ROWS = 2048;
+constexpr uint32_t SMALL_ROWS = 2048;  // vectors
 template <typename T, bool MASKED, bool RULES>
 cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
 {
     const uint32_t n = q.V / EPV<T>;
     uint32_t log_parts = 0;
     const uint64_t sms = (uint64_t)vl_device_sm_count(device);
-    if (n >= 2048)
-        while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= sms * 8 / 3 && n >> log_parts >= 4096) ++log_parts;
+    // Blocks of a row: more of them shorten the pass and cost barriers of 1 us; they pay where most multiprocessors would be idle and a block
+    // keeps 4,096 vectors (2,048 for a handful of rows).  Device time in us with 1, 2, 4, 8 blocks, bf16, top_k 50 and top_p 0.9: one row of 131,072
+    // 29, 26, 20, 18; 100 rows 33, 30, 26, 28; 300 rows 40, 39, 51, 69; 100 rows of 32,768 18.6, 21, 21, 24.
+    const uint32_t least = q.n_rows <= 8 ? 2048 : 4096;
+    while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= sms * 3 && n >> (log_parts + 1) >= least) ++log_parts;
+    // One warp at a row where a row is short and there are rows for all the places: it has no barriers, and 28 rows are at their ends at once
+    // instead of seven (5,000 rows of 8,192 bf16 logits 76 us with four warps at each, 57 with one; 4,000 of 32,768 98 and 155).
     const bool small = n <= SMALL_ROWS && q.n_rows >= 4 * sms;
     const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true, 128>(q, s, o, log_parts, device, st)
                           : small   ? run_sample_long<T, MASKED, RULES, false, 32>(q, s, o, 0, device, st)

@@ -6,6 +6,9 @@
 //     u T (4 * 2 a (1 - a) + 1.4 log2(entries / S) max(a, 1 - a) + a (additions of C and of T) + 4):
 // the equal part of the errors is shared by C and T, the other one may be all on one side.  Where a border is nearer than that to the number
 // that it is compared with, the warp works out the row in 64 bits (some hundred of 200,000 rows of 256 entries).
+//
+// What bounds them: instructions and the loads' latency.  200,000 rows of 256 bf16 logits (17 us of bytes) take 42 us without rules, 46 with min_p,
+// 52 under masks and widths as well; a warp per row, which top_k and top_p take, is 189 with top_k 8, 432 with top_p 0.9.
 #pragma once
 #include "vl_sample.cuh"
 
