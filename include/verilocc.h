@@ -420,7 +420,7 @@ typedef struct {
     double min_p;   /* 0 to 1; 0: all */
 } vl_sampling;
 
-/* Bytes of working memory of a vl_token_sample call: 0 for rows of up to 1,020 entries. */
+/* Bytes of working memory of a vl_token_sample call: 0 for rows of up to 1,000 entries. */
 uint64_t vl_sample_work(uint64_t n_rows, uint32_t n_vocab);
 
 /*

@@ -637,7 +637,7 @@ def vl_token_sample(logits, uniform, occupied=None, mask_rows=None, widths=None,
         ptr = _Torch.current(dev)
     else:
         ptr, scope = _on(stream, dev)
-    work_size = int(_lib.vl_sample_work(R, V)) if V > 1020 else 0
+    work_size = int(_lib.vl_sample_work(R, V)) if V > 1000 else 0
     with scope or _HERE:        # memory of their own: what is kept keeps nothing else
         lp = logits.new_empty(R, dtype=torch.float32)
         drawn, kept, tokens = lp.new_empty(R), lp.new_empty(R, dtype=torch.int32), lp.new_empty(R, dtype=kind)

@@ -29,6 +29,10 @@ struct SampleOut {
 cudaError_t vl_sample_f32(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st);
 cudaError_t vl_sample_f16(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st);
 cudaError_t vl_sample_bf16(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st);
+// Whether the rows are short ones, and if so the launch.
+bool vl_sample_short_f32(const LogitRows &q, const SampleRules &s, const SampleOut &o, cudaStream_t st);
+bool vl_sample_short_f16(const LogitRows &q, const SampleRules &s, const SampleOut &o, cudaStream_t st);
+bool vl_sample_short_bf16(const LogitRows &q, const SampleRules &s, const SampleOut &o, cudaStream_t st);
 
 namespace {
 

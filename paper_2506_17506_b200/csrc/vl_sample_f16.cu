@@ -1,7 +1,7 @@
-// The kernels of vl_token_sample for f16 logits (a file per type: they compile side by side).
-#include "vl_sample_launch.cuh"
+// The kernels of vl_token_sample for long rows of f16 logits (files of their own: they compile side by side).
+#include "vl_sample_long.cuh"
 
 cudaError_t vl_sample_f16(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
 {
-    return launch_sample<__half>(q, s, o, device, st);
+    return vl_sample_short_f16(q, s, o, st) ? cudaGetLastError() : launch_sample_long<__half>(q, s, o, device, st);
 }

@@ -842,4 +842,14 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     return cudaLaunchKernelEx(&cfg, rest, q, s, o, log_rest);
 }
 
+template <typename T>
+cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const SampleOut &o, int device, cudaStream_t st)
+{
+    if (!s.left) return cudaErrorInvalidValue;  // (vl_sample_work is 0 for short rows alone)
+    const bool masked = q.occupied || q.widths;
+    if (s.top_k || s.top_p < 1.0 || s.min_p > 0.0)
+        return masked ? launch_sample_long<T, true, true>(q, s, o, device, st) : launch_sample_long<T, false, true>(q, s, o, device, st);
+    return masked ? launch_sample_long<T, true, false>(q, s, o, device, st) : launch_sample_long<T, false, false>(q, s, o, device, st);
+}
+
 }  // namespace

@@ -568,16 +568,22 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 4 ? 4 : 3) : NV
     }
 }
 
-// The vectors of a lane for rows of at most n vectors that a warp holds (a lane for every word of a mask up to four of them).
-template <typename F>
+// The vectors of a lane for rows of at most n vectors that a warp holds with top_k or top_p: 1,024 entries and some (a lane for every word of a
+// mask); longer ones are read twice instead.
+template <typename T, typename F>
 bool warp_shape(uint32_t n, F &&f)
 {
     using std::integral_constant;
     if (n <= 32) f(integral_constant<int, 1>{});
     else if (n <= 64) f(integral_constant<int, 2>{});
     else if (n <= 128) f(integral_constant<int, 4>{});
-    else if (n <= 256) f(integral_constant<int, 8>{});
-    return n <= 256;
+    else if constexpr (sizeof(T) == 4) {
+        if (n > 256) return false;
+        f(integral_constant<int, 8>{});
+    } else {
+        return false;
+    }
+    return true;
 }
 
 template <typename T, bool MASKED, bool ALIGNED>
@@ -600,7 +606,16 @@ bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleO
         else k_sample_warp<T, MASKED, ALIGNED, false, NV><<<grid, SHORT_WARPS * 32, 0, st>>>(q, s, o);
         g_vl_launches.fetch_add(1);
     };
-    return order ? warp_shape(n, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
+    return order ? warp_shape<T>(n, run_warp) : short_shape<false, ALIGNED>(n, q.W, run);
+}
+
+template <typename T>
+bool launch_sample_short(const LogitRows &q, const SampleRules &s, const SampleOut &o, cudaStream_t st)
+{
+    bool aligned;
+    const uint32_t n = row_vectors(q, sizeof(T), &aligned);
+    if (q.occupied || q.widths) return aligned ? launch_sample_short<T, true, true>(q, s, o, n, st) : launch_sample_short<T, true, false>(q, s, o, n, st);
+    return aligned ? launch_sample_short<T, false, true>(q, s, o, n, st) : launch_sample_short<T, false, false>(q, s, o, n, st);
 }
 
 }  // namespace

@@ -1,0 +1,4 @@
+// The kernels of vl_token_sample for short rows of f32 logits (files of their own: they compile side by side).
+#include "vl_sample_short.cuh"
+
+bool vl_sample_short_f32(const LogitRows &q, const SampleRules &s, const SampleOut &o, cudaStream_t st) { return launch_sample_short<float>(q, s, o, st); }
