@@ -39,6 +39,7 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr uint32_t LEAST_KEY = 0x00800000u;  // of the lowest number; minus infinity lies below
+constexpr uint32_t ZERO_KEY = 0x80000000u;   // of 0 (of both signs)
 
 __device__ __forceinline__ void put_sample(const SampleOut &o, uint64_t r, int64_t token, float logprob, float drawn, uint32_t kept)
 {
@@ -576,7 +577,8 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
     const uint32_t lowest = ordered(fmaxf(__double2float_ru(M + rules.drop), LOWEST));
     const bool by_min = rules.min_p > 0.0 && cut < lowest;
     if (by_min) {
-        cut = lowest - 1;
+        // (the key below that of 0 is the one of -0, which no entry has and which as a logit is equal to 0)
+        cut = lowest - (lowest == ZERO_KEY ? 2 : 1);
         ties = 0;
         high = 0.0;
         high_count = 0;
@@ -644,7 +646,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         // the run that the number falls into: the first up to whose end the sum is above it, or the last with something kept
         const double at = (double)rules.uniform[r] * total;
         double up = 0.0;
-        mine = 0xFFFFFFFFu;
+        mine = 0;
         bool hit = false;
         runs([&](uint32_t w0, double own, double incl, uint32_t b, uint32_t) {
             const uint32_t some = __ballot_sync(0xffffffffu, own > 0.0), past = __ballot_sync(0xffffffffu, own > 0.0 && up + incl > at);
@@ -713,7 +715,10 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
         base += __shfl_sync(0xffffffffu, up, 31);
         if (past) break;
     }
-    if (lane == 0) {
+    if (lane == 0 && token == 0xFFFFFFFFu) {  // (the largest entry is always kept: no weight at all is an error, told as what is no number)
+        const float nan = __int_as_float(0x7fc00000);
+        put_sample(o, r, -1, nan, nan, 0);
+    } else if (lane == 0) {
         const double z = scale * ((double)to_f32(x.row[token]) - M);
         put_sample(o, r, token, (float)(z - log(S)), (float)(z - log(total)), kept);
     }
