@@ -547,8 +547,8 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
         const float low = RULES ? from_ordered(__reduce_min_sync(0xffffffffu, lane < warps ? ordered(s_min[lane]) : 0xFFFFFFFFu)) : 0.0f;
         count = RULES ? 0u : __reduce_add_sync(0xffffffffu, lane < warps ? s_count[lane] : 0u);
         const double cM = (double)c * (double)M;
-        auto relative = [&](uint32_t i) {  // (a warp's sums are relative to its rounded product)
-            return s_ref[i] == -inf ? 0.0 : s_sum[i] * exp_below_1(((double)__fmul_rn(s_ref[i], c) - cM) * LN2_64, s_table);
+        auto relative = [&](uint32_t i) {  // (a warp's sums are relative to its rounded product; without one they are 0, or no number)
+            return s_ref[i] == -inf ? s_sum[i] : s_sum[i] * exp_below_1(((double)__fmul_rn(s_ref[i], c) - cM) * LN2_64, s_table);
         };
         double S = 0.0;
         for (uint32_t i0 = 0; i0 < parts * RECS; i0 += 32) {
