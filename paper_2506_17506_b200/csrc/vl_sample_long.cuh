@@ -477,8 +477,9 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
                 if (__any_sync(0xffffffffu, m > limit)) {
                     const float top = from_ordered(__reduce_max_sync(0xffffffffu, ordered(m)));
                     limit = top + margin;
-                    if (top * c > -FAR_OUT) {  // (below, every power of two is 0 as it is)
-                        total *= ref == -inf ? 0.0 : (double)ex2(step_down(ref, top, c));
+                    // twice as far below as the largest logit may lie: what has no reference there is 0 as it is, and next to any row's largest
+                    if (top * c > -2.0f * FAR_OUT) {
+                        total *= ref == -inf ? 0.0 : (double)ex2(__fsub_rn(__fmul_rn(ref, c), __fmul_rn(top, c)));
                         ref = top;
                     }
                 }
