@@ -435,6 +435,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             __syncthreads();  // (the last sums have been read)
             // in 64 bits: the whole sum, and what is above these steps; and which keys lie in them, with a list of the first ones of each block
             uint32_t *const list_keys = reinterpret_cast<uint32_t *>(held + TEAM_HELD * NT);
+            static_assert(4 * LISTED * 4 + 3 * LISTED * 8 <= 16 * NT * 8, "fits the runs' sums");
             double *const list_weights = reinterpret_cast<double *>(list_keys + 4 * LISTED);
             double sum = 0.0;
             Three t{0u, 0xFFFFFFFFu, 0u};
@@ -513,11 +514,22 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                             front += m;
                         }
                         __syncthreads();
-                        uint32_t best = 0;
+                        // in falling order, as the order in which they were listed is any: equal ones weigh the same
+                        uint32_t *const sorted_keys = list_keys + 3 * LISTED;
+                        double *const sorted_weights = list_weights + 2 * LISTED;
                         if (threadIdx.x < t.sum) {
                             const uint32_t key = all_keys[threadIdx.x];
+                            uint32_t rank = 0;
+                            for (uint32_t j = 0; j < t.sum; ++j) rank += all_keys[j] > key || (all_keys[j] == key && j < threadIdx.x);
+                            sorted_keys[rank] = key;
+                            sorted_weights[rank] = all_weights[threadIdx.x];
+                        }
+                        __syncthreads();
+                        uint32_t best = 0;
+                        if (threadIdx.x < t.sum) {
+                            const uint32_t key = sorted_keys[threadIdx.x];
                             double up = above;
-                            for (uint32_t j = 0; j < t.sum; ++j) up += all_keys[j] >= key ? all_weights[j] : 0.0;
+                            for (uint32_t j = 0; j < t.sum && sorted_keys[j] >= key; ++j) up += sorted_weights[j];
                             if (up >= need) best = key;
                         }
                         best = __reduce_max_sync(0xffffffffu, best);
