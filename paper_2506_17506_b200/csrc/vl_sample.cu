@@ -3,7 +3,7 @@
 
 #include "vl_sample.cuh"
 
-// (rows of that many entries are short ones, whatever their type and wherever they start: at most 250 vectors of fp32, 126 of 16 bits)
+// (rows of that many entries are short ones, whatever their type and wherever they start: at most 251 vectors of fp32, 126 of 16 bits)
 extern "C" uint64_t vl_sample_work(uint64_t n_rows, uint32_t n_vocab) { return n_vocab <= 1000 ? 0 : 4 * n_rows; }
 
 extern "C" int vl_token_sample(int device, const vl_logits *x, const vl_sampling *rules, const float *d_uniform, void *d_tokens,

@@ -38,6 +38,10 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+// A weight of 32 bits is within (4 + POWER_ERROR |y|) u of its value relatively, u = 2^-24, y its power of two: scale log2 e is a rounded
+// product (u) with a rounded constant (0.22 u), a multiply-add makes y of it (u), and ln 2 times these 2.22 u is 1.54.
+constexpr float POWER_ERROR = 1.6f;
+
 constexpr uint32_t LEAST_KEY = 0x00800000u;  // of the lowest number; minus infinity lies below
 constexpr uint32_t ZERO_KEY = 0x80000000u;   // of 0 (of both signs)
 
@@ -392,7 +396,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             cut = search(all ? least : cut + 1, most, false, &above, needed);
         } else {
             // Where the cut lies as far as 32 bits tell it: the logits in 2^28 steps below the largest one, sixteen runs of steps at a time.  A sum of
-            // 32-bit terms is within NARROW of its value: (4 + 1.4 |y|) u of a weight, |y| up to 40 for what is not nothing, a thread's
+            // 32-bit terms is within NARROW of its value: (4 + 1.6 |y|) u of a weight, |y| up to 40 for what is not nothing, a thread's
             // additions to a bin (TEAM_HELD vectors; longer rows are not narrowed down).
             constexpr double NARROW = 2e-5;
             constexpr uint32_t LISTED = NT;  // entries that are looked at one by one

@@ -10,9 +10,9 @@
 // A row is left to k_sample_rest where a border is nearer to what it is compared with than the 32-bit terms are known (eps, below), where more
 // than CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
 //
-// eps: a weight is within (4 + 1.4 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
+// eps: a weight is within (4 + 1.6 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
 // passes by more than 3; a lane's 32 entries go through 8 additions, and 64 bits hold what these make.  The mean of |y| relative to the largest logit
-// is at most log2(V / S).  S is therefore known to eps S, eps = (16 + 1.4 (log2(V / S) + 3)) u, and a border between two parts of it as in the
+// is at most log2(V / S).  S is therefore known to eps S, eps = (16 + 1.6 (log2(V / S) + 3)) u, and a border between two parts of it as in the
 // short rows.
 //
 // What bounds it: the pass reads the logits once (1,024 rows of 131,072 bf16: 42 us after the median of the rows, 65 after the last, for a floor of
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) k_sample_long(const LogitRows q
             if (part == 0 && tid == 0) put_sample(o, r, -1, -inf, -inf, 0);
             settled = true;
         } else if (number) {
-            const float mean = 1.4f * __log2f((float)q.V / (float)S) + 5.0f;  // (of what a weight's power of two costs; the references add up to 3)
+            const float mean = POWER_ERROR * (__log2f((float)q.V / (float)S) + 3.1f);  // (of what a weight's power of two costs; the references add up to 3)
             const double eps = (double)((16.0f + mean) * 0x1p-24f);
             // what a border between two parts of S is known to
             const double slack = S * (double)(0x1p-24f * (8.0f * u * (1.0f - u) + mean * fmaxf(u, 1.0f - u) + 24.0f * u + 4.0f));

@@ -1,9 +1,9 @@
 // Drawing from short rows: a group of lanes, or a warp, holds a row in registers.
 //
-// Weights and sums are in 32 bits, u = 2^-24.  A weight is within (4 + 1.4 |y|) u of its value relatively, y its power of two (two
-// roundings in y, and the exponential's own error), and the mean of |y| over a row's probabilities is at most log2(entries / S), S the sum relative to
+// Weights and sums are in 32 bits, u = 2^-24.  A weight is within (4 + 1.6 |y|) u of its value relatively, y its power of two (its
+// roundings and the scale's, and the exponential's own error), and the mean of |y| over a row's probabilities is at most log2(entries / S), S the sum relative to
 // the largest one (their entropy is at most that of equal ones).  With C the sum up to a border and T the whole one, C - a T is then known to
-//     u T (4 * 2 a (1 - a) + 1.4 log2(entries / S) max(a, 1 - a) + a (additions of C and of T) + 4):
+//     u T (4 * 2 a (1 - a) + 1.6 log2(entries / S) max(a, 1 - a) + a (additions of C and of T) + 4):
 // the equal part of the errors is shared by C and T, the other one may be all on one side.  Where a border is nearer than that to the number
 // that it is compared with, the warp works out the row in 64 bits (some hundred of 200,000 rows of 256 entries).
 //
@@ -159,7 +159,7 @@ __device__ __forceinline__ bool draw(const uint4 (&raw)[NV], const Keep<NV> &kee
     // round by round: the group's vectors that the number falls into, and what lies in front of them
     constexpr float ADDS = EPV<T> / 2 + NV + (G == 4 ? 2 : G == 8 ? 3 : G == 16 ? 4 : 5), MORE = ADDS - EPV<T> / 2 + EPV<T> + 1;  // of T, and of C beyond
     const float at = u * T_all;
-    const float margin = T_all * 0x1p-24f * (8.0f * u * (1.0f - u) + 1.4f * fmaxf(u, 1.0f - u) * __log2f((float)x.V / S) + u * (2.0f * ADDS + MORE) + 4.5f);
+    const float margin = T_all * 0x1p-24f * (8.0f * u * (1.0f - u) + POWER_ERROR * fmaxf(u, 1.0f - u) * __log2f((float)x.V / S) + u * (2.0f * ADDS + MORE) + 4.5f);
     float base = 0.0f, up = 0.0f, own = 0.0f;
     uint4 vector = raw[0];
     uint32_t ties = TIES ? keep.ties[0] : 0u, turn = 0;
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(SHORT_WARPS * 32, FEW ? (NV <= 4 ? 4 : 3) : NV
         if (s.top_p < 1.0) {
             // Where the cut lies: weights in 32 runs of half a power of two below the largest one, added up by every lane for its own entries and by a
             // lane for each run.  What is in the run of the cut, if a warp can hold it, is put in order; else the halves begin from it.
-            const float need = (float)s.top_p * among, margin = among * 0x1p-24f * ((float)(NV * EPV<T>) + 50.0f + 1.4f * __log2f((float)q.V));  // (a lane's additions, the warp's, and the weights' errors)
+            const float need = (float)s.top_p * among, margin = among * 0x1p-24f * ((float)(NV * EPV<T>) + 50.0f + POWER_ERROR * __log2f((float)q.V));  // (a lane's additions, the warp's, and the weights' errors)
             uint32_t lo = cut, hi = most + 1;
             float above = 0.0f;
             const float over = cut < LEAST_KEY ? -inf : from_ordered(cut);
