@@ -759,31 +759,31 @@ def _gradients(where, grads, outs):
         if outs:
             _refuse(where, "outs: one for every tensor")
         return array.array("Q", (0,)), 0, torch.cuda.current_device()
-    dev = grads[0].get_device()
-    types = [g.dtype for g in grads]
-    kinds = list(map(_Torch.kinds.get, types))
     what = "grads: dense CUDA tensors of float32, float16 or bfloat16 on one device"
-    if dev < 0 or None in kinds or set(map(each.get_device, grads)) != {dev}:
-        _refuse(where, what)
     try:
+        dev = each.get_device(grads[0])
+        types = [g.dtype for g in grads]
+        kinds = list(map(_Torch.kinds.get, types))
+        if dev < 0 or None in kinds or set(map(each.get_device, grads)) != {dev}:
+            _refuse(where, what)
         at, n = list(map(each.data_ptr, grads)), list(map(each.numel, grads))
         plain = all(map(each.is_contiguous, grads))
         if not plain and not all(map(_dense, grads)):
             _refuse(where, what)
-    except (RuntimeError, NotImplementedError):     # (sparse ones have no memory of their own)
+        to = at
+        if outs is not None:
+            what = "outs: tensors of the gradients' types and sizes, with their elements in the same order"
+            if len(outs) != len(grads) or [o.dtype for o in outs] != types or set(map(each.get_device, outs)) != {dev}:
+                _refuse(where, what)
+            if list(map(each.numel, outs)) != n:
+                _refuse(where, what)
+            if not (plain and all(map(each.is_contiguous, outs))):
+                for o, g in zip(outs, grads):
+                    if not (o.is_contiguous() and g.is_contiguous()) and (o.shape != g.shape or (o.stride() != g.stride() and g.numel() > 1)):
+                        _refuse(where, what)
+            to = list(map(each.data_ptr, outs))
+    except (RuntimeError, AttributeError, TypeError):   # (sparse ones have no memory of their own; None is no tensor)
         _refuse(where, what)
-    to = at
-    if outs is not None:
-        what = "outs: tensors of the gradients' types and sizes, with their elements in the same order"
-        if len(outs) != len(grads) or [o.dtype for o in outs] != types or set(map(each.get_device, outs)) != {dev}:
-            _refuse(where, what)
-        if list(map(each.numel, outs)) != n:
-            _refuse(where, what)
-        if not (plain and all(map(each.is_contiguous, outs))):
-            for o, g in zip(outs, grads):
-                if not (o.is_contiguous() and g.is_contiguous()) and (o.shape != g.shape or (o.stride() != g.stride() and g.numel() > 1)):
-                    _refuse(where, what)
-        to = list(map(each.data_ptr, outs))
     # (a descriptor is four words: two addresses, the size, and the type in the low half of the last)
     words = [0] * (4 * len(grads))
     words[0::4], words[1::4], words[2::4], words[3::4] = at, to, n, kinds
@@ -821,11 +821,13 @@ def vl_clip_grads(grads, max_norm: float, scale: float = 1.0, outs=None, sum_squ
     the tensors' device), without waiting."""
     where = "vl_clip_grads"
     grads = grads if isinstance(grads, (list, tuple)) else list(grads)
+    if outs is not None and not isinstance(outs, (list, tuple)) and hasattr(outs, "__iter__"):
+        outs = list(outs)
     t, n, dev = _gradients(where, grads, outs)
     torch = _Torch.torch
     given = 0
     if sum_squares is not None:
-        if sum_squares.get_device() != dev or sum_squares.dtype != torch.float64 or sum_squares.numel() != 1:
+        if not isinstance(sum_squares, torch.Tensor) or sum_squares.get_device() != dev or sum_squares.dtype != torch.float64 or sum_squares.numel() != 1:
             _refuse(where, f"sum_squares: one float64 number on cuda:{dev}")
         given = sum_squares.data_ptr()
     scope = None
