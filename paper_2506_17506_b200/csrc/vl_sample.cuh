@@ -439,8 +439,11 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
             __syncthreads();  // (the last sums have been read)
             // in 64 bits: the whole sum, and what is above these steps; and which keys lie in them, with a list of the first ones of each block
             uint32_t *const list_keys = reinterpret_cast<uint32_t *>(held + TEAM_HELD * NT);
-            static_assert(4 * LISTED * 4 + 3 * LISTED * 8 <= 16 * NT * 8, "fits the runs' sums");
-            double *const list_weights = reinterpret_cast<double *>(list_keys + 4 * LISTED);
+            static_assert(4 * LISTED * 4 + 2 * LISTED * 8 <= 16 * NT * 8, "fits the runs' sums");
+            // (the order in which entries are listed is any: their weights, at most 1, are added up as whole numbers of 2^-54, LISTED of which are below
+            // 2^64, so that it makes no difference; what that leaves out is below 2^-45, next to sums of 1 and more.  By their order instead, as 64-bit
+            // numbers: 165 us for 157, 1,024 rows of 131,072 bf16 logits with top_p 0.95)
+            unsigned long long *const list_weights = reinterpret_cast<unsigned long long *>(list_keys + 4 * LISTED);
             double sum = 0.0;
             Three t{0u, 0xFFFFFFFFu, 0u};
             each_vector([&](const uint4 &raw) {
@@ -461,7 +464,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                         const uint32_t place = atomicAdd(&mem->listed, 1u);
                         if (place < LISTED) {
                             list_keys[place] = key;
-                            list_weights[place] = w[i];
+                            list_weights[place] = __double2ull_rn(w[i] * 0x1p54);
                         }
                     }
                 }
@@ -507,7 +510,7 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                 } else if (t.sum <= LISTED) {  // the first block looks at all of them
                     if (part == 0) {
                         uint32_t *const all_keys = list_keys + 2 * LISTED;
-                        double *const all_weights = list_weights + LISTED;
+                        unsigned long long *const all_weights = list_weights + LISTED;
                         uint32_t front = 0;
                         for (uint32_t p = 0; p < parts; ++p) {
                             const uint32_t m = *cg::this_cluster().map_shared_rank(&mem->listed, p);
@@ -518,23 +521,12 @@ __device__ __noinline__ void sample_row_64(const LogitRows &q, const SampleRules
                             front += m;
                         }
                         __syncthreads();
-                        // in falling order, as the order in which they were listed is any: equal ones weigh the same
-                        uint32_t *const sorted_keys = list_keys + 3 * LISTED;
-                        double *const sorted_weights = list_weights + 2 * LISTED;
-                        if (threadIdx.x < t.sum) {
-                            const uint32_t key = all_keys[threadIdx.x];
-                            uint32_t rank = 0;
-                            for (uint32_t j = 0; j < t.sum; ++j) rank += all_keys[j] > key || (all_keys[j] == key && j < threadIdx.x);
-                            sorted_keys[rank] = key;
-                            sorted_weights[rank] = all_weights[threadIdx.x];
-                        }
-                        __syncthreads();
                         uint32_t best = 0;
                         if (threadIdx.x < t.sum) {
-                            const uint32_t key = sorted_keys[threadIdx.x];
-                            double up = above;
-                            for (uint32_t j = 0; j < t.sum && sorted_keys[j] >= key; ++j) up += sorted_weights[j];
-                            if (up >= need) best = key;
+                            const uint32_t key = all_keys[threadIdx.x];
+                            unsigned long long up = 0;
+                            for (uint32_t j = 0; j < t.sum; ++j) up += all_keys[j] >= key ? all_weights[j] : 0ull;
+                            if (above + (double)up * 0x1p-54 >= need) best = key;
                         }
                         best = __reduce_max_sync(0xffffffffu, best);
                         if (lane == 0) mem->best[threadIdx.x >> 5] = best;
