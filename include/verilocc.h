@@ -412,7 +412,7 @@ int vl_token_logprobs_backward(int device, const vl_logits *x, const float *d_ro
  * numbers, the kept entries are the shortest of these prefixes: the first top_k; those whose sum of w reaches top_p times that of the first
  * top_k; those with w >= min_p.  With T the sum of w over the kept ones, the token of row r is the lowest kept entry i for which the sum of w
  * over the kept entries 0..i is above d_uniform[r] * T.  What is decided is what 64-bit arithmetic decides (a sum within 2^-40 of what it is
- * compared with may count as either side of it).
+ * compared with, and a w as near to min_p, may count as either side of it).
  */
 typedef struct {
     uint32_t top_k; /* 0: all */

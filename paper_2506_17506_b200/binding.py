@@ -818,7 +818,8 @@ def vl_clip_grads(grads, max_norm: float, scale: float = 1.0, outs=None, sum_squ
     place, or into ``outs`` (tensors of the same types and sizes, contiguous or of the gradient's strides; none shares memory with another
     one, or with a gradient that is not its own).  With ``sum_squares`` (float64 scalar tensor: of all ranks together) the norm is its root.  A norm that is no finite number
     makes every result 0.  Returns Clipped(norm, factor: float32 scalar tensors; outs).  On ``stream`` (default: the current one of
-    the tensors' device), without waiting."""
+    the tensors' device), without waiting.  Like all results that are written to given memory, these leave the tensors' version numbers
+    as they were."""
     where = "vl_clip_grads"
     grads = grads if isinstance(grads, (list, tuple)) else list(grads)
     if outs is not None and not isinstance(outs, (list, tuple)) and hasattr(outs, "__iter__"):

@@ -352,7 +352,8 @@ cudaError_t clip(uint32_t n, const vl_gradient *t, const Total &total, bool over
 }
 
 // Sixteen vectors of a thread in flight where there are some rounds of them for every block; eight where that would leave blocks idle.
-// us with 8 and 16: norm of 400 MB 92, 63; norm of 0.5 MB 3.7, 4.0; clipping 25 MB to 25 MB 18.6, 22; 1.2 GB to 1.2 GB 599, 580.
+// us with 8 and 16, 40 tensors of bf16: norm of 25, 100, 200, 400 MB 7.7, 7.2; 23, 17; 45, 35; 88, 63 (and of 0.5 MB 3.7, 4.0); clipping these to as many
+// bytes elsewhere 21, 27; 63, 84; 118, 140; 228, 249; 1.2 GB of fp32 599, 580.
 bool large(uint32_t n, const vl_gradient *t)
 {
     uint64_t bytes = 0;

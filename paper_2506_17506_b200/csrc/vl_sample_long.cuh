@@ -1,14 +1,14 @@
 // Drawing from long rows: one pass over the row, and a second look at what matters of it.
 //
-// A block of four warps, or a cluster of such blocks, is at a row; each warp has a run of the row's vectors and cuts it into eight segments.
+// A block of four warps, a cluster of such blocks, or one warp is at a row; each warp has a run of the row's vectors and cuts it into eight segments.
 // The pass keeps for every segment the sum of its weights (in 64 bits from 32 entries of a lane in 32), and for every lane of it the largest
-// logit: 1,024 groups of a block.
+// logit: 1,024 groups of a block, 256 of a warp alone.
 //   No rules: the sums tell the segment that the number falls into, and that one is read again.
 //   top_k, top_p, min_p: the groups' largest logits, counted in 128 steps below the largest one, bound the cut from below: top_k groups with
 //   such a logit, or groups whose largest entries alone have weight enough, mean that the cut is no lower.  The groups that reach the bound are
 //   read again, and what reaches it is gathered, put in order, and the rules are applied in 64 bits.
 // A row is left to k_sample_rest where a border is nearer to what it is compared with than the 32-bit terms are known (eps, below), where more
-// than CAP entries reach the bound, or where a logit is no number or beyond the range of the sums.
+// than CAP entries reach the bound (1,024; 256 of a warp alone), or where a logit is no number or beyond the range of the sums.
 //
 // eps: a weight is within (4 + 1.6 |y|) u of its value, u = 2^-24, y its power of two relative to the warp's reference, which no entry
 // passes by more than 3; a lane's 32 entries go through 8 additions, and 64 bits hold what these make.  The mean of |y| relative to the largest logit
@@ -812,11 +812,14 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     const uint64_t sms = (uint64_t)vl_device_sm_count(device);
     // Blocks of a row: more of them shorten the pass and cost barriers of 1 us; they pay where most multiprocessors would be idle and a block
     // keeps 4,096 vectors (2,048 for a handful of rows).  Device time in us with 1, 2, 4, 8 blocks, bf16, top_k 50 and top_p 0.9: one row of 131,072
-    // 29, 26, 20, 18; 100 rows 33, 30, 26, 28; 300 rows 40, 39, 51, 69; 100 rows of 32,768 18.6, 21, 21, 24.
+    // 29, 26, 20, 18; 100 rows 33, 30, 26, 28; 300 rows 40, 39, 51, 69; 100 rows of 32,768 18.6, 21, 21, 24.  With 4,096 and with 2,048, top_p 0.95: one
+    // row of 131,072 20.5, 18.4, eight 21.1, 19.3, 64 25.4, 25.3; one row of 32,768 14.8, 17.4.
     const uint32_t least = q.n_rows <= 8 ? 2048 : 4096;
     while ((1u << log_parts) < LD_PARTS && q.n_rows << (log_parts + 1) <= sms * 3 && n >> (log_parts + 1) >= least) ++log_parts;
     // One warp at a row where a row is short and there are rows for all the places: it has no barriers, and 28 rows are at their ends at once
-    // instead of seven (5,000 rows of 8,192 bf16 logits 76 us with four warps at each, 57 with one; 4,000 of 32,768 98 and 155).
+    // instead of seven (5,000 rows of 8,192 bf16 logits 76 us with four warps at each, 57 with one; 4,000 of 32,768 98 and 155).  It has a quarter of
+    // the groups and of the list, which a large top_k does not fit: 5,000 of 8,192 with top_k 50, 100, 150, 200, 300 59, 117, 273, 1,197, 1,211 with one,
+    // 81, 130, 177, 218, 1,219 with four.
     const bool small = n <= SMALL_ROWS && q.n_rows >= 4 * sms;
     const cudaError_t e = log_parts ? run_sample_long<T, MASKED, RULES, true, 128>(q, s, o, log_parts, device, st)
                           : small   ? run_sample_long<T, MASKED, RULES, false, 32>(q, s, o, 0, device, st)
@@ -826,7 +829,8 @@ cudaError_t launch_sample_long(const LogitRows &q, const SampleRules &s, const S
     if (const cudaError_t f = allow_smem<rest, (int)RS_BYTES>(device); f != cudaSuccess) return f;
     // Blocks at a row: where few rows can be left, or a thread would have more than eight vectors of it.  A pass over a row takes a block 2 us and
     // more whatever the row is, and a cluster another 1: 5,000 rows of 8,192 bf16 logits of which a third is left take
-    // 213 us with one block at each, 953 with four.
+    // 213 us with one block at each, 953 with four.  Few broad rows of 131,072 bf16 logits, four blocks and eight: one row 66, 55, eight 71, 55, twelve 74,
+    // 59, sixteen (for which there is no room at once) 75, 92.
     const uint32_t log_rest = q.n_rows <= 8 && n >= 2048 ? 3 : n < 4096 ? 0 : n < 8192 ? 1 : 2;
     const uint64_t clusters = (uint64_t)vl_device_sm_count(device) >> log_rest;
     cudaLaunchAttribute at[2]{};
